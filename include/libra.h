@@ -13,8 +13,8 @@
  * ---------------------------------
  * - All tensors are borrowed pointers owned by the caller.  "device" pointers must be
  *   HIP device memory of the current device; "host" pointers are ordinary host memory.
- * - Handles (libra_kv_layout, libra_plan, libra_trie) are created and destroyed by the
- *   library.  Layouts and plans are immutable after creation, except that a plan
+ * - Handles (libra_kv_layout, libra_plan, libra_rotary, libra_trie) are created and
+ *   destroyed by the library.  Layouts, rotaries and plans are immutable after creation, except that a plan
  *   remembers (under a lock) which workspace its tables were last uploaded to, so calls
  *   on different streams with distinct workspaces and outputs may share a plan; a prefix
  *   tree grows by libra_trie_insert and must not be inserted into while another thread
@@ -28,7 +28,7 @@
  *   single-token and chunk rows creates the device's auxiliary stream (default
  *   priority, kept until the process ends); libra_plan_destroy returns image and events
  *   to the pool.  Decode, append and upload calls allocate nothing.
- * - Host-only entry points (plan construction, cost evaluator, RolloutDP, prefix tree,
+ * - Host-only entry points (plan construction, libra_rotary_create / _get, cost evaluator, RolloutDP, prefix tree,
  *   routing, libra_kv_reshard_host) touch no GPU; the reshard may use up to 8 host
  *   threads for large runs.
  * - Every entry point returns a libra_status; nothing aborts, prints or throws.  On an
@@ -69,11 +69,16 @@ enum {
   LIBRA_UNIT_INTS = 12      /* int32 fields per plan unit */
 };
 
-enum { LIBRA_DTYPE_BF16 = 0 };
+enum {
+  LIBRA_DTYPE_BF16 = 0,     /* the cache's type, and that of every attention call */
+  LIBRA_DTYPE_FP16 = 1,     /* libra_rotary_apply only */
+  LIBRA_DTYPE_FP32 = 2      /* libra_rotary_apply only */
+};
 enum { LIBRA_MODE_DECODE = 0, LIBRA_MODE_APPEND = 1 };
 
 typedef struct libra_kv_layout_s* libra_kv_layout;
 typedef struct libra_plan_s* libra_plan;
+typedef struct libra_rotary_s* libra_rotary;
 
 /* Human-readable name of a status code (static storage). */
 const char* libra_status_string(libra_status status);
@@ -431,6 +436,117 @@ libra_status libra_append_attn(libra_kv_layout layout, libra_plan plan, const vo
                                void* stream);
 
 /* ------------------------------------------------------------------------------ */
+/* Rotary positions                                                                */
+/* ------------------------------------------------------------------------------ */
+/*
+ * The first R = rotary_dim channels of a head are R / 2 pairs (x1, x2); pair j of a row at
+ * position p is turned by p theta_j and scaled by the amplitude A:
+ *
+ *   y1 = A (x1 cos(p theta_j) - x2 sin(p theta_j)),
+ *   y2 = A (x2 cos(p theta_j) + x1 sin(p theta_j)),
+ *
+ * the pairs being channels (j, j + R / 2) (LIBRA_ROTARY_HALF) or (2 j, 2 j + 1)
+ * (LIBRA_ROTARY_INTERLEAVED); channels from R on are copied bit for bit.  theta_j =
+ * base^(-2 j / R), or frequencies[j] where the caller gives them.  Long contexts scale it
+ * (s = factor):
+ *
+ *   LIBRA_ROTARY_LINEAR  theta_j / s (positions interpolated);
+ *   LIBRA_ROTARY_BASE    base replaced by base * s^(R / (R - 2)): the slowest pair turns s
+ *                        times slower, the fastest as before;
+ *   LIBRA_ROTARY_BANDS   theta_j (w + (1 - w) / s), w = clamp((n_j - slow) / (fast - slow),
+ *                        0, 1), n_j = original_length * |theta_j| / 2 pi: pairs that make
+ *                        more than `fast` turns over the original context keep their
+ *                        frequency, those with fewer than `slow` are interpolated.
+ *
+ * Frequencies are taken in extended precision and angles kept modulo one turn in 64-bit
+ * fixed point, so the angle of a position of 2^31 is still good to 1e-9 turns.  Cosine and
+ * sine are float32 (within 1.2e-7 of the exact ones, times A), the products too, and the
+ * result is rounded once to the output's type.
+ */
+enum { LIBRA_ROTARY_HALF = 0, LIBRA_ROTARY_INTERLEAVED = 1 };
+enum {
+  LIBRA_ROTARY_PLAIN = 0,
+  LIBRA_ROTARY_LINEAR = 1,
+  LIBRA_ROTARY_BASE = 2,
+  LIBRA_ROTARY_BANDS = 3
+};
+
+typedef struct libra_rotary_desc {
+  int32_t head_dim;         /* channels per head, in [2, 512]; 128 for cached heads */
+  int32_t rotary_dim;       /* R: even, in [2, min(head_dim, 256)]; 0 = head_dim */
+  int32_t pairing;          /* LIBRA_ROTARY_HALF or _INTERLEAVED */
+  int32_t scaling;          /* LIBRA_ROTARY_PLAIN, _LINEAR, _BASE or _BANDS */
+  double base;              /* > 0; not read where frequencies are given */
+  double factor;            /* s > 0; not read by _PLAIN */
+  int64_t original_length;  /* _BANDS: the context length before scaling, > 0 */
+  double fast;              /* _BANDS: turns above which a pair is not scaled */
+  double slow;              /* _BANDS: turns below which it is scaled by s; 0 <= slow < fast */
+  double amplitude;         /* A > 0; 0 = 1 */
+  const double* frequencies; /* host, R / 2 values of theta_j (|theta| <= 1e6; read during
+                               the call only), or NULL; not with _BASE */
+} libra_rotary_desc;
+
+/* Validates the descriptor and returns a handle (host memory only; any device's calls may
+ * use it). */
+libra_status libra_rotary_create(const libra_rotary_desc* desc, libra_rotary* out);
+void libra_rotary_destroy(libra_rotary rotary);
+/* Channels per head, R, the R / 2 scaled frequencies and A (as used, rounded to float32);
+ * each may be NULL. */
+libra_status libra_rotary_get(libra_rotary rotary, int32_t* head_dim, int32_t* rotary_dim,
+                              double* frequencies, double* amplitude);
+
+/* Turns rows x num_heads vectors of head_dim elements.  Element (r, h, d) of x lies at
+ * x + r * x_row_stride + h * x_head_stride + d, of out likewise (strides in elements; any
+ * order of rows and heads; x's strides may be 0, out's vectors must not overlap).  positions:
+ * device int32 [rows], any value.  backward != 0 gives the gradient's pass, the turn by the
+ * negative angle with the same amplitude: dx from dy.  out may be x (in place, the same
+ * strides); otherwise the two must not overlap.  dtype: LIBRA_DTYPE_BF16, _FP16 or _FP32, of
+ * x and out; pointers aligned to it. */
+libra_status libra_rotary_apply(libra_rotary rotary, int32_t dtype, const void* x,
+                                int64_t x_row_stride, int64_t x_head_stride,
+                                const int32_t* positions, int64_t rows, int32_t num_heads,
+                                int32_t backward, void* out, int64_t out_row_stride,
+                                int64_t out_head_stride, void* stream);
+
+/* Writes new rows into the cache, keys turned on the way: row r goes to slots[r] = page * 16
+ * + slot (device int64 [rows]).  A row whose slot lies outside [0, 16 num_pages) is padding:
+ * nothing of it is written, here or in q_out.  Slots must be distinct (repeated slots race).
+ * No plan is needed, so a captured call serves every later step whose slots and positions
+ * are written to the same memory; libra_decode_attn reads what it wrote.
+ *
+ * k_new, v_new: device bf16, row r's heads at r * k_row_stride (v_row_stride) elements, 128
+ * apart, so that slices of one projection can be given: strides >= num_kv_heads * 128 and
+ * multiples of 8, pointers 16-byte aligned.  rotary NULL: keys are written as they are and
+ * positions is not read; else positions: device int32 [rows].
+ * q (may be NULL, with q_out): device bf16 rows of num_q_heads heads at q_row_stride; turned
+ * to q_out, [rows][num_q_heads][128], which may be q if its rows are dense.  Needs a rotary. */
+libra_status libra_kv_append(libra_kv_layout layout, libra_rotary rotary,
+                             const int32_t* positions, const int64_t* slots, int64_t rows,
+                             const void* q, int64_t q_row_stride, int32_t num_q_heads,
+                             const void* k_new, int64_t k_row_stride, const void* v_new,
+                             int64_t v_row_stride, void* q_out, void* stream);
+
+/* libra_append_attn from unturned projections: keys are turned on their way into the cache
+ * (to the bits libra_rotary_apply gives), queries where the attention kernels load them, and
+ * neither is written out.  A turned query enters the scores as the sum of two bf16 numbers a
+ * channel, 16 bits, so that scores and lse are float32's of the unrounded queries (within
+ * 2^-17 of each product; turned queries rounded to bf16 would put 2^-8 into them).  q, k_new
+ * and v_new are rows as in libra_kv_append, [sum C_b] of them in libra_append_attn's order.
+ * positions: device int32 [sum C_b], or NULL for each token's index in its sequence's cache
+ * (P_b + i); positions need not follow the index, as where part of a context has been
+ * dropped, but the causal order is the cache's.  A key that a row sees must be finite (an
+ * infinite channel makes the row NaN); what lies behind a sequence's end may be anything.
+ * Plans, workspaces, streams and graph capture are as for libra_append_attn. */
+libra_status libra_append_attn_rotary(libra_kv_layout layout, libra_plan plan,
+                                      libra_rotary rotary, const int32_t* positions,
+                                      const void* q, int64_t q_row_stride, const void* k_new,
+                                      int64_t k_row_stride, const void* v_new,
+                                      int64_t v_row_stride, const int32_t* block_table,
+                                      int32_t bt_stride, int32_t batch, int32_t num_q_heads,
+                                      float scale, void* workspace, size_t ws_bytes, void* out,
+                                      float* lse, void* stream);
+
+/* ------------------------------------------------------------------------------ */
 /* Per-kernel timing                                                               */
 /* ------------------------------------------------------------------------------ */
 /*
@@ -452,7 +568,8 @@ enum {
   LIBRA_KERNEL_UPLOAD = 7,
   LIBRA_KERNEL_COPY_OUT = 8,
   LIBRA_KERNEL_COPY_IN = 9,
-  LIBRA_KERNEL_KINDS = 10
+  LIBRA_KERNEL_ROTARY = 10,
+  LIBRA_KERNEL_KINDS = 11
 };
 
 typedef struct libra_kernel_times {

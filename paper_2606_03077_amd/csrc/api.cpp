@@ -10,6 +10,7 @@
 #include <unordered_map>
 #include <vector>
 
+#include "calls.h"
 #include "internal.h"
 
 namespace libra {
@@ -60,38 +61,35 @@ struct Profiler {
 };
 Profiler g_prof;
 
-// Brackets one kernel launch with events when profiling is on.
-class ProfScope {
- public:
-  ProfScope(int kind, hipStream_t s, bool active) : kind_(kind), s_(s) {
-    if (!active) return;
-    std::lock_guard<std::mutex> lk(g_prof.mu);
-    if (!g_prof.enabled) return;
-    a_ = g_prof.get();
-    b_ = g_prof.get();
-    if (a_ && b_ && hipEventRecord(a_, s_) == hipSuccess) return;
+}  // namespace
+
+ProfScope::ProfScope(int kind, hipStream_t s, bool active) : kind_(kind), s_(s) {
+  if (!active) return;
+  std::lock_guard<std::mutex> lk(g_prof.mu);
+  if (!g_prof.enabled) return;
+  a_ = g_prof.get();
+  b_ = g_prof.get();
+  if (a_ && b_ && hipEventRecord(a_, s_) == hipSuccess) return;
+  release();
+}
+
+ProfScope::~ProfScope() {
+  if (!a_) return;
+  std::lock_guard<std::mutex> lk(g_prof.mu);
+  if (hipEventRecord(b_, s_) == hipSuccess) {
+    g_prof.pending.push_back({kind_, a_, b_});
+  } else {
     release();
   }
-  ~ProfScope() {
-    if (!a_) return;
-    std::lock_guard<std::mutex> lk(g_prof.mu);
-    if (hipEventRecord(b_, s_) == hipSuccess) {
-      g_prof.pending.push_back({kind_, a_, b_});
-    } else {
-      release();
-    }
-  }
+}
 
- private:
-  void release() {
-    if (a_) g_prof.free_events.push_back(a_);
-    if (b_) g_prof.free_events.push_back(b_);
-    a_ = b_ = nullptr;
-  }
-  int kind_;
-  hipStream_t s_;
-  hipEvent_t a_ = nullptr, b_ = nullptr;
-};
+void ProfScope::release() {
+  if (a_) g_prof.free_events.push_back(a_);
+  if (b_) g_prof.free_events.push_back(b_);
+  a_ = b_ = nullptr;
+}
+
+namespace {
 
 libra_status check_layout(const libra_kv_layout_desc* d) {
   if (!d) return set_error(LIBRA_E_INVAL, "layout descriptor is NULL");
@@ -109,8 +107,6 @@ libra_status check_layout(const libra_kv_layout_desc* d) {
     return set_error(LIBRA_E_INVAL, "k_cache / v_cache must be 16-byte aligned");
   return LIBRA_OK;
 }
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
 // Which plan's tables each workspace holds, by plan id: a call skips the table upload
 // only if its own plan was the last to upload to that workspace, so plans that take
@@ -236,13 +232,16 @@ libra_status ensure_aux_stream() {
   return LIBRA_OK;
 }
 
-// The current device's auxiliary stream, or null if it has none (then run sequentially).
+}  // namespace
+
 hipStream_t aux_stream() {
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= kMaxAuxDevices) return nullptr;
   std::lock_guard<std::mutex> lk(g_aux_mu);
   return g_aux_stream[dev];
 }
+
+namespace {
 
 // Fills the plan's pinned image with its tables (at plan creation).
 void staging_fill(Plan& P) {
@@ -289,11 +288,8 @@ libra_status enqueue_tables(const Plan& P, void* ws, hipStream_t s) {
   return LIBRA_OK;
 }
 
-// Picks the form of plan P that runs in a workspace of ws_bytes bytes and copies its tables
-// there unless they are there already (or always, if forced).  The faster form is taken if
-// the workspace is large enough for it; a call whose workspace holds the plain tables runs
-// the plain form, so that a call on uploaded tables enqueues kernels only, whatever size
-// it states: the plain tables are there with the fine tiles' as well.
+}  // namespace
+
 libra_status upload(Plan& P, void* ws, size_t ws_bytes, hipStream_t s, bool force,
                     const Plan** form) {
   std::lock_guard<std::mutex> lk(P.upload_mu);
@@ -342,60 +338,20 @@ libra_status check_call(const KvLayout* L, const Plan* P, int mode, const void* 
   return LIBRA_OK;
 }
 
-// Decode units, chunk units, then the merge of split rows.  `timed` allows per-kernel
-// timing events (which may create events while timing is enabled).  When the plan has
-// both decode rows and chunk tiles, the chunk launch goes first on `s` and the decode
-// launch on the device's auxiliary stream, forked from `s` after everything enqueued
-// before and joined back before the merge: the dispatcher then fills the CUs that the
-// matrix-core bound chunk tiles free with the HBM-bound decode rows as they come.
-std::mutex g_fork_mu;  // record / wait pairs of concurrent callers must not interleave
+std::mutex& fork_mutex() {
+  static std::mutex mu;
+  return mu;
+}
+
+namespace {
 
 libra_status launch_attention(const KvLayout& L, const Plan& P, void* ws, const void* q,
                               const int32_t* bt, int32_t stride, float scale, void* out,
                               float* lse, hipStream_t s, bool timed = true) {
-  hipError_t e;
-  hipStream_t s2 = nullptr;
-  if (P.info.n_single > 0 && P.info.n_chunk > 0 && P.fork_ev && P.join_ev) s2 = aux_stream();
-  if (s2) {
-    {
-      std::lock_guard<std::mutex> lk(g_fork_mu);
-      e = hipEventRecord(P.fork_ev, s);
-      if (e == hipSuccess) e = hipStreamWaitEvent(s2, P.fork_ev, 0);
-    }
-    if (e != hipSuccess) return hip_error(e, "forking the decode rows");
-    {
-      ProfScope ps(LIBRA_KERNEL_CHUNK, s, timed);
-      e = launch_chunk(L, P, ws, q, bt, stride, scale, out, lse, s);
-    }
-    if (e != hipSuccess) return hip_error(e, "chunk launch");
-    {
-      ProfScope ps(LIBRA_KERNEL_DECODE, s2, timed);
-      e = launch_decode(L, P, ws, q, bt, stride, scale, out, lse, s2);
-    }
-    if (e != hipSuccess) return hip_error(e, "decode launch");
-    {
-      std::lock_guard<std::mutex> lk(g_fork_mu);
-      e = hipEventRecord(P.join_ev, s2);
-      if (e == hipSuccess) e = hipStreamWaitEvent(s, P.join_ev, 0);
-    }
-    if (e != hipSuccess) return hip_error(e, "joining the decode rows");
-  } else {
-    {
-      ProfScope ps(LIBRA_KERNEL_DECODE, s, timed && P.info.n_single > 0);
-      e = launch_decode(L, P, ws, q, bt, stride, scale, out, lse, s);
-    }
-    if (e != hipSuccess) return hip_error(e, "decode launch");
-    {
-      ProfScope ps(LIBRA_KERNEL_CHUNK, s, timed && P.info.n_chunk > 0);
-      e = launch_chunk(L, P, ws, q, bt, stride, scale, out, lse, s);
-    }
-    if (e != hipSuccess) return hip_error(e, "chunk launch");
-  }
-  {
-    ProfScope ps(LIBRA_KERNEL_MERGE, s, timed && merge_launches(P));
-    e = launch_merge(P, ws, out, lse, s);
-  }
-  return e == hipSuccess ? LIBRA_OK : hip_error(e, "merge launch");
+  return run_attention(
+      P, ws, out, lse, s, timed,
+      [&](hipStream_t at) { return launch_chunk(L, P, ws, q, bt, stride, scale, out, lse, at); },
+      [&](hipStream_t at) { return launch_decode(L, P, ws, q, bt, stride, scale, out, lse, at); });
 }
 
 // The address a kernel uses for a page run: device memory as is, pinned host memory
@@ -448,9 +404,6 @@ libra_status page_copy(const KvLayout* layout, const int32_t* page_ids, int64_t 
 }  // namespace libra
 
 using namespace libra;
-
-struct libra_kv_layout_s : KvLayout {};
-struct libra_plan_s : Plan {};
 
 extern "C" {
 

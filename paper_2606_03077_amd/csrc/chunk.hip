@@ -51,6 +51,7 @@
 #include <type_traits>
 
 #include "internal.h"
+#include "rotary_calls.h"
 
 namespace libra {
 namespace {
@@ -106,9 +107,16 @@ struct ChunkArgs {
 // Row (M index) of element r of a 32x32 accumulator in a lane of half h.
 __device__ __forceinline__ constexpr int acc_row(int r, int h) { return 8 * (r / 4) + 4 * h + (r % 4); }
 
-template <int kWaves>
+// Queries that are turned as they are loaded.
+struct ChunkRotaryArgs : ChunkArgs {
+  RotaryArgs<kRotaryPairs> rot;
+  const int32_t* positions;  // null: the row's index in the cache
+  int64_t q_row;
+};
+
+template <int kWaves, bool kRotary>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2)))
-void chunk_kernel(ChunkArgs A) {
+void chunk_kernel(std::conditional_t<kRotary, ChunkRotaryArgs, ChunkArgs> A) {
   constexpr bool kWide = kWaves == kWideWaves;
   constexpr int kThreads = 64 * kWaves;
   constexpr int kRows = 32 * kWaves;
@@ -199,7 +207,8 @@ void chunk_kernel(ChunkArgs A) {
   // Q operand of MFMA c (channels 16 c .. 16 c + 15): lane (col, hh) holds channels
   // 16 c + 8 hh .. + 7 of its row.
   bf16x8 qop[8];
-  {
+  [[maybe_unused]] bf16x8 qlow[8];  // what bf16 leaves of turned queries
+  if constexpr (!kRotary) {
     const uint4* qrow = reinterpret_cast<const uint4*>(
         A.q + (size_t(row0 + (ok ? t_tok : 0)) * A.hq + size_t(g) * G + head) * kDim);
 #pragma unroll
@@ -272,6 +281,44 @@ void chunk_kernel(ChunkArgs A) {
     for (int j = 0; j < 4; ++j)
       if (i0 + j * kThreads < nids) lds_ids[i0 + j * kThreads] = v[j];
   }
+  // Turned queries, while the first copies land.  The wave's rows are those of a few tokens;
+  // eight tokens at a time, a lane computes one pair's cosine and sine of each, and the wave
+  // shares them through its 4 KiB of the last K and V stage, which step 0 fills first, behind
+  // the barrier below.
+  if constexpr (kRotary) {
+    constexpr int kBatch = 8;
+    float2* const cs = reinterpret_cast<float2*>(
+        (wave < kWaves / 2 ? &ldk3[0][0] : &ldv3[0][0]) + (wave % (kWaves / 2)) * 256);
+    const int tok0 = q0 + (r_first + 32 * wave) / G;
+    const int tok1 = min(q0 + (r_first + 32 * wave + 31) / G + 1, q1);  // the wave's tokens
+    const uint16_t* const qrow =
+        A.q + size_t(row0 + (ok ? t_tok : 0)) * A.q_row + (size_t(g) * G + head) * kDim;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) qop[c] = qlow[c] = as_bf16x8(make_uint4(0, 0, 0, 0));
+    for (int base = tok0; base < tok1; base += kBatch) {
+      for (int i = 0; i < kBatch && base + i < tok1; ++i) {
+        const int32_t pos = A.positions ? A.positions[row0 + base + i] : prior + base + i;
+        if (lane < A.rot.rdim / 2)
+          cs[i * kRotaryPairs + lane] = rotary_cos_sin(A.rot.turn[lane], pos, A.rot.amplitude);
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+      if (ok && t_tok >= base && t_tok < base + kBatch) {
+        const uint16_t* row = qrow;
+        int rdim = A.rot.rdim;
+        asm volatile("" : "+v"(row), "+s"(rdim));  // nothing of these is held over the batches
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          const TurnedGranule v = turned_granule<true>(
+              row, 2 * c + hh, cs + (t_tok - base) * kRotaryPairs, rdim, A.rot.interleaved);
+          qop[c] = as_bf16x8(v.hi);
+          qlow[c] = as_bf16x8(v.lo);
+        }
+      }
+      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+      __builtin_amdgcn_wave_barrier();
+    }
+  }
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();
 
@@ -287,6 +334,8 @@ void chunk_kernel(ChunkArgs A) {
     for (int c = 0; c < 8; ++c) {
       const uint4 kr = kst(stage_tag)[j][(2 * c + hh) * 16 + (col & 15)];
       a = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kr), qop[c], a, 0, 0, 0);
+      if constexpr (kRotary)
+        a = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kr), qlow[c], a, 0, 0, 0);
     }
     s = a;
   };
@@ -398,6 +447,8 @@ void chunk_kernel(ChunkArgs A) {
     for (int c = 0; c < 8; ++c) {
       if constexpr (!kLast) {
         qs = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kpre[c]), qop[c], qs, 0, 0, 0);
+        if constexpr (kRotary)
+          qs = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kpre[c]), qlow[c], qs, 0, 0, 0);
       }
       const int jj = c >> 2, cb = c & 3;
       uint4 vo = vst(vread)[2 * P + jj][128 * hh + 32 * cb + col];
@@ -551,12 +602,8 @@ void chunk_kernel(ChunkArgs A) {
     A.lse[size_t(row0 + t_tok) * A.hq + head0 + head] = ls > 0.f ? (m + log2f(ls)) * kLn2 : -INFINITY;
 }
 
-}  // namespace
-
-hipError_t launch_chunk(const KvLayout& L, const Plan& P, void* ws, const void* q,
-                        const int32_t* bt, int32_t stride, float scale, void* out, float* lse,
-                        hipStream_t s) {
-  if (P.info.n_chunk == 0) return hipSuccess;
+ChunkArgs chunk_args(const KvLayout& L, const Plan& P, void* ws, const void* q,
+                     const int32_t* bt, int32_t stride, float scale, void* out, float* lse) {
   char* w = static_cast<char*>(ws);
   ChunkArgs A;
   A.k_cache = static_cast<const uint16_t*>(L.desc.k_cache);
@@ -580,13 +627,38 @@ hipError_t launch_chunk(const KvLayout& L, const Plan& P, void* ws, const void* 
   A.hq = P.num_q_heads;
   A.group = P.group;
   A.sl2 = scale * kLog2e;
+  return A;
+}
+
+template <bool kRotary, class Args>
+hipError_t launch_form(const Plan& P, const Args& A, hipStream_t s) {
+  const dim3 grid{unsigned(P.chunk_grid)};
   if (P.chunk_form != kUnits)
-    hipLaunchKernelGGL(chunk_kernel<kNarrowWaves>, dim3(unsigned(P.chunk_grid)),
-                       dim3(64 * kNarrowWaves), 0, s, A);
+    hipLaunchKernelGGL((chunk_kernel<kNarrowWaves, kRotary>), grid, dim3(64 * kNarrowWaves), 0, s, A);
   else
-    hipLaunchKernelGGL(chunk_kernel<kWideWaves>, dim3(unsigned(P.chunk_grid)),
-                       dim3(64 * kWideWaves), 0, s, A);
+    hipLaunchKernelGGL((chunk_kernel<kWideWaves, kRotary>), grid, dim3(64 * kWideWaves), 0, s, A);
   return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_chunk(const KvLayout& L, const Plan& P, void* ws, const void* q,
+                        const int32_t* bt, int32_t stride, float scale, void* out, float* lse,
+                        hipStream_t s) {
+  if (P.info.n_chunk == 0) return hipSuccess;
+  return launch_form<false>(P, chunk_args(L, P, ws, q, bt, stride, scale, out, lse), s);
+}
+
+hipError_t launch_chunk_rotary(const KvLayout& L, const Plan& P, void* ws, const NewRows& n,
+                               const int32_t* bt, int32_t stride, float scale, void* out,
+                               float* lse, hipStream_t s) {
+  if (P.info.n_chunk == 0) return hipSuccess;
+  ChunkRotaryArgs A;
+  static_cast<ChunkArgs&>(A) = chunk_args(L, P, ws, n.q, bt, stride, scale, out, lse);
+  A.rot = rotary_args<kRotaryPairs>(*n.rotary);
+  A.positions = n.positions;
+  A.q_row = n.q_row;
+  return launch_form<true>(P, A, s);
 }
 
 }  // namespace libra

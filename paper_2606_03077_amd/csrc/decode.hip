@@ -20,8 +20,10 @@
 // each split row by their log-sum-exps (the launch boundary orders the two without
 // device-wide cache flushes inside either kernel).
 #include <cmath>
+#include <type_traits>
 
 #include "internal.h"
+#include "rotary_calls.h"
 
 namespace libra {
 namespace {
@@ -101,6 +103,15 @@ __device__ __forceinline__ f32x4 qk_page(const PageRegs& r, const bf16x8 (&qop)[
   return s;
 }
 
+// Queries as a sum of two bf16 parts.
+struct SplitQuery {
+  bf16x8 hi[4], lo[4];
+};
+__device__ __forceinline__ f32x4 qk_page(const PageRegs& r, const SplitQuery& q) {
+  const f32x4 s = qk_page(r, q.hi);
+  return s + qk_page(r, q.lo);
+}
+
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
@@ -125,8 +136,9 @@ __device__ __forceinline__ bf16x4_bits as_bf16x4(uint32_t lo, uint32_t hi) {
 //   O^T[128 x 16 heads] += V^T[128 x 16 slots] . P^T: 8 x mfma 16x16x16 (k = slots),
 // whose B operand (lane = head + 16 * quad, slots 4 quad .. + 3) is exactly the score
 // tile's accumulator layout, so probabilities never leave registers.
+template <class Query>
 __device__ __forceinline__ void process_page(const PageRegs& r, int valid, int quad,
-                                             const bf16x8 (&qop)[4], float sl2, Softmax& sm,
+                                             const Query& qop, float sl2, Softmax& sm,
                                              f32x4 (&acc)[8]) {
   const f32x4 s = qk_page(r, qop);
   float x[4];
@@ -169,7 +181,16 @@ struct DecodeArgs {
   float sl2;  // scale * log2(e)
 };
 
-__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(LIBRA_DECODE_WAVES_PER_EU, 8))) void decode_kernel(DecodeArgs A) {
+// Queries that are turned as they are loaded.
+struct DecodeRotaryArgs : DecodeArgs {
+  RotaryArgs<kRotaryPairs> rot;
+  const int32_t* positions;  // null: the row's index in the cache
+  int64_t q_row;
+};
+
+template <bool kRotary>
+__global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(LIBRA_DECODE_WAVES_PER_EU, 8)))
+void decode_kernel(std::conditional_t<kRotary, DecodeRotaryArgs, DecodeArgs> A) {
   __shared__ float red_m[kWaves][16];
   __shared__ float red_l[kWaves][16];
   __shared__ __align__(16) float red_o[kWaves][16][kRedStride];
@@ -184,8 +205,24 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(LIBRA_
   const int G = A.group;
 
   // Q operand: lane (col, quad) holds head col's channels 8 * (4 i + quad) .. + 7 at step i.
-  bf16x8 qop[4];
-  {
+  std::conditional_t<kRotary, SplitQuery, bf16x8[4]> qop;
+  if constexpr (kRotary) {
+    // A lane computes one pair's cosine and sine; the wave shares them through its part of
+    // red_o, which is written only after the next barrier.
+    float2* cs = reinterpret_cast<float2*>(&red_o[wave][0][0]);
+    const int32_t pos = A.positions ? A.positions[row] : u[U_PRIOR];
+    if (lane < A.rot.rdim / 2) cs[lane] = rotary_cos_sin(A.rot.turn[lane], pos, A.rot.amplitude);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    const uint16_t* qrow = A.q + size_t(row) * A.q_row + (size_t(g) * G + col) * kDim;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      TurnedGranule v{make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
+      if (col < G) v = turned_granule<true>(qrow, 4 * i + quad, cs, A.rot.rdim, A.rot.interleaved);
+      qop.hi[i] = as_bf16x8(v.hi);
+      qop.lo[i] = as_bf16x8(v.lo);
+    }
+  } else {
     const uint4* qrow = reinterpret_cast<const uint4*>(
         A.q + (size_t(row) * A.hq + size_t(g) * G + col) * kDim);
 #pragma unroll
@@ -341,11 +378,10 @@ __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(LIBRA_
 
 }  // namespace
 
-hipError_t launch_decode(const KvLayout& L, const Plan& P, void* ws, const void* q,
-                         const int32_t* bt, int32_t stride, float scale, void* out, float* lse,
-                         hipStream_t s) {
-  const int n = P.info.n_single;
-  if (n == 0) return hipSuccess;
+namespace {
+
+DecodeArgs decode_args(const KvLayout& L, const Plan& P, void* ws, const void* q,
+                       const int32_t* bt, int32_t stride, float scale, void* out, float* lse) {
   char* w = static_cast<char*>(ws);
   DecodeArgs A;
   A.k_cache = static_cast<const uint16_t*>(L.desc.k_cache);
@@ -362,7 +398,32 @@ hipError_t launch_decode(const KvLayout& L, const Plan& P, void* ws, const void*
   A.hq = P.num_q_heads;
   A.group = P.group;
   A.sl2 = scale * kLog2e;
-  hipLaunchKernelGGL(decode_kernel, dim3(unsigned(n)), dim3(kThreads), 0, s, A);
+  return A;
+}
+
+}  // namespace
+
+hipError_t launch_decode(const KvLayout& L, const Plan& P, void* ws, const void* q,
+                         const int32_t* bt, int32_t stride, float scale, void* out, float* lse,
+                         hipStream_t s) {
+  const int n = P.info.n_single;
+  if (n == 0) return hipSuccess;
+  const DecodeArgs A = decode_args(L, P, ws, q, bt, stride, scale, out, lse);
+  hipLaunchKernelGGL(decode_kernel<false>, dim3(unsigned(n)), dim3(kThreads), 0, s, A);
+  return hipGetLastError();
+}
+
+hipError_t launch_decode_rotary(const KvLayout& L, const Plan& P, void* ws, const NewRows& n,
+                                const int32_t* bt, int32_t stride, float scale, void* out,
+                                float* lse, hipStream_t s) {
+  const int units = P.info.n_single;
+  if (units == 0) return hipSuccess;
+  DecodeRotaryArgs A;
+  static_cast<DecodeArgs&>(A) = decode_args(L, P, ws, n.q, bt, stride, scale, out, lse);
+  A.rot = rotary_args<kRotaryPairs>(*n.rotary);
+  A.positions = n.positions;
+  A.q_row = n.q_row;
+  hipLaunchKernelGGL(decode_kernel<true>, dim3(unsigned(units)), dim3(kThreads), 0, s, A);
   return hipGetLastError();
 }
 

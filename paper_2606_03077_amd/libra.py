@@ -22,6 +22,14 @@ STATUS_NAMES = {0: "LIBRA_OK", 1: "LIBRA_E_INVAL", 2: "LIBRA_E_UNSUPPORTED",
 LIBRA_MODE_DECODE = 0
 LIBRA_MODE_APPEND = 1
 LIBRA_DTYPE_BF16 = 0
+LIBRA_DTYPE_FP16 = 1
+LIBRA_DTYPE_FP32 = 2
+LIBRA_ROTARY_HALF = 0
+LIBRA_ROTARY_INTERLEAVED = 1
+LIBRA_ROTARY_PLAIN = 0
+LIBRA_ROTARY_LINEAR = 1
+LIBRA_ROTARY_BASE = 2
+LIBRA_ROTARY_BANDS = 3
 PAGE_SIZE = 16
 HEAD_DIM = 128
 UNIT_INTS = 12
@@ -36,13 +44,15 @@ EXPORTS = ("libra_status_string", "libra_last_error", "libra_alloc_calls",
            "libra_plan_get_info",
            "libra_plan_workspace_bytes", "libra_plan_upload", "libra_plan_destroy",
            "libra_decode_attn", "libra_decode_attn_noalloc", "libra_append_attn",
+           "libra_rotary_create", "libra_rotary_destroy", "libra_rotary_get",
+           "libra_rotary_apply", "libra_kv_append", "libra_append_attn_rotary",
            "libra_profile_enable",
            "libra_profile_collect", "libra_ce_fit", "libra_ce_mape", "libra_ce_poly_sum",
            "libra_rollout_dp", "libra_trie_create", "libra_trie_destroy", "libra_trie_insert",
            "libra_trie_lookup", "libra_route_bucket")
 TP_SLOTS = {1: 0, 2: 1, 4: 2, 8: 3}
 KERNEL_KINDS = ("pack", "unpack", "gather", "cache_write", "decode", "merge", "chunk", "upload",
-                "copy_out", "copy_in")
+                "copy_out", "copy_in", "rotary")
 
 
 class LibraError(RuntimeError):
@@ -76,6 +86,15 @@ class PlanInfo(ctypes.Structure):
                 ("n_rows", ctypes.c_int32), ("n_write_tiles", ctypes.c_int32),
                 ("num_cus", ctypes.c_int32), ("n_merge_groups", ctypes.c_int32),
                 ("balanced", ctypes.c_int32)]
+
+
+class RotaryDesc(ctypes.Structure):
+    _fields_ = [("head_dim", ctypes.c_int32), ("rotary_dim", ctypes.c_int32),
+                ("pairing", ctypes.c_int32), ("scaling", ctypes.c_int32),
+                ("base", ctypes.c_double), ("factor", ctypes.c_double),
+                ("original_length", ctypes.c_int64), ("fast", ctypes.c_double),
+                ("slow", ctypes.c_double), ("amplitude", ctypes.c_double),
+                ("frequencies", ctypes.POINTER(ctypes.c_double))]
 
 
 class CePoly(ctypes.Structure):
@@ -140,6 +159,14 @@ def load() -> ctypes.CDLL:
                                                      P, P, P]),
         "libra_append_attn": (ctypes.c_int, [P, P, P, P, P, P, I32, I32, I32, ctypes.c_float, P,
                                              SZ, P, P, P]),
+        "libra_rotary_create": (ctypes.c_int, [ctypes.POINTER(RotaryDesc), ctypes.POINTER(P)]),
+        "libra_rotary_destroy": (None, [P]),
+        "libra_rotary_get": (ctypes.c_int, [P, P, P, DP, DP]),
+        "libra_rotary_apply": (ctypes.c_int, [P, I32, P, I64, I64, P, I64, I32, I32, P, I64, I64,
+                                              P]),
+        "libra_kv_append": (ctypes.c_int, [P, P, P, P, I64, P, I64, I32, P, I64, P, I64, P, P]),
+        "libra_append_attn_rotary": (ctypes.c_int, [P, P, P, P, P, I64, P, I64, P, I64, P, I32,
+                                                    I32, I32, ctypes.c_float, P, SZ, P, P, P]),
         "libra_profile_enable": (ctypes.c_int, [ctypes.c_int]),
         "libra_profile_collect": (ctypes.c_int, [ctypes.POINTER(KernelTimes)]),
         "libra_ce_fit": (ctypes.c_int, [DP, DP, I32, ctypes.POINTER(CePoly)]),
@@ -390,6 +417,128 @@ def libra_append_attn(layout: int, plan: int, q, k_new, v_new, block_table, bt_s
                                     _ptr(block_table), bt_stride, batch, num_q_heads, scale,
                                     _ptr(workspace), ws_bytes, _ptr(out), _ptr(lse),
                                     _stream(stream)), "libra_append_attn")
+
+
+_ROTARY_DTYPES = {torch.bfloat16: LIBRA_DTYPE_BF16, torch.float16: LIBRA_DTYPE_FP16,
+                  torch.float32: LIBRA_DTYPE_FP32}
+_BF16_BITS = (torch.bfloat16, torch.int16)
+
+
+def libra_rotary_create(head_dim: int = HEAD_DIM, rotary_dim: int = 0,
+                        pairing: int = LIBRA_ROTARY_HALF, base: float = 10000.0,
+                        scaling: int = LIBRA_ROTARY_PLAIN, factor: float = 1.0,
+                        original_length: int = 0, fast: float = 0.0, slow: float = 0.0,
+                        amplitude: float = 0.0, frequencies=None) -> int:
+    """A rotary handle (formulas in include/libra.h).  frequencies: rotary_dim / 2 angles per
+    position, in place of base^(-2 j / rotary_dim)."""
+    f = None
+    if frequencies is not None:
+        f = _f64(frequencies)
+        if f.shape != ((rotary_dim or head_dim) // 2,):
+            raise ValueError("frequencies needs one entry per pair")
+    d = RotaryDesc(head_dim, rotary_dim, pairing, scaling, base, factor, original_length, fast,
+                   slow, amplitude, None if f is None else _dp(f))
+    h = ctypes.c_void_p()
+    _check(load().libra_rotary_create(ctypes.byref(d), ctypes.byref(h)), "libra_rotary_create")
+    return h.value
+
+
+def libra_rotary_destroy(rotary: int) -> None:
+    load().libra_rotary_destroy(rotary)
+
+
+def libra_rotary_get(rotary: int) -> dict:
+    """{"head_dim", "rotary_dim", "frequencies" (scaled, one per pair), "amplitude"}."""
+    dims = (ctypes.c_int32 * 2)()
+    _check(load().libra_rotary_get(rotary, ctypes.byref(dims, 0), ctypes.byref(dims, 4), None,
+                                   None), "libra_rotary_get")
+    f, a = np.empty(dims[1] // 2), ctypes.c_double()
+    _check(load().libra_rotary_get(rotary, None, None, _dp(f), ctypes.byref(a)),
+           "libra_rotary_get")
+    return {"head_dim": dims[0], "rotary_dim": dims[1], "frequencies": f, "amplitude": a.value}
+
+
+def _vector(t, dtype, n: Optional[int], what: str) -> Optional[int]:
+    """A contiguous device vector of n elements (any number of them if n is None)."""
+    if t is None:
+        return None
+    if t.device.type != "cuda" or t.dtype != dtype or not t.is_contiguous():
+        raise ValueError(f"{what}: contiguous {dtype} device tensor expected")
+    if n is not None and t.numel() != n:
+        raise ValueError(f"{what}: {n} elements expected")
+    return t.data_ptr()
+
+
+def _rows(t, rows: Optional[int], heads: Optional[int], what: str):
+    """(pointer, row stride) of a projection's bf16 rows [rows, heads, 128], 128 apart."""
+    if t is None:
+        return None, 0
+    if t.device.type != "cuda" or t.dtype not in _BF16_BITS:
+        raise ValueError(f"{what}: bf16 device tensor expected")
+    if t.dim() != 3 or t.shape[2] != HEAD_DIM or (rows is not None and t.shape[0] != rows) or \
+            (heads is not None and t.shape[1] != heads):
+        raise ValueError(f"{what}: [{rows or 'rows'}, {heads or 'heads'}, {HEAD_DIM}] expected")
+    if t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != HEAD_DIM):
+        raise ValueError(f"{what}: heads must lie {HEAD_DIM} elements apart")
+    return t.data_ptr(), t.stride(0) if t.shape[0] > 1 else t.shape[1] * HEAD_DIM
+
+
+def libra_rotary_apply(rotary: int, x, positions, out, backward: bool = False, stream=None):
+    """Turns x [rows, heads, head_dim] (bf16, fp16 or fp32; any row and head strides) by
+    positions [rows] (int32) into out, of the same shape and type, which may be x."""
+    if x.dim() != 3 or out.shape != x.shape or out.dtype != x.dtype:
+        raise ValueError("x and out must be [rows, heads, head_dim] of one type")
+    if x.device.type != "cuda" or out.device != x.device or x.dtype not in _ROTARY_DTYPES:
+        raise ValueError("bf16, fp16 or fp32 device tensors expected")
+    dim = ctypes.c_int32()
+    _check(load().libra_rotary_get(rotary, ctypes.byref(dim), None, None, None),
+           "libra_rotary_get")
+    if x.shape[2] != dim.value:
+        raise ValueError("x's head size differs from the rotary's")
+    if x.stride(2) != 1 or out.stride(2) != 1:
+        raise ValueError("the channels of a head must be contiguous")
+    rows, heads = x.shape[:2]
+    _check(load().libra_rotary_apply(rotary, _ROTARY_DTYPES[x.dtype], x.data_ptr(), x.stride(0),
+                                     x.stride(1), _vector(positions, torch.int32, rows, "positions"),
+                                     rows, heads, int(bool(backward)), out.data_ptr(),
+                                     out.stride(0), out.stride(1), _stream(stream)),
+           "libra_rotary_apply")
+
+
+def libra_kv_append(layout: int, rotary: Optional[int], positions, slots, q, k_new, v_new, q_out,
+                    stream=None):
+    """Writes k_new (turned) and v_new [rows, Hkv, 128] to slots [rows] (int64; outside the
+    cache: padding), and q [rows, Hq, 128] turned to q_out.  Rows may be slices of one
+    projection.  rotary None: keys as they are; q and q_out may be None."""
+    rows = slots.numel()
+    qp, qs = _rows(q, rows, None, "q")
+    kp, ks = _rows(k_new, rows, None, "k_new")
+    vp, vs = _rows(v_new, rows, k_new.shape[1], "v_new")
+    if q_out is not None and (q is None or q_out.shape != q.shape or not q_out.is_contiguous()
+                              or q_out.dtype not in _BF16_BITS):
+        raise ValueError("q_out must be contiguous bf16 of q's shape")
+    _check(load().libra_kv_append(layout, rotary, _vector(positions, torch.int32, rows, "positions"),
+                                  _vector(slots, torch.int64, rows, "slots"), rows, qp, qs,
+                                  0 if q is None else q.shape[1], kp, ks, vp, vs, _ptr(q_out),
+                                  _stream(stream)), "libra_kv_append")
+
+
+def libra_append_attn_rotary(layout: int, plan: int, rotary: int, positions, q, k_new, v_new,
+                             block_table, bt_stride: int, batch: int, num_q_heads: int,
+                             scale: float, workspace, out, lse=None, stream=None):
+    """libra_append_attn from unturned projections, whose rows may be slices of one tensor;
+    positions [rows] (int32), or None for each token's index in its cache."""
+    ws_bytes = workspace.numel() * workspace.element_size()
+    rows = q.shape[0]
+    qp, qs = _rows(q, rows, num_q_heads, "q")
+    kp, ks = _rows(k_new, rows, None, "k_new")
+    vp, vs = _rows(v_new, rows, k_new.shape[1], "v_new")
+    _check(load().libra_append_attn_rotary(layout, plan, rotary,
+                                           _vector(positions, torch.int32, rows, "positions"), qp,
+                                           qs, kp, ks, vp, vs, _ptr(block_table), bt_stride, batch,
+                                           num_q_heads, scale, _ptr(workspace), ws_bytes,
+                                           _ptr(out), _ptr(lse), _stream(stream)),
+           "libra_append_attn_rotary")
 
 
 def libra_profile_enable(enable: bool = True) -> None:

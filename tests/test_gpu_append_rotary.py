@@ -1,0 +1,258 @@
+"""libra_append_attn_rotary on the GPU, in every launched form (decode units, wide and narrow
+chunk tiles, split keys).
+
+Where nothing turns (frequencies of zero) it gives libra_append_attn's bits.  Turned, the cache
+holds libra_rotary_apply's bits, and outputs are those of float64 attention of the exactly turned
+queries over that cache: queries enter the scores as two bf16 parts, so what is left of them is
+2^-17 of each channel (two halvings of 2^-8 and the turn's own error), and a score, a sum of 128
+float32 products, is within scale |q| |k| (2^-17 + 128 * 2^-24) of exact."""
+import numpy as np
+import pytest
+import torch
+
+from paper_2606_03077_amd import libra
+from paper_2606_03077_amd import workloads as wl
+
+import gpu_harness as H
+from test_gpu_rotary import Handle, f64, randn
+
+pytestmark = pytest.mark.gpu
+
+BF16 = torch.bfloat16
+NAN = 0x7FC0
+
+
+class Step:
+    """A batch's cache, projections and plan."""
+
+    def __init__(self, lens, news, hq, hkv, seed=1, shift=None, **params):
+        self.lens, self.news, self.hq, self.hkv = lens, news, hq, hkv
+        self.batch = wl.custom_batch(lens, news, num_q_heads=hq, num_kv_heads=hkv, seed=seed,
+                                     append=True)
+        self.cache = H.DeviceCache(self.batch)
+        self.rows = sum(news)
+        self.qkv = torch.empty((self.rows, hq + 2 * hkv, 128), dtype=BF16, device="cuda")
+        self.q, self.k, self.v = self.qkv.split([hq, hkv, hkv], dim=1)
+        for dst, src in ((self.q, self.batch.q), (self.k, self.batch.k_new), (self.v, self.batch.v_new)):
+            dst.copy_(H.u16_to_dev(src).view(BF16))
+        at = np.concatenate([np.arange(n - c, n) for n, c in zip(lens, news)]).astype(np.int32)
+        self.pos = at if shift is None else (at + shift).astype(np.int32)
+        self.pd = torch.from_numpy(self.pos).cuda()
+        self.given = None if shift is None else self.pd
+        self.params = params
+        self.plan = H.plan_for(self.batch, **params)
+        self.ws = libra.alloc_workspace(self.plan)
+        self.k0, self.v0 = self.cache.k.clone(), self.cache.v.clone()
+
+    def outputs(self):
+        return (torch.full((self.rows, self.hq, 128), NAN, dtype=torch.int16, device="cuda"),
+                torch.full((self.rows, self.hq), float("nan"), device="cuda"))
+
+    def reset(self):
+        self.cache.k.copy_(self.k0)
+        self.cache.v.copy_(self.v0)
+
+    def call(self, rope, out, lse, ws=None, stream=None):
+        libra.libra_append_attn_rotary(
+            self.cache.layout, self.plan, rope.h, self.given, self.q, self.k, self.v, self.cache.bt,
+            self.cache.bt_stride, len(self.lens), self.hq, self.batch.scale,
+            self.ws if ws is None else ws, out, lse, stream=stream)
+
+    def unturned(self):
+        """libra_append_attn on the projections as they are."""
+        out, lse = self.outputs()
+        libra.libra_append_attn(self.cache.layout, self.plan, self.q.contiguous(),
+                                self.k.contiguous(), self.v.contiguous(), self.cache.bt,
+                                self.cache.bt_stride, len(self.lens), self.hq, self.batch.scale,
+                                self.ws, out, lse)
+        torch.cuda.synchronize()
+        return out, lse, self.cache.k.clone(), self.cache.v.clone()
+
+    def one_step(self, rope, **kw):
+        out, lse = self.outputs()
+        self.call(rope, out, lse, **kw)
+        torch.cuda.synchronize()
+        return out, lse, self.cache.k.clone(), self.cache.v.clone()
+
+    def tokens(self):
+        """[sequence] -> (K, V), [length, hkv, 128] as cached, bf16."""
+        k, v = torch.empty_like(self.cache.k), torch.empty_like(self.cache.v)
+        libra.libra_kv_unpack_pages(self.cache.layout, k, v, 0, self.cache.num_pages)
+        k, v = (t.view(BF16).view(-1, self.hkv, 16, 128) for t in (k, v))
+        for b, n in enumerate(self.lens):
+            ids = self.cache.bt[b, :(n + 15) // 16].long()
+            yield [t[ids].transpose(1, 2).reshape(-1, self.hkv, 128)[:n] for t in (k, v)]
+
+    def check(self, rope, got, label):
+        """The cache and the outputs after a call."""
+        out, lse = H.bf16_dev_to_f64(got[0]), got[1].double().cpu().numpy()
+        turned = torch.empty((self.rows, self.hkv, 128), dtype=BF16, device="cuda")
+        libra.libra_rotary_apply(rope.h, self.k, self.pd, turned)
+        q = torch.from_numpy(rope.turn(f64(self.q), self.pos)).cuda()
+        G, r0, worst, rms = self.hq // self.hkv, 0, 0.0, []
+        ro, rl = torch.empty_like(q), torch.empty(q.shape[:2], dtype=torch.float64, device="cuda")
+        for (k, v), n, c in zip(self.tokens(), self.lens, self.news):
+            rows = slice(r0, r0 + c)
+            assert torch.equal(k[n - c:], turned[rows]) and torch.equal(v[n - c:], self.v[rows]), label
+            seen = torch.arange(n, device="cuda")[None] <= torch.arange(n - c, n, device="cuda")[:, None]
+            for h in range(self.hq):
+                z = (q[rows, h] @ k[:, h // G].double().t()) * self.batch.scale
+                z.masked_fill_(~seen, -np.inf)
+                rl[rows, h] = torch.logsumexp(z, dim=1)
+                ro[rows, h] = torch.exp(z - rl[rows, h][:, None]) @ v[:, h // G].double()
+            size = self.batch.scale * q[rows].norm(dim=-1).max() * k.double().norm(dim=-1).max()
+            # ... and float32 exponentials and logarithm of a sum.
+            tol = float(size) * (2.0 ** -17 + 2.0 ** -17) + 2.0 ** -20 * (4 + np.abs(rl[rows].cpu().numpy()))
+            err = np.abs(lse[rows] - rl[rows].cpu().numpy())
+            worst = max(worst, float((err / tol).max()))
+            rms.append(err.ravel() ** 2)
+            r0 += c
+        rms = float(np.sqrt(np.concatenate(rms).mean()))
+        H.say(f"[parity] {label}: lse error {worst:.3f} of its bound, rms {rms:.2e}")
+        assert worst <= 1.0, label
+        # Independent parts: 2^-18 / sqrt(3) of scores of size 1 to 2, and float32's roundings.
+        assert rms <= 1e-5, label
+        H.assert_parity(out, lse, ro.cpu().numpy(), rl.cpu().numpy(), label=label)
+
+    def close(self):
+        libra.libra_plan_destroy(self.plan)
+        self.cache.close()
+
+
+def same(a, b, label):
+    for x, y, what in zip(a, b, ("out", "lse", "k", "v")):
+        x, y = (t.view(torch.int32) if t.dtype == torch.float32 else t for t in (x, y))
+        assert torch.equal(x, y), f"{label}: {what} differs"
+
+
+CASES = [
+    # lens, news, hq, hkv, plan parameters
+    ("decode rows", [1, 2, 17, 300, 5000, 64], [1] * 6, 28, 4, dict(num_cus=64)),
+    ("one decode row", [700], [1], 40, 8, {}),
+    ("prompt of one page", [16], [16], 4, 2, {}),
+    ("first tokens", [1, 2, 3], [1, 2, 3], 8, 8, {}),
+    ("mixed", [70, 300, 45, 2200, 33], [1, 100, 45, 1, 2], 32, 8, dict(num_cus=32, units_per_cu=1,
+                                                                     min_split_pages=2)),
+    ("one head a group", [600, 90], [333, 1], 4, 4, {}),
+    ("three heads a group", [600, 90], [333, 70], 12, 4, {}),
+    ("seven heads a group", [1000, 50], [400, 20], 14, 2, {}),
+    ("sixteen heads a group", [300, 1500], [50, 200], 32, 2, {}),
+    ("split keys", [2900, 700], [32, 1], 8, 2, dict(num_cus=4)),
+    ("wide tiles", [2100, 1500, 900], [2100, 700, 900], 40, 8, dict(num_cus=16)),
+    ("long prior", [70000], [40], 10, 2, {}),
+]
+ROPES = [dict(), dict(rdim=64, interleaved=True), dict(rdim=20), dict(rdim=96, amplitude=1.25),
+         dict(interleaved=True), dict(rdim=32), dict(rdim=2, interleaved=True), dict(rdim=112)]
+
+
+def still():
+    """A rotary that turns nothing."""
+    r = Handle(rdim=44)
+    libra.libra_rotary_destroy(r.h)
+    r.theta = np.zeros(22, np.longdouble)
+    r.h = libra.libra_rotary_create(rotary_dim=44, frequencies=np.zeros(22))
+    return r
+
+
+@pytest.mark.parametrize("shift", [None, 100000])
+@pytest.mark.parametrize("case", range(len(CASES)), ids=[c[0] for c in CASES])
+def test_cases(case, shift):
+    name, lens, news, hq, hkv, params = CASES[case]
+    s = Step(lens, news, hq, hkv, seed=case, shift=shift, **params)
+    plain = s.unturned()
+    s.reset()
+    rope = still()
+    same(s.one_step(rope), plain, f"{name}, still")
+    rope.close()
+    for j in range(2):
+        kw = ROPES[(case + 3 * j + 5 * (shift is not None)) % len(ROPES)]
+        H.say(f"[case] append rotary {name} shift={shift} {kw}")
+        rope = Handle(**kw)
+        s.reset()
+        s.check(rope, s.one_step(rope), f"{name} {kw}")
+        rope.close()
+    s.close()
+
+
+@pytest.mark.parametrize("seed", range(8))
+def test_random_batches(seed):
+    rng = np.random.default_rng(300 + seed)
+    hkv, G, B = int(rng.choice([1, 2, 3, 8])), int(rng.choice([1, 2, 4, 5, 7, 8])), int(rng.integers(1, 12))
+    news = [int(rng.choice([1, 1, 2, 15, 16, 17, 64, 300])) for _ in range(B)]
+    lens = [c + int(rng.choice([0, 1, 15, 31, 500, 2000])) for c in news]
+    params = dict(num_cus=int(rng.choice([4, 16, 64, 256])), min_split_pages=int(rng.choice([1, 4, 16])))
+    s = Step(lens, news, G * hkv, hkv, seed=seed, shift=int(rng.integers(0, 5000)), **params)
+    rope = Handle(rdim=2 * int(rng.integers(1, 65)), interleaved=bool(rng.integers(2)))
+    H.say(f"[case] append rotary random {seed}: G={G} hkv={hkv} lens={lens} news={news} R={rope.rdim}")
+    s.check(rope, s.one_step(rope), f"random {seed}")
+    rope.close()
+    s.close()
+
+
+def test_smaller_workspace_other_stream_and_no_lse():
+    H.say("[case] append rotary workspace and stream")
+    s = Step([2900, 700], [32, 1], 8, 2, num_cus=4)
+    rope = Handle()
+    two = s.one_step(rope)
+    s.reset()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    small = torch.empty(H.plain_workspace(s.plan), dtype=torch.uint8, device="cuda")
+    out, lse = s.outputs()
+    torch.cuda.synchronize()
+    s.call(rope, out, lse, ws=small, stream=side)
+    torch.cuda.synchronize()
+    H.assert_parity(H.bf16_dev_to_f64(out), lse.double().cpu().numpy(), H.bf16_dev_to_f64(two[0]),
+                    two[1].double().cpu().numpy(), label="whole tiles against split ones")
+    out2, _ = s.outputs()
+    s.call(rope, out2, None, ws=small)
+    torch.cuda.synchronize()
+    assert torch.equal(out, out2)
+    rope.close()
+    s.close()
+
+
+def test_replays_from_a_graph_with_new_positions():
+    H.say("[case] append rotary graph")
+    s = Step([600, 1500, 300, 2200], [1, 200, 64, 1], 32, 8, shift=7, num_cus=32, units_per_cu=1,
+             min_split_pages=2)
+    rope = Handle(rdim=64)
+    out, lse = s.outputs()
+    s.call(rope, out, lse)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        s.call(rope, out, lse)
+    for i in range(3):
+        s.pd.add_(1000)
+        torch.cuda.synchronize()
+        s.reset()
+        out.fill_(NAN)
+        lse.fill_(float("nan"))
+        g.replay()
+        torch.cuda.synchronize()
+        got = out.clone(), lse.clone(), s.cache.k.clone(), s.cache.v.clone()
+        s.reset()
+        same(s.one_step(rope), got, f"replay {i}")
+    del g
+    rope.close()
+    s.close()
+
+
+def test_stale_nan_behind_the_last_token():
+    """Slots behind a sequence's end hold NaN: nothing of them comes out."""
+    H.say("[case] append rotary stale slots")
+    s = Step([37, 100], [5, 1], 8, 2)
+    rope = Handle()
+    clean = s.one_step(rope)
+    s.reset()
+    k, v = s.cache.unpack()
+    for b, n in enumerate(s.lens):
+        page, slot = int(s.batch.block_table[b, (n - 1) // 16]), (n - 1) % 16 + 1
+        k[page, :, slot:] = NAN
+        v[page, :, slot:] = NAN
+    libra.libra_kv_pack_pages(s.cache.layout, H.u16_to_dev(k), H.u16_to_dev(v), 0, s.cache.num_pages)
+    dirty = s.one_step(rope)
+    same(dirty[:2], clean[:2], "stale")
+    rope.close()
+    s.close()
