@@ -53,9 +53,9 @@ struct Fp32 {
   }
 };
 
+// Rows x heads to turn, for both forms below.
 template <class T>
-struct ApplyArgs {
-  RotaryArgs<kMaxPairs> rot;
+struct RowsArgs {
   const typename T::Elem* x;
   typename T::Elem* out;
   int64_t x_row, x_head, out_row, out_head;
@@ -66,39 +66,65 @@ struct ApplyArgs {
   int heads, dim;
   int backward;
   // The wide form's block: per_row = per_head * head_slots threads take a row, each one of its
-  // eight-channel pieces in kHeads heads, head_slots apart.
-  int per_head, head_slots, per_row, block_rows;
+  // eight-channel pieces in up to kHeads heads, head_slots apart; y_blocks blocks share a row.
+  int per_head, head_slots, per_row, block_rows, y_blocks;
 };
 
-// Sign of the sine: the gradient turns back.
-template <class Args>
-__device__ __forceinline__ float2 cos_sin_of(const Args& A, int j, int32_t pos) {
-  float2 cs = rotary_cos_sin(A.rot.turn[j], pos, A.rot.amplitude);
-  if (A.backward) cs.y = -cs.y;
-  return cs;
+template <class T>
+__device__ __forceinline__ bool skipped(const RowsArgs<T>& A, int64_t row) {
+  return A.slots && uint64_t(A.slots[row]) >= uint64_t(A.slot_end);
 }
 
-template <class Args>
-__device__ __forceinline__ bool skipped(const Args& A, int64_t row) {
-  return A.slots && uint64_t(A.slots[row]) >= uint64_t(A.slot_end);
+// Four pairs in two quads, which is what a thread turns: half pairing takes channel e of both
+// quads as a pair, interleaved pairing two neighbours of one.
+template <class T, bool kInter>
+__device__ __forceinline__ void turn_quads(typename T::Quad& a, typename T::Quad& b,
+                                           const float2 (&cs)[4]) {
+  float f[4], g[4], y[4], z[4];
+  T::unpack(a, f);
+  T::unpack(b, g);
+  if (kInter) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      y[2 * e] = turn_first(f[2 * e], f[2 * e + 1], cs[e]);
+      y[2 * e + 1] = turn_second(f[2 * e], f[2 * e + 1], cs[e]);
+      z[2 * e] = turn_first(g[2 * e], g[2 * e + 1], cs[2 + e]);
+      z[2 * e + 1] = turn_second(g[2 * e], g[2 * e + 1], cs[2 + e]);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      y[e] = turn_first(f[e], g[e], cs[e]);
+      z[e] = turn_second(f[e], g[e], cs[e]);
+    }
+  }
+  a = T::pack(y);
+  b = T::pack(z);
+}
+
+// The quads of piece j of a head: pairs 4 j .. 4 j + 3 while j < R / 8, copied ones after.
+template <bool kInter>
+__device__ __forceinline__ int2 quads_of(int j, int R8) {
+  return kInter || j >= R8 ? make_int2(2 * j, 2 * j + 1) : make_int2(j, j + R8);
 }
 
 // Wide form: R and the head size are multiples of 8, rows are aligned for four channels at a
 // time.  A thread owns two quads of a head (4 pairs, or 8 copied channels), computes their
 // cosines and sines once, and turns them in up to kHeads heads.
-template <class T, bool kInter, int kHeads>
-__global__ __launch_bounds__(kThreads) void rotary_wide_kernel(ApplyArgs<T> A) {
+template <class T, bool kInter, int kHeads, class Rot>
+__device__ __forceinline__ void turn_rows_wide(const Rot& rot, const RowsArgs<T>& A, int64_t bx,
+                                               int by) {
   using Quad = typename T::Quad;
   const int t = threadIdx.x;
   const int r = t / A.per_row, in_row = t - r * A.per_row;
   const int h0 = in_row / A.per_head, j = in_row - h0 * A.per_head;
-  const int64_t row = int64_t(blockIdx.x) * A.block_rows + r;
+  const int64_t row = bx * A.block_rows + r;
   if (r >= A.block_rows || row >= A.rows || skipped(A, row)) return;
-  const int R8 = A.rot.rdim / 8;
+  const int R8 = rot.rdim / 8;
   const bool turned = j < R8;
   if (!turned && A.x == A.out) return;
-  const int qa = kInter || !turned ? 2 * j : j, qb = kInter || !turned ? 2 * j + 1 : j + R8;
-  const int head0 = blockIdx.y * A.head_slots * kHeads + h0;
+  const int2 qd = quads_of<kInter>(j, R8);
+  const int head0 = by * A.head_slots * kHeads + h0;
   const typename T::Elem* x = A.x + row * A.x_row;
   typename T::Elem* out = A.out + row * A.out_row;
   Quad a[kHeads], b[kHeads];
@@ -106,44 +132,26 @@ __global__ __launch_bounds__(kThreads) void rotary_wide_kernel(ApplyArgs<T> A) {
   for (int i = 0; i < kHeads; ++i) {
     const int h = head0 + i * A.head_slots;
     if (h < A.heads) {
-      a[i] = *reinterpret_cast<const Quad*>(x + h * A.x_head + 4 * qa);
-      b[i] = *reinterpret_cast<const Quad*>(x + h * A.x_head + 4 * qb);
+      a[i] = *reinterpret_cast<const Quad*>(x + h * A.x_head + 4 * qd.x);
+      b[i] = *reinterpret_cast<const Quad*>(x + h * A.x_head + 4 * qd.y);
     }
   }
   float2 cs[4];
   if (turned) {
     const int32_t pos = A.positions[row];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) cs[i] = cos_sin_of(A, 4 * j + i, pos);
+    for (int i = 0; i < 4; ++i) {
+      cs[i] = rotary_cos_sin(rot.turn[4 * j + i], pos, rot.amplitude);
+      if (A.backward) cs[i].y = -cs[i].y;
+    }
   }
 #pragma unroll
   for (int i = 0; i < kHeads; ++i) {
     const int h = head0 + i * A.head_slots;
     if (h < A.heads) {
-      if (turned) {
-        float f[4], g[4], y[4], z[4];
-        T::unpack(a[i], f);
-        T::unpack(b[i], g);
-        if (kInter) {
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            y[2 * e] = turn_first(f[2 * e], f[2 * e + 1], cs[e]);
-            y[2 * e + 1] = turn_second(f[2 * e], f[2 * e + 1], cs[e]);
-            z[2 * e] = turn_first(g[2 * e], g[2 * e + 1], cs[2 + e]);
-            z[2 * e + 1] = turn_second(g[2 * e], g[2 * e + 1], cs[2 + e]);
-          }
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            y[e] = turn_first(f[e], g[e], cs[e]);
-            z[e] = turn_second(f[e], g[e], cs[e]);
-          }
-        }
-        a[i] = T::pack(y);
-        b[i] = T::pack(z);
-      }
-      *reinterpret_cast<Quad*>(out + h * A.out_head + 4 * qa) = a[i];
-      *reinterpret_cast<Quad*>(out + h * A.out_head + 4 * qb) = b[i];
+      if (turned) turn_quads<T, kInter>(a[i], b[i], cs);
+      *reinterpret_cast<Quad*>(out + h * A.out_head + 4 * qd.x) = a[i];
+      *reinterpret_cast<Quad*>(out + h * A.out_head + 4 * qd.y) = b[i];
     }
   }
 }
@@ -151,25 +159,27 @@ __global__ __launch_bounds__(kThreads) void rotary_wide_kernel(ApplyArgs<T> A) {
 // Narrow form: any even R, any alignment.  A thread owns one pair (or one copied channel) of
 // a row, in every kNarrowHeads heads of its block row.
 constexpr int kNarrowHeads = 8;
-template <class T>
-__global__ __launch_bounds__(kThreads) void rotary_narrow_kernel(ApplyArgs<T> A) {
-  const int half = A.rot.rdim / 2;
+template <class T, class Rot>
+__device__ __forceinline__ void turn_rows_narrow(const Rot& rot, const RowsArgs<T>& A, int64_t bx,
+                                                 int by) {
+  const int half = rot.rdim / 2;
   const int items = A.dim - half;
-  const int64_t idx = int64_t(blockIdx.x) * kThreads + threadIdx.x;
+  const int64_t idx = bx * kThreads + threadIdx.x;
   const int64_t row = idx / items;
   const int j = int(idx - row * items);
   if (row >= A.rows || skipped(A, row)) return;
   const typename T::Elem* x = A.x + row * A.x_row;
   typename T::Elem* out = A.out + row * A.out_row;
-  const int h0 = blockIdx.y * kNarrowHeads, h1 = min(A.heads, h0 + kNarrowHeads);
+  const int h0 = by * kNarrowHeads, h1 = min(A.heads, h0 + kNarrowHeads);
   if (j >= half) {
     if (A.x == A.out) return;
     const int d = j + half;
     for (int h = h0; h < h1; ++h) out[h * A.out_head + d] = x[h * A.x_head + d];
     return;
   }
-  const int d1 = A.rot.interleaved ? 2 * j : j, d2 = A.rot.interleaved ? 2 * j + 1 : j + half;
-  const float2 cs = cos_sin_of(A, j, A.positions[row]);
+  const int d1 = rot.interleaved ? 2 * j : j, d2 = rot.interleaved ? 2 * j + 1 : j + half;
+  float2 cs = rotary_cos_sin(rot.turn[j], A.positions[row], rot.amplitude);
+  if (A.backward) cs.y = -cs.y;
   for (int h = h0; h < h1; ++h) {
     const float x1 = T::get(x[h * A.x_head + d1]), x2 = T::get(x[h * A.x_head + d2]);
     out[h * A.out_head + d1] = T::put(turn_first(x1, x2, cs));
@@ -177,51 +187,83 @@ __global__ __launch_bounds__(kThreads) void rotary_narrow_kernel(ApplyArgs<T> A)
   }
 }
 
+template <class T, bool kInter, int kHeads>
+__global__ __launch_bounds__(kThreads) void rotary_wide_kernel(RotaryArgs<kMaxPairs> rot,
+                                                               RowsArgs<T> A) {
+  turn_rows_wide<T, kInter, kHeads>(rot, A, blockIdx.x, blockIdx.y);
+}
+template <class T>
+__global__ __launch_bounds__(kThreads) void rotary_narrow_kernel(RotaryArgs<kMaxPairs> rot,
+                                                                 RowsArgs<T> A) {
+  turn_rows_narrow(rot, A, blockIdx.x, blockIdx.y);
+}
+
 constexpr int64_t kMaxBlocks = int64_t(1) << 22;  // per launch: 2^30 threads
 
+// How rows x heads are cut: the form, heads per thread, rows per block.
 template <class T>
-hipError_t apply(const Rotary& r, const RotaryRows& a, const int64_t* slots, int64_t slot_end,
-                 hipStream_t s) {
-  using Elem = typename T::Elem;
-  ApplyArgs<T> A;
-  A.rot = rotary_args<kMaxPairs>(r);
+struct RowsPlan {
+  RowsArgs<T> args;
+  bool wide, many;
+  int threads;
+  // Blocks along x for `rows` rows, and the rows that n of them take.
+  int64_t blocks(int64_t rows) const {
+    return wide ? (rows + args.block_rows - 1) / args.block_rows
+                : (rows * items() + kThreads - 1) / kThreads;
+  }
+  int64_t rows_of(int64_t n) const { return wide ? n * args.block_rows : n * kThreads / items(); }
+  int64_t items() const { return args.dim - half; }
+  int half;
+};
+
+template <class T>
+RowsPlan<T> plan_rows(const Rotary& r, const RotaryRows& a) {
+  RowsPlan<T> p{};
+  RowsArgs<T>& A = p.args;
+  A.x = static_cast<const typename T::Elem*>(a.x);
+  A.out = static_cast<typename T::Elem*>(a.out);
   A.x_row = a.x_row, A.x_head = a.x_head, A.out_row = a.out_row, A.out_head = a.out_head;
-  A.slot_end = slot_end;
+  A.positions = a.positions;
+  A.rows = a.rows;
   A.heads = a.heads, A.dim = r.head_dim;
   A.backward = a.backward;
   A.per_head = r.head_dim / 8;
   const size_t quad = sizeof(typename T::Quad);
-  const bool wide = r.rotary_dim % 8 == 0 && r.head_dim % 8 == 0 &&
-                    (reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.out)) % quad == 0 &&
-                    ((a.x_row | a.x_head | a.out_row | a.out_head) & 3) == 0;
-  const bool many = a.rows * a.heads * A.per_head >= int64_t(4) * 2048 * kThreads;
-  const int per_thread = many ? 4 : 1;
-  if (wide) {
+  p.wide = r.rotary_dim % 8 == 0 && r.head_dim % 8 == 0 &&
+           (reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.out)) % quad == 0 &&
+           ((a.x_row | a.x_head | a.out_row | a.out_head) & 3) == 0;
+  p.many = a.rows * a.heads * A.per_head >= int64_t(4) * 2048 * kThreads;
+  const int per_thread = p.many ? 4 : 1;
+  p.threads = kThreads;
+  A.y_blocks = (a.heads + kNarrowHeads - 1) / kNarrowHeads;
+  p.half = r.rotary_dim / 2;
+  if (p.wide) {
     A.head_slots = std::min<int>((a.heads + per_thread - 1) / per_thread, kThreads / A.per_head);
     A.per_row = A.head_slots * A.per_head;
     A.block_rows = kThreads / A.per_row;
+    A.y_blocks = (a.heads + A.head_slots * per_thread - 1) / (A.head_slots * per_thread);
+    p.threads = A.per_row * A.block_rows;
   }
-  const int items = r.head_dim - r.rotary_dim / 2;
-  const int64_t rows_per_launch = wide ? kMaxBlocks * A.block_rows : kMaxBlocks * kThreads / items;
-  for (int64_t r0 = 0; r0 < a.rows; r0 += rows_per_launch) {
-    A.rows = std::min(rows_per_launch, a.rows - r0);
-    A.x = static_cast<const Elem*>(a.x) + r0 * a.x_row;
-    A.out = static_cast<Elem*>(a.out) + r0 * a.out_row;
-    A.positions = a.positions + r0;
-    A.slots = slots ? slots + r0 : nullptr;
-    if (wide) {
-      const int per_block = A.head_slots * per_thread;
-      const dim3 grid(unsigned((A.rows + A.block_rows - 1) / A.block_rows),
-                      unsigned((a.heads + per_block - 1) / per_block));
-      const bool inter = r.pairing == LIBRA_ROTARY_INTERLEAVED;
-      auto k = many ? (inter ? rotary_wide_kernel<T, true, 4> : rotary_wide_kernel<T, false, 4>)
-                    : (inter ? rotary_wide_kernel<T, true, 1> : rotary_wide_kernel<T, false, 1>);
-      hipLaunchKernelGGL(k, grid, dim3(unsigned(A.per_row * A.block_rows)), 0, s, A);
-    } else {
-      const dim3 grid(unsigned((A.rows * items + kThreads - 1) / kThreads),
-                      unsigned((a.heads + kNarrowHeads - 1) / kNarrowHeads));
-      hipLaunchKernelGGL(rotary_narrow_kernel<T>, grid, dim3(kThreads), 0, s, A);
-    }
+  return p;
+}
+
+template <class T>
+hipError_t apply(const Rotary& r, const RotaryRows& a, hipStream_t s) {
+  const RowsPlan<T> p = plan_rows<T>(r, a);
+  const RotaryArgs<kMaxPairs> rot = rotary_args<kMaxPairs>(r);
+  const int64_t step = p.rows_of(kMaxBlocks);
+  for (int64_t r0 = 0; r0 < a.rows; r0 += step) {
+    RowsArgs<T> A = p.args;
+    A.rows = std::min(step, a.rows - r0);
+    A.x += r0 * a.x_row;
+    A.out += r0 * a.out_row;
+    A.positions += r0;
+    const dim3 grid(unsigned(p.blocks(A.rows)), unsigned(A.y_blocks));
+    const bool inter = r.pairing == LIBRA_ROTARY_INTERLEAVED;
+    auto k = !p.wide ? rotary_narrow_kernel<T>
+             : p.many ? (inter ? rotary_wide_kernel<T, true, 4> : rotary_wide_kernel<T, false, 4>)
+                      : (inter ? rotary_wide_kernel<T, true, 1> : rotary_wide_kernel<T, false, 1>);
+    hipLaunchKernelGGL(k, grid, dim3(unsigned(p.threads)), 0, s, rot, A);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
@@ -231,7 +273,6 @@ hipError_t apply(const Rotary& r, const RotaryRows& a, const int64_t* slots, int
 // --- cache append ------------------------------------------------------------------------
 
 struct WriteArgs {
-  RotaryArgs<kRotaryPairs> rot;  // rdim 0: keys are copied
   uint16_t* k_cache;
   uint16_t* v_cache;
   const uint16_t* k_new;
@@ -243,11 +284,18 @@ struct WriteArgs {
   const int64_t* slots;
   int64_t slot_end;
   int64_t rows;
+  int64_t first_block;  // of 16 rows
+  int kv_blocks;        // blocks of this launch that write the cache; the others turn queries
   // by an append plan's records
   const int32_t* writes;
   const int32_t* bt;
   int64_t bt_stride;
 };
+using Rot = RotaryArgs<kRotaryPairs>;  // rdim 0: keys are copied
+
+// How a key is turned: quads in half or interleaved pairing (R a multiple of 8; copies are
+// interleaved quads of which none turns), or granules whose pairs may lie anywhere.
+enum KeyForm : int { kHalfQuads, kInterQuads, kAnyPairs };
 
 // Element offsets inside a tile (kv_layout.hip has the layout).
 __device__ __forceinline__ int k_off(int s, int d) { return ((d >> 3) * 16 + s) * 8 + (d & 7); }
@@ -260,30 +308,80 @@ __device__ __forceinline__ void v_scatter8(uint16_t* tile, int s, int d0, uint4 
   for (int i = 0; i < 8; ++i) tile[v_off(s, d0 + i)] = uint16_t(w[i / 2] >> (16 * (i & 1)));
 }
 
-// Granule j (8 channels) of row `row`'s key of head g, turned.  The 16 threads of a row, in
-// one wave, share the row's cosines and sines through cs.
-__device__ __forceinline__ uint4 key_granule(const WriteArgs& A, int64_t row, int g, int j,
-                                             int32_t pos, float2* cs) {
+// What thread j of a row's 16 holds of it, for one KV head: eight channels of the key (two
+// quads; not used by kAnyPairs, which reads them when it turns them) and of the value.
+struct NewPiece {
+  uint2 a, b;
+  uint4 v;
+  int32_t pos;
+};
+
+template <int kForm>
+__device__ __forceinline__ NewPiece load_piece(const WriteArgs& A, const Rot& rot, int64_t row,
+                                               int g, int j) {
+  NewPiece p;
   const uint16_t* k = A.k_new + row * A.k_row + g * kDim;
-  if (A.rot.rdim == 0) return *reinterpret_cast<const uint4*>(k + 8 * j);
-#pragma unroll
-  for (int i = 0; i < 4; ++i)
-    if (4 * j + i < A.rot.rdim / 2)
-      cs[4 * j + i] = rotary_cos_sin(A.rot.turn[4 * j + i], pos, A.rot.amplitude);
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  return turned_granule<false>(k, j, cs, A.rot.rdim, A.rot.interleaved).hi;
+  if constexpr (kForm != kAnyPairs) {
+    const int2 qd = quads_of<kForm == kInterQuads>(j, rot.rdim / 8);
+    p.a = *reinterpret_cast<const uint2*>(k + 4 * qd.x);
+    p.b = *reinterpret_cast<const uint2*>(k + 4 * qd.y);
+  }
+  p.v = *reinterpret_cast<const uint4*>(A.v_new + row * A.v_row + g * kDim + 8 * j);
+  p.pos = rot.rdim && A.positions ? A.positions[row] : 0;
+  return p;
 }
 
-// Block (i, g): new rows [16 i, 16 i + 16) of KV head g.  Rows with consecutive slots of one
-// page form a run; the block writes the runs that begin among its rows, so a long chunk's
-// blocks write whole pages wherever its pages begin.  Whole pages go through LDS (V tiles are
-// transposed), single rows straight to their slots.
-__global__ __launch_bounds__(kThreads) void kv_append_kernel(WriteArgs A, int64_t block0) {
+// Turns the piece's key and stores it to slot s of the K tile.  kAnyPairs: the 16 threads of
+// a row, in one wave, share the row's cosines and sines through cs.
+template <int kForm>
+__device__ __forceinline__ void store_key(const WriteArgs& A, const Rot& rot, const NewPiece& p,
+                                          int64_t row, int g, int j, int s, uint16_t* tile,
+                                          float2* cs) {
+  if constexpr (kForm == kAnyPairs) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (4 * j + i < rot.rdim / 2)
+        cs[4 * j + i] = rotary_cos_sin(rot.turn[4 * j + i], p.pos, rot.amplitude);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    const uint16_t* k = A.k_new + row * A.k_row + g * kDim;
+    *reinterpret_cast<uint4*>(tile + k_off(s, 8 * j)) =
+        turned_granule<false>(k, j, cs, rot.rdim, rot.interleaved).hi;
+  } else {
+    constexpr bool kInter = kForm == kInterQuads;
+    const int2 qd = quads_of<kInter>(j, rot.rdim / 8);
+    uint2 a = p.a, b = p.b;
+    if (j < rot.rdim / 8) {
+      float2 t[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) t[i] = rotary_cos_sin(rot.turn[4 * j + i], p.pos, rot.amplitude);
+      turn_quads<Bf16, kInter>(a, b, t);
+    }
+    *reinterpret_cast<uint2*>(tile + k_off(s, 4 * qd.x)) = a;
+    *reinterpret_cast<uint2*>(tile + k_off(s, 4 * qd.y)) = b;
+  }
+}
+
+// Blocks below kv_blocks: new rows [16 i, 16 i + 16) of one KV head.  Rows with consecutive
+// slots of one page form a run; the block writes the runs that begin among its rows, so a long
+// chunk's blocks write whole pages wherever its pages begin.  Whole pages go through LDS (V
+// tiles are transposed), single rows straight to their slots.  The other blocks turn queries.
+template <int kForm, int kHeads>
+__global__ __launch_bounds__(kThreads) void kv_append_kernel(Rot rot, WriteArgs A,
+                                                             RowsArgs<Bf16> Q) {
   __shared__ __align__(16) uint16_t vt[kTileElems];
-  __shared__ __align__(16) float2 cs[kPage][kRotaryPairs];
-  const int g = blockIdx.y;
-  const int64_t r0 = (block0 + blockIdx.x) * kPage;
+  __shared__ __align__(16) float2 cs[kForm == kAnyPairs ? kPage : 1][kRotaryPairs];
+  if (int(blockIdx.x) >= A.kv_blocks) {
+    const int i = int(blockIdx.x) - A.kv_blocks;
+    const int bx = i / Q.y_blocks;
+    if constexpr (kForm == kAnyPairs)
+      turn_rows_narrow<Bf16>(rot, Q, bx, i - bx * Q.y_blocks);
+    else
+      turn_rows_wide<Bf16, kForm == kInterQuads, kHeads>(rot, Q, bx, i - bx * Q.y_blocks);
+    return;
+  }
+  const int blk = int(blockIdx.x) / A.hkv, g = int(blockIdx.x) - blk * A.hkv;
+  const int64_t r0 = (A.first_block + blk) * kPage;
   const int t = threadIdx.x, lane = t & 63;
   const int s = t >> 4, j = t & 15;
   // Lane l looks at row r0 - 1 + l.
@@ -303,33 +401,30 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(WriteArgs A, int64_
   if (whole) {
     const int64_t row = r0 + a + s;
     const size_t base = (size_t(first >> 4) * A.hkv + g) * kTileElems;
-    const uint4 v = *reinterpret_cast<const uint4*>(A.v_new + row * A.v_row + g * kDim + 8 * j);
-    const int32_t pos = A.rot.rdim ? A.positions[row] : 0;
-    const uint4 k = key_granule(A, row, g, j, pos, cs[s]);
-    *reinterpret_cast<uint4*>(A.k_cache + base + k_off(s, 8 * j)) = k;
-    v_scatter8(vt, s, 8 * j, v);
+    const NewPiece p = load_piece<kForm>(A, rot, row, g, j);
+    v_scatter8(vt, s, 8 * j, p.v);
+    store_key<kForm>(A, rot, p, row, g, j, s, A.k_cache + base, cs[kForm == kAnyPairs ? s : 0]);
     __syncthreads();
     *reinterpret_cast<uint4*>(A.v_cache + base + t * 8) = *reinterpret_cast<const uint4*>(vt + t * 8);
     return;
   }
   for (int i = a + s; i - s < e; i += kPage) {
-    const int64_t at = __shfl(slot, i + 1 < 64 ? i + 1 : 63);
+    const int64_t at = __shfl(slot, i + 1);
     if (i >= e || at < 0) continue;
     const int64_t row = r0 + i;
     const size_t base = (size_t(at >> 4) * A.hkv + g) * kTileElems;
     const int sl = int(at & 15);
-    const uint4 v = *reinterpret_cast<const uint4*>(A.v_new + row * A.v_row + g * kDim + 8 * j);
-    const int32_t pos = A.rot.rdim ? A.positions[row] : 0;
-    const uint4 k = key_granule(A, row, g, j, pos, cs[s]);
-    *reinterpret_cast<uint4*>(A.k_cache + base + k_off(sl, 8 * j)) = k;
-    v_scatter8(A.v_cache + base, sl, 8 * j, v);
+    const NewPiece p = load_piece<kForm>(A, rot, row, g, j);
+    v_scatter8(A.v_cache + base, sl, 8 * j, p.v);
+    store_key<kForm>(A, rot, p, row, g, j, sl, A.k_cache + base, cs[kForm == kAnyPairs ? s : 0]);
   }
 }
 
 // Block (w, g): record w of an append plan's write table, as cache_write_kernel.
-__global__ __launch_bounds__(kThreads) void cache_write_rotary_kernel(WriteArgs A) {
+template <int kForm>
+__global__ __launch_bounds__(kThreads) void cache_write_rotary_kernel(Rot rot, WriteArgs A) {
   __shared__ __align__(16) uint16_t vt[kTileElems];
-  __shared__ __align__(16) float2 cs[kPage][kRotaryPairs];
+  __shared__ __align__(16) float2 cs[kForm == kAnyPairs ? kPage : 1][kRotaryPairs];
   const int32_t* w = A.writes + size_t(blockIdx.x) * kWriteInts;
   const int g = blockIdx.y;
   const int b = w[W_B], pg = w[W_PAGE], s0 = w[W_SLOT0], s1 = w[W_SLOT1];
@@ -337,27 +432,24 @@ __global__ __launch_bounds__(kThreads) void cache_write_rotary_kernel(WriteArgs 
   const int s = t >> 4, j = t & 15;
   const int from = min(max(s, s0), s1 - 1);  // a new slot: the loads then need no mask
   const int64_t row = int64_t(w[W_ROW]) + from - s0;
-  const uint4 v = *reinterpret_cast<const uint4*>(A.v_new + row * A.v_row + g * kDim + 8 * j);
+  NewPiece p = load_piece<kForm>(A, rot, row, g, j);
+  if (!A.positions) p.pos = pg * kPage + from;
   const int64_t page = A.bt[int64_t(b) * A.bt_stride + pg];
-  const int32_t pos = A.positions ? A.positions[row] : pg * kPage + from;
-  const uint4 k = key_granule(A, row, g, j, pos, cs[s]);
   const size_t base = (size_t(page) * A.hkv + g) * kTileElems;
   if (s1 - s0 < kPage) {  // uniform over the block
-    if (s == from) {
-      *reinterpret_cast<uint4*>(A.k_cache + base + k_off(s, 8 * j)) = k;
-      v_scatter8(A.v_cache + base, s, 8 * j, v);
-    }
+    if (s != from) return;
+    v_scatter8(A.v_cache + base, s, 8 * j, p.v);
+    store_key<kForm>(A, rot, p, row, g, j, s, A.k_cache + base, cs[kForm == kAnyPairs ? s : 0]);
     return;
   }
-  *reinterpret_cast<uint4*>(A.k_cache + base + k_off(s, 8 * j)) = k;
-  v_scatter8(vt, s, 8 * j, v);
+  v_scatter8(vt, s, 8 * j, p.v);
+  store_key<kForm>(A, rot, p, row, g, j, s, A.k_cache + base, cs[kForm == kAnyPairs ? s : 0]);
   __syncthreads();
   *reinterpret_cast<uint4*>(A.v_cache + base + t * 8) = *reinterpret_cast<const uint4*>(vt + t * 8);
 }
 
 WriteArgs write_args(const KvLayout& L, const NewRows& n) {
   WriteArgs A{};
-  if (n.rotary) A.rot = rotary_args<kRotaryPairs>(*n.rotary);
   A.k_cache = static_cast<uint16_t*>(L.desc.k_cache);
   A.v_cache = static_cast<uint16_t*>(L.desc.v_cache);
   A.k_new = static_cast<const uint16_t*>(n.k);
@@ -368,34 +460,61 @@ WriteArgs write_args(const KvLayout& L, const NewRows& n) {
   return A;
 }
 
+KeyForm key_form(const Rotary* r) {
+  if (!r) return kInterQuads;
+  if (r->rotary_dim % 8) return kAnyPairs;
+  return r->pairing == LIBRA_ROTARY_INTERLEAVED ? kInterQuads : kHalfQuads;
+}
+
 }  // namespace
 
 hipError_t launch_rotary(const Rotary& r, const RotaryRows& a, hipStream_t s) {
   switch (a.dtype) {
-    case LIBRA_DTYPE_BF16: return apply<Bf16>(r, a, nullptr, 0, s);
-    case LIBRA_DTYPE_FP16: return apply<Fp16>(r, a, nullptr, 0, s);
-    default: return apply<Fp32>(r, a, nullptr, 0, s);
+    case LIBRA_DTYPE_BF16: return apply<Bf16>(r, a, s);
+    case LIBRA_DTYPE_FP16: return apply<Fp16>(r, a, s);
+    default: return apply<Fp32>(r, a, s);
   }
 }
 
 hipError_t launch_kv_append(const KvLayout& L, const NewRows& n, const int64_t* slots,
                             int64_t rows, int32_t hq, void* q_out, hipStream_t s) {
+  Rot rot{};
+  if (n.rotary) rot = rotary_args<kRotaryPairs>(*n.rotary);
+  const KeyForm form = key_form(n.rotary);
+  RowsPlan<Bf16> q{};
+  if (hq > 0)
+    q = plan_rows<Bf16>(*n.rotary, {n.q, q_out, n.q_row, kDim, int64_t(hq) * kDim, kDim, n.positions,
+                                    rows, hq, LIBRA_DTYPE_BF16, false});
+  auto k = form == kAnyPairs     ? kv_append_kernel<kAnyPairs, 1>
+           : form == kInterQuads ? (q.many ? kv_append_kernel<kInterQuads, 4> : kv_append_kernel<kInterQuads, 1>)
+                                 : (q.many ? kv_append_kernel<kHalfQuads, 4> : kv_append_kernel<kHalfQuads, 1>);
+  // Rows that one launch takes: at most kMaxBlocks blocks of either kind.
   WriteArgs A = write_args(L, n);
   A.slots = slots;
   A.slot_end = L.desc.num_pages * kPage;
   A.rows = rows;
-  const int64_t blocks = (rows + kPage - 1) / kPage;
-  for (int64_t b0 = 0; b0 < blocks; b0 += kMaxBlocks) {
-    const int64_t n_blocks = std::min(kMaxBlocks, blocks - b0);
-    hipLaunchKernelGGL(kv_append_kernel, dim3(unsigned(n_blocks), unsigned(A.hkv)),
-                       dim3(kThreads), 0, s, A, b0);
+  int64_t step = kMaxBlocks / A.hkv * kPage;
+  if (hq > 0) step = std::max<int64_t>(kPage, std::min(step, q.rows_of(kMaxBlocks / q.args.y_blocks)) / kPage * kPage);
+  for (int64_t r0 = 0; r0 < rows; r0 += step) {
+    const int64_t n_rows = std::min(step, rows - r0);
+    A.first_block = r0 / kPage;
+    A.kv_blocks = int((n_rows + kPage - 1) / kPage * A.hkv);
+    RowsArgs<Bf16> Q = q.args;
+    int64_t blocks = A.kv_blocks;
+    if (hq > 0) {
+      Q.rows = n_rows;
+      Q.x += r0 * Q.x_row;
+      Q.out += r0 * Q.out_row;
+      Q.positions += r0;
+      Q.slots = slots + r0;
+      Q.slot_end = A.slot_end;
+      blocks += q.blocks(n_rows) * Q.y_blocks;
+    }
+    hipLaunchKernelGGL(k, dim3(unsigned(blocks)), dim3(kThreads), 0, s, rot, A, Q);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (hq == 0) return hipSuccess;
-  const RotaryRows a{n.q, q_out, n.q_row, kDim, int64_t(hq) * kDim, kDim, n.positions, rows, hq,
-                     LIBRA_DTYPE_BF16, false};
-  return apply<Bf16>(*n.rotary, a, slots, A.slot_end, s);
+  return hipSuccess;
 }
 
 hipError_t launch_cache_write_rotary(const KvLayout& L, const Plan& P, const void* ws,
@@ -407,8 +526,12 @@ hipError_t launch_cache_write_rotary(const KvLayout& L, const Plan& P, const voi
   A.writes = reinterpret_cast<const int32_t*>(static_cast<const char*>(ws) + P.off_writes);
   A.bt = bt;
   A.bt_stride = stride;
-  hipLaunchKernelGGL(cache_write_rotary_kernel, dim3(unsigned(tiles), unsigned(A.hkv)),
-                     dim3(kThreads), 0, s, A);
+  const KeyForm form = key_form(n.rotary);
+  auto k = form == kAnyPairs     ? cache_write_rotary_kernel<kAnyPairs>
+           : form == kInterQuads ? cache_write_rotary_kernel<kInterQuads>
+                                 : cache_write_rotary_kernel<kHalfQuads>;
+  hipLaunchKernelGGL(k, dim3(unsigned(tiles), unsigned(A.hkv)), dim3(kThreads), 0, s,
+                     rotary_args<kRotaryPairs>(*n.rotary), A);
   return hipGetLastError();
 }
 
