@@ -208,7 +208,12 @@ void chunk_kernel(std::conditional_t<kRotary, ChunkRotaryArgs, ChunkArgs> A) {
   // 16 c + 8 hh .. + 7 of its row.
   bf16x8 qop[8];
   [[maybe_unused]] bf16x8 qlow[8];  // what bf16 leaves of turned queries
-  if constexpr (!kRotary) {
+  [[maybe_unused]] Granules<8> qin;
+  [[maybe_unused]] const int gq[8] = {hh, 2 + hh, 4 + hh, 6 + hh, 8 + hh, 10 + hh, 12 + hh, 14 + hh};
+  if constexpr (kRotary) {
+    load_granules(qin, A.q + size_t(row0 + (ok ? t_tok : 0)) * A.q_row + (size_t(g) * G + head) * kDim,
+                  gq, A.rot.rdim, A.rot.interleaved);
+  } else {
     const uint4* qrow = reinterpret_cast<const uint4*>(
         A.q + (size_t(row0 + (ok ? t_tok : 0)) * A.hq + size_t(g) * G + head) * kDim);
 #pragma unroll
@@ -291,10 +296,9 @@ void chunk_kernel(std::conditional_t<kRotary, ChunkRotaryArgs, ChunkArgs> A) {
         (wave < kWaves / 2 ? &ldk3[0][0] : &ldv3[0][0]) + (wave % (kWaves / 2)) * 256);
     const int tok0 = q0 + (r_first + 32 * wave) / G;
     const int tok1 = min(q0 + (r_first + 32 * wave + 31) / G + 1, q1);  // the wave's tokens
-    const uint16_t* const qrow =
-        A.q + size_t(row0 + (ok ? t_tok : 0)) * A.q_row + (size_t(g) * G + head) * kDim;
+    uint4 hi[8], lo[8];
 #pragma unroll
-    for (int c = 0; c < 8; ++c) qop[c] = qlow[c] = as_bf16x8(make_uint4(0, 0, 0, 0));
+    for (int c = 0; c < 8; ++c) hi[c] = lo[c] = make_uint4(0, 0, 0, 0);
     for (int base = tok0; base < tok1; base += kBatch) {
       for (int i = 0; i < kBatch && base + i < tok1; ++i) {
         const int32_t pos = A.positions ? A.positions[row0 + base + i] : prior + base + i;
@@ -304,20 +308,22 @@ void chunk_kernel(std::conditional_t<kRotary, ChunkRotaryArgs, ChunkArgs> A) {
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
       if (ok && t_tok >= base && t_tok < base + kBatch) {
-        const uint16_t* row = qrow;
+        // Nothing that depends on these is worked out before the batches and held over them.
         int rdim = A.rot.rdim;
-        asm volatile("" : "+v"(row), "+s"(rdim));  // nothing of these is held over the batches
+        asm volatile("" : "+s"(rdim));
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
-          const TurnedGranule v = turned_granule<true>(
-              row, 2 * c + hh, cs + (t_tok - base) * kRotaryPairs, rdim, A.rot.interleaved);
-          qop[c] = as_bf16x8(v.hi);
-          qlow[c] = as_bf16x8(v.lo);
-        }
+        for (int c = 0; c < 8; ++c)
+          asm volatile("" : "+v"(qin.own[c].x), "+v"(qin.own[c].y), "+v"(qin.own[c].z),
+                       "+v"(qin.own[c].w), "+v"(qin.partner[c].x), "+v"(qin.partner[c].y),
+                       "+v"(qin.partner[c].z), "+v"(qin.partner[c].w));
+        turn_granules<8, true>(qin, gq, cs + (t_tok - base) * kRotaryPairs, rdim,
+                               A.rot.interleaved, hi, lo);
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
     }
+#pragma unroll
+    for (int c = 0; c < 8; ++c) qop[c] = as_bf16x8(hi[c]), qlow[c] = as_bf16x8(lo[c]);
   }
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();

@@ -103,13 +103,25 @@ __device__ __forceinline__ f32x4 qk_page(const PageRegs& r, const bf16x8 (&qop)[
   return s;
 }
 
-// Queries as a sum of two bf16 parts.
+// Queries as a sum of two bf16 parts, in products of their own ...
 struct SplitQuery {
   bf16x8 hi[4], lo[4];
 };
 __device__ __forceinline__ f32x4 qk_page(const PageRegs& r, const SplitQuery& q) {
   const f32x4 s = qk_page(r, q.hi);
   return s + qk_page(r, q.lo);
+}
+// ... or, of at most 8 heads, in the two halves of one product's 16 columns: column c and
+// column c ^ 8 of a quad (8 lanes on, of 16) add up to one head's scores, in both.
+struct PairedQuery {
+  bf16x8 part[4];
+};
+__device__ __forceinline__ f32x4 qk_page(const PageRegs& r, const PairedQuery& q) {
+  f32x4 s = qk_page(r, q.part);
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    s[i] += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(s[i]), 0x128, 0xF, 0xF, true));
+  return s;
 }
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -165,8 +177,8 @@ __device__ __forceinline__ void process_page(const PageRegs& r, int valid, int q
 }
 
 struct DecodeArgs {
-  const uint16_t* k_cache;
-  const uint16_t* v_cache;
+  uint16_t* k_cache;
+  uint16_t* v_cache;
   const int32_t* units;
   const int32_t* bt;
   const uint16_t* q;
@@ -181,16 +193,52 @@ struct DecodeArgs {
   float sl2;  // scale * log2(e)
 };
 
-// Queries that are turned as they are loaded.
+// Queries that are turned as they are loaded, and (if k_new is set) the new token's key and
+// value, which the unit that ends with it writes to the cache.
 struct DecodeRotaryArgs : DecodeArgs {
   RotaryArgs<kRotaryPairs> rot;
   const int32_t* positions;  // null: the row's index in the cache
   int64_t q_row;
+  const uint16_t* k_new;
+  const uint16_t* v_new;
+  int64_t k_row, v_row;
 };
 
-template <bool kRotary>
+// Turned rows in LDS, 16 granules each.  kPaired: the heads' upper parts, and from kNewRow on
+// the new token's key and value; the heads' lower parts are further rows.
+struct TurnedRows {
+  float2 cs[kRotaryPairs];
+  uint4 hi[16][kDim / 8], lo[16][kDim / 8];
+};
+constexpr int kNewRow = 8;
+
+// Puts a new token into slot s of a loaded page.
+__device__ __forceinline__ void patch_page(PageRegs& r, const TurnedRows& n, int s, int lane) {
+  const int col = lane & 15, quad = lane >> 4;
+  if (col == s) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.k[i] = n.hi[kNewRow][4 * i + quad];
+  }
+  if (quad == s >> 2) {
+    const uint16_t* v = reinterpret_cast<const uint16_t*>(n.hi[kNewRow + 1]);
+    const uint32_t keep = s & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+    const int shift = 16 * (s & 1);
+#pragma unroll
+    for (int db = 0; db < 8; ++db) {
+      const uint32_t e = uint32_t(v[16 * db + col]) << shift;
+      if (s & 2) r.v[db].y = (r.v[db].y & keep) | e;
+      else r.v[db].x = (r.v[db].x & keep) | e;
+    }
+  }
+}
+
+// How queries enter the scores: as they are, or turned, as two parts.
+enum QueryForm : int { kPlain, kPaired, kSplit };
+
+template <int kForm>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(LIBRA_DECODE_WAVES_PER_EU, 8)))
-void decode_kernel(std::conditional_t<kRotary, DecodeRotaryArgs, DecodeArgs> A) {
+void decode_kernel(std::conditional_t<kForm == kPlain, DecodeArgs, DecodeRotaryArgs> A) {
+  constexpr bool kRotary = kForm != kPlain;
   __shared__ float red_m[kWaves][16];
   __shared__ float red_l[kWaves][16];
   __shared__ __align__(16) float red_o[kWaves][16][kRedStride];
@@ -205,22 +253,61 @@ void decode_kernel(std::conditional_t<kRotary, DecodeRotaryArgs, DecodeArgs> A) 
   const int G = A.group;
 
   // Q operand: lane (col, quad) holds head col's channels 8 * (4 i + quad) .. + 7 at step i.
-  std::conditional_t<kRotary, SplitQuery, bf16x8[4]> qop;
+  std::conditional_t<kForm == kPaired, PairedQuery,
+                     std::conditional_t<kForm == kSplit, SplitQuery, bf16x8[4]>> qop;
+  [[maybe_unused]] int new_slot = -1;  // this wave's last page holds the new token there
   if constexpr (kRotary) {
-    // A lane computes one pair's cosine and sine; the wave shares them through its part of
-    // red_o, which is written only after the next barrier.
-    float2* cs = reinterpret_cast<float2*>(&red_o[wave][0][0]);
-    const int32_t pos = A.positions ? A.positions[row] : u[U_PRIOR];
-    if (lane < A.rot.rdim / 2) cs[lane] = rotary_cos_sin(A.rot.turn[lane], pos, A.rot.amplitude);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    const uint16_t* qrow = A.q + size_t(row) * A.q_row + (size_t(g) * G + col) * kDim;
+    // The workgroup turns its heads together, a thread one granule of a head, through LDS that
+    // is not used until the waves' results are: little code, which matters as every launch
+    // fetches it anew (four granules a lane, each wave for itself: 20 us of a 100 us step).
+    // Where the unit ends with the new token, the same pass turns its key, stores key and value
+    // to the cache, and keeps them for the last wave, which alone reads that page for this head:
+    // the page as loaded may or may not have them, and to wait for the stores takes longer.
+    static_assert(sizeof(TurnedRows) <= sizeof(red_o), "turned rows lie in the waves' exchange");
+    TurnedRows& rows = *reinterpret_cast<TurnedRows*>(&red_o[0][0][0]);
+    const int prior = u[U_PRIOR], rdim = A.rot.rdim, inter = A.rot.interleaved;
+    const bool owner = kForm == kPaired && A.k_new && kv1 == prior + 1;
+    const int h = tid >> 4, gi[1] = {tid & 15};
+    const bool is_k = owner && h == kNewRow, is_v = owner && h == kNewRow + 1;
+    const uint16_t* src = is_k   ? A.k_new + size_t(row) * A.k_row + size_t(g) * kDim
+                          : is_v ? A.v_new + size_t(row) * A.v_row + size_t(g) * kDim
+                                 : A.q + size_t(row) * A.q_row + (size_t(g) * G + min(h, G - 1)) * kDim;
+    Granules<1> in;
+    load_granules(in, src, gi, rdim, inter);
+    if (tid < rdim / 2) {
+      const int32_t pos = A.positions ? A.positions[row] : prior;
+      rows.cs[tid] = rotary_cos_sin(A.rot.turn[tid], pos, A.rot.amplitude);
+    }
+    __syncthreads();
+    uint4 hi[1], lo[1];
+    turn_granules<1, true>(in, gi, rows.cs, is_v ? 0 : rdim, inter, hi, lo);
+    const bool unused = h >= G && !is_k && !is_v;
+    rows.hi[h][gi[0]] = unused ? make_uint4(0, 0, 0, 0) : hi[0];
+    rows.lo[h][gi[0]] = unused ? make_uint4(0, 0, 0, 0) : lo[0];
+    if (is_k || is_v) {
+      const size_t page = size_t(A.bt[int64_t(b) * A.bt_stride + prior / kPage]);
+      const size_t tile = (page * A.hkv + g) * kTileElems;
+      const int slot = prior % kPage;
+      if (is_k) {
+        *reinterpret_cast<uint4*>(A.k_cache + tile + (gi[0] * 16 + slot) * 8) = hi[0];
+      } else {
+        const uint32_t w[4] = {hi[0].x, hi[0].y, hi[0].z, hi[0].w};
+        uint16_t* const to = A.v_cache + tile + (128 * ((slot >> 2) & 1) + 8 * gi[0]) * 8 +
+                             (slot >> 3) * 4 + (slot & 3);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) to[8 * i] = uint16_t(w[i / 2] >> (16 * (i & 1)));
+      }
+    }
+    if (owner && wave == kWaves - 1) new_slot = prior % kPage;
+    __syncthreads();
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      TurnedGranule v{make_uint4(0, 0, 0, 0), make_uint4(0, 0, 0, 0)};
-      if (col < G) v = turned_granule<true>(qrow, 4 * i + quad, cs, A.rot.rdim, A.rot.interleaved);
-      qop.hi[i] = as_bf16x8(v.hi);
-      qop.lo[i] = as_bf16x8(v.lo);
+      if constexpr (kForm == kPaired) {
+        qop.part[i] = as_bf16x8((col < 8 ? rows.hi : rows.lo)[col & 7][4 * i + quad]);
+      } else {
+        qop.hi[i] = as_bf16x8(rows.hi[col][4 * i + quad]);
+        qop.lo[i] = as_bf16x8(rows.lo[col][4 * i + quad]);
+      }
     }
   } else {
     const uint4* qrow = reinterpret_cast<const uint4*>(
@@ -267,6 +354,10 @@ void decode_kernel(std::conditional_t<kRotary, DecodeRotaryArgs, DecodeArgs> A) 
     auto consume = [&](PageRegs& r, int k) {
       const int valid = min(kPage, kv1 - (w0 + k) * kPage);
       if (valid < kPage) clear_v_slots(r, quad, valid);
+      if constexpr (kForm == kPaired) {
+        if (new_slot >= 0 && k == nw - 1)
+          patch_page(r, *reinterpret_cast<const TurnedRows*>(&red_o[0][0][0]), new_slot, lane);
+      }
       process_page(r, valid, quad, qop, A.sl2, sm, acc);
     };
 
@@ -384,8 +475,8 @@ DecodeArgs decode_args(const KvLayout& L, const Plan& P, void* ws, const void* q
                        const int32_t* bt, int32_t stride, float scale, void* out, float* lse) {
   char* w = static_cast<char*>(ws);
   DecodeArgs A;
-  A.k_cache = static_cast<const uint16_t*>(L.desc.k_cache);
-  A.v_cache = static_cast<const uint16_t*>(L.desc.v_cache);
+  A.k_cache = static_cast<uint16_t*>(L.desc.k_cache);
+  A.v_cache = static_cast<uint16_t*>(L.desc.v_cache);
   A.units = reinterpret_cast<const int32_t*>(w + P.off_units);
   A.bt = bt;
   A.q = static_cast<const uint16_t*>(q);
@@ -409,13 +500,13 @@ hipError_t launch_decode(const KvLayout& L, const Plan& P, void* ws, const void*
   const int n = P.info.n_single;
   if (n == 0) return hipSuccess;
   const DecodeArgs A = decode_args(L, P, ws, q, bt, stride, scale, out, lse);
-  hipLaunchKernelGGL(decode_kernel<false>, dim3(unsigned(n)), dim3(kThreads), 0, s, A);
+  hipLaunchKernelGGL(decode_kernel<kPlain>, dim3(unsigned(n)), dim3(kThreads), 0, s, A);
   return hipGetLastError();
 }
 
 hipError_t launch_decode_rotary(const KvLayout& L, const Plan& P, void* ws, const NewRows& n,
                                 const int32_t* bt, int32_t stride, float scale, void* out,
-                                float* lse, hipStream_t s) {
+                                float* lse, bool write, hipStream_t s) {
   const int units = P.info.n_single;
   if (units == 0) return hipSuccess;
   DecodeRotaryArgs A;
@@ -423,7 +514,12 @@ hipError_t launch_decode_rotary(const KvLayout& L, const Plan& P, void* ws, cons
   A.rot = rotary_args<kRotaryPairs>(*n.rotary);
   A.positions = n.positions;
   A.q_row = n.q_row;
-  hipLaunchKernelGGL(decode_kernel<true>, dim3(unsigned(units)), dim3(kThreads), 0, s, A);
+  A.k_new = write ? static_cast<const uint16_t*>(n.k) : nullptr;
+  A.v_new = static_cast<const uint16_t*>(n.v);
+  A.k_row = n.k_row;
+  A.v_row = n.v_row;
+  auto k = P.group <= 8 ? decode_kernel<kPaired> : decode_kernel<kSplit>;
+  hipLaunchKernelGGL(k, dim3(unsigned(units)), dim3(kThreads), 0, s, A);
   return hipGetLastError();
 }
 

@@ -253,19 +253,25 @@ libra_status libra_append_attn_rotary(libra_kv_layout layout, libra_plan plan,
   const Plan& P = *form;
   const KvLayout& L = *layout;
   const NewRows n{rotary, positions, q, k_new, v_new, q_row_stride, k_row_stride, v_row_stride};
-  hipError_t e;
-  {
-    ProfScope ps(LIBRA_KERNEL_CACHE_WRITE, s, P.info.n_write_tiles > 0);
-    e = launch_cache_write_rotary(L, P, workspace, n, block_table, bt_stride, s);
+  // Decode units of up to 8 heads write their rows' tokens themselves, and without chunk rows
+  // there are no others.
+  const bool fused = P.info.n_chunk == 0 && P.group <= 8;
+  if (!fused) {
+    hipError_t e;
+    {
+      ProfScope ps(LIBRA_KERNEL_CACHE_WRITE, s, P.info.n_write_tiles > 0);
+      e = launch_cache_write_rotary(L, P, workspace, n, block_table, bt_stride, s);
+    }
+    if (e != hipSuccess) return hip_error(e, "cache-write launch");
   }
-  if (e != hipSuccess) return hip_error(e, "cache-write launch");
   return run_attention(
       P, workspace, out, lse, s, /*timed=*/true,
       [&](hipStream_t at) {
         return launch_chunk_rotary(L, P, workspace, n, block_table, bt_stride, scale, out, lse, at);
       },
       [&](hipStream_t at) {
-        return launch_decode_rotary(L, P, workspace, n, block_table, bt_stride, scale, out, lse, at);
+        return launch_decode_rotary(L, P, workspace, n, block_table, bt_stride, scale, out, lse, fused,
+                                    at);
       });
 }
 

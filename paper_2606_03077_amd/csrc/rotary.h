@@ -92,77 +92,115 @@ __device__ __forceinline__ uint32_t rotary_pack_bf16(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2{lo, hi}, b2));
 }
 
-// Eight turned channels: as bf16 (nearest), and what that leaves of the float32 values, as
-// bf16 again (both together hold 16 bits).  Nothing is left of copied channels, of values
-// that are not finite, or of those beyond bf16's range.
-struct TurnedGranule {
-  uint4 hi, lo;
+// Granules (8 channels) of a bf16 row of 128 channels and their channels' partners in the
+// pairs, loaded together so that their latencies overlap.
+template <int N>
+struct Granules {
+  uint4 own[N], partner[N];
 };
 
-template <bool kLow>
-__device__ __forceinline__ void split_pair(float y0, float y1, bool turned0, bool turned1,
-                                           uint32_t raw, uint32_t& hi, uint32_t& lo) {
-  const uint32_t h = rotary_pack_bf16(y0, y1);
-  const uint32_t keep = (turned0 ? 0u : 0x0000FFFFu) | (turned1 ? 0u : 0xFFFF0000u);
-  hi = (raw & keep) | (h & ~keep);
-  if constexpr (kLow) {
-    const float h0 = bf16_to_f32(h & 0xFFFF), h1 = bf16_to_f32(h >> 16);
-    const float l0 = turned0 && __builtin_isfinite(h0) ? y0 - h0 : 0.f;
-    const float l1 = turned1 && __builtin_isfinite(h1) ? y1 - h1 : 0.f;
-    lo = rotary_pack_bf16(l0, l1);
+// Whether a granule's partners are a granule too (or the granule itself).
+__device__ __forceinline__ bool granules_pair(int rdim, int interleaved) {
+  return (rdim & (interleaved ? 7 : 15)) == 0;
+}
+
+template <int N>
+__device__ __forceinline__ void load_granules(Granules<N>& in, const uint16_t* row,
+                                              const int (&gi)[N], int rdim, int interleaved) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) in.own[i] = *reinterpret_cast<const uint4*>(row + 8 * gi[i]);
+  const int h = rdim / 2;
+  if (interleaved) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const uint4 w = in.own[i];
+      in.partner[i] = make_uint4(w.x >> 16 | w.x << 16, w.y >> 16 | w.y << 16,
+                                 w.z >> 16 | w.z << 16, w.w >> 16 | w.w << 16);
+    }
+  } else if (granules_pair(rdim, interleaved)) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int d = 8 * gi[i];
+      in.partner[i] =
+          *reinterpret_cast<const uint4*>(row + (d < h ? d + h : d < rdim ? d - h : d));
+    }
   } else {
-    lo = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      auto at = [&](int e) -> uint32_t {
+        const int d = 8 * gi[i] + e;
+        return row[d < h ? d + h : d < rdim ? d - h : d];
+      };
+      in.partner[i] = make_uint4(at(0) | at(1) << 16, at(2) | at(3) << 16, at(4) | at(5) << 16,
+                                 at(6) | at(7) << 16);
+    }
   }
 }
 
-// Granule gi (channels 8 gi .. + 7) of a bf16 row of 128 channels, turned (lo only if kLow).
-// cs: the row's (cos, sin) by pair.  Reads the partner channels from the row too.
-template <bool kLow>
-__device__ __forceinline__ TurnedGranule turned_granule(const uint16_t* row, int gi,
-                                                        const float2* cs, int rdim,
-                                                        int interleaved) {
-  const int d0 = 8 * gi;
-  const uint4 raw = *reinterpret_cast<const uint4*>(row + d0);
-  if (d0 >= rdim) return {raw, make_uint4(0, 0, 0, 0)};
-  const uint32_t rw[4] = {raw.x, raw.y, raw.z, raw.w};
-  uint32_t hi[4], lo[4];
-  if (interleaved) {
+// Turns the granules: hi is bf16 (nearest), lo (if kLow) what that leaves of the float32
+// values, as bf16 again, so that both together hold 16 bits.  Nothing is left of copied
+// channels and of values that bf16 makes infinite or NaN.  cs: the row's (cos, sin) by pair.
+template <int N, bool kLow, bool kPaired>
+__device__ __forceinline__ void turn_granules_as(const Granules<N>& in, const int (&gi)[N],
+                                                 const float2* cs, int rdim, int interleaved,
+                                                 uint4 (&hi)[N], uint4 (&lo)[N]) {
+  const int h = rdim / 2;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float2 t = cs[4 * gi + i];  // past the last pair: not used
-      const float x1 = bf16_to_f32(rw[i] & 0xFFFF), x2 = bf16_to_f32(rw[i] >> 16);
-      const bool turned = d0 + 2 * i < rdim;
-      split_pair<kLow>(turn_first(x1, x2, t), turn_second(x1, x2, t), turned, turned, rw[i], hi[i],
-                       lo[i]);
-    }
-  } else {
-    const int h = rdim / 2;
-    uint32_t pw[4];  // the partners, two in a word
-    if ((h & 7) == 0) {
-      const uint4 p = *reinterpret_cast<const uint4*>(row + (d0 < h ? d0 + h : d0 - h));
-      pw[0] = p.x, pw[1] = p.y, pw[2] = p.z, pw[3] = p.w;
-    } else {
-      auto partner = [&](int d) -> uint32_t { return row[d < h ? d + h : d < rdim ? d - h : d]; };
+  for (int i = 0; i < N; ++i) {
+    const int d0 = 8 * gi[i];
+    const uint32_t own[4] = {in.own[i].x, in.own[i].y, in.own[i].z, in.own[i].w};
+    const uint32_t oth[4] = {in.partner[i].x, in.partner[i].y, in.partner[i].z, in.partner[i].w};
+    uint32_t ho[4], lw[4];
+    // Past the last pair: any entry, its result is not used.
+    const int base = d0 >= rdim ? 0 : interleaved ? d0 / 2 : d0 < h ? d0 : d0 - h;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) pw[i] = partner(d0 + 2 * i) | partner(d0 + 2 * i + 1) << 16;
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      float y[2];
+    for (int w = 0; w < 4; ++w) {
+      float y[2], left[2];
+      bool turned[2];
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
-        const int d = d0 + 2 * i + e;
-        const bool first = d < h;
-        const float2 t = cs[first ? d : d < rdim ? d - h : 0];
-        const float x = bf16_to_f32((rw[i] >> (16 * e)) & 0xFFFF);
-        const float o = bf16_to_f32((pw[i] >> (16 * e)) & 0xFFFF);
-        y[e] = first ? turn_first(x, o, t) : turn_second(o, x, t);
+        const int d = d0 + 2 * w + e;
+        turned[e] = d < rdim;
+        float2 t;
+        bool first;
+        if constexpr (kPaired) {
+          t = cs[base + ((2 * w + e) >> interleaved)];
+          first = interleaved ? e == 0 : d0 < h;
+        } else {
+          t = cs[!turned[e] ? 0 : interleaved ? d / 2 : d < h ? d : d - h];
+          first = interleaved ? e == 0 : d < h;
+        }
+        const float x = bf16_to_f32((own[w] >> (16 * e)) & 0xFFFF);
+        const float o = bf16_to_f32((oth[w] >> (16 * e)) & 0xFFFF);
+        y[e] = __builtin_fmaf(x, t.x, o * (first ? -t.y : t.y));  // as turn_first / turn_second
       }
-      const int d = d0 + 2 * i;
-      split_pair<kLow>(y[0], y[1], d < rdim, d + 1 < rdim, rw[i], hi[i], lo[i]);
+      const uint32_t b = rotary_pack_bf16(y[0], y[1]);
+      const uint32_t keep = (turned[0] ? 0u : 0x0000FFFFu) | (turned[1] ? 0u : 0xFFFF0000u);
+      ho[w] = (own[w] & keep) | (b & ~keep);
+      if constexpr (kLow) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float r = bf16_to_f32((b >> (16 * e)) & 0xFFFF);
+          left[e] = turned[e] && __builtin_isfinite(r) ? y[e] - r : 0.f;
+        }
+        lw[w] = rotary_pack_bf16(left[0], left[1]);
+      }
     }
+    hi[i] = make_uint4(ho[0], ho[1], ho[2], ho[3]);
+    if constexpr (kLow) lo[i] = make_uint4(lw[0], lw[1], lw[2], lw[3]);
+    if constexpr (N > 4) __builtin_amdgcn_sched_barrier(0);  // one granule's registers at a time
   }
-  return {make_uint4(hi[0], hi[1], hi[2], hi[3]), make_uint4(lo[0], lo[1], lo[2], lo[3])};
+}
+
+template <int N, bool kLow>
+__device__ __forceinline__ void turn_granules(const Granules<N>& in, const int (&gi)[N],
+                                              const float2* cs, int rdim, int interleaved,
+                                              uint4 (&hi)[N], uint4 (&lo)[N]) {
+  // rdim may differ between lanes where it is 0 (copies) or the row's.
+  if (granules_pair(rdim, interleaved))
+    turn_granules_as<N, kLow, true>(in, gi, cs, rdim, interleaved, hi, lo);
+  else
+    turn_granules_as<N, kLow, false>(in, gi, cs, rdim, interleaved, hi, lo);
 }
 
 #endif  // __HIPCC__

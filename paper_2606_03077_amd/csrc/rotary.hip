@@ -344,9 +344,12 @@ __device__ __forceinline__ void store_key(const WriteArgs& A, const Rot& rot, co
         cs[4 * j + i] = rotary_cos_sin(rot.turn[4 * j + i], p.pos, rot.amplitude);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
-    const uint16_t* k = A.k_new + row * A.k_row + g * kDim;
-    *reinterpret_cast<uint4*>(tile + k_off(s, 8 * j)) =
-        turned_granule<false>(k, j, cs, rot.rdim, rot.interleaved).hi;
+    const int gi[1] = {j};
+    Granules<1> in;
+    uint4 k[1], none[1];
+    load_granules(in, A.k_new + row * A.k_row + g * kDim, gi, rot.rdim, rot.interleaved);
+    turn_granules<1, false>(in, gi, cs, rot.rdim, rot.interleaved, k, none);
+    *reinterpret_cast<uint4*>(tile + k_off(s, 8 * j)) = k[0];
   } else {
     constexpr bool kInter = kForm == kInterQuads;
     const int2 qd = quads_of<kInter>(j, rot.rdim / 8);

@@ -35,10 +35,11 @@ hipError_t launch_kv_append(const KvLayout& L, const NewRows& n, const int64_t* 
 hipError_t launch_cache_write_rotary(const KvLayout& L, const Plan& P, const void* ws,
                                      const NewRows& n, const int32_t* bt, int32_t stride,
                                      hipStream_t s);
-// Attention whose queries are turned as they are loaded.
+// Attention whose queries are turned as they are loaded.  write: the decode units also write
+// the new tokens to the cache (plans of single rows only: chunk tiles read what others write).
 hipError_t launch_decode_rotary(const KvLayout& L, const Plan& P, void* ws, const NewRows& n,
                                 const int32_t* bt, int32_t stride, float scale, void* out,
-                                float* lse, hipStream_t s);
+                                float* lse, bool write, hipStream_t s);
 hipError_t launch_chunk_rotary(const KvLayout& L, const Plan& P, void* ws, const NewRows& n,
                                const int32_t* bt, int32_t stride, float scale, void* out,
                                float* lse, hipStream_t s);

@@ -27,7 +27,7 @@ hipError_t launch_kv_append(const KvLayout&, const NewRows&, const int64_t*, int
 hipError_t launch_cache_write_rotary(const KvLayout&, const Plan&, const void*, const NewRows&,
                                      const int32_t*, int32_t, hipStream_t) { return ++g_write, hipSuccess; }
 hipError_t launch_decode_rotary(const KvLayout&, const Plan&, void*, const NewRows&, const int32_t*,
-                                int32_t, float, void*, float*, hipStream_t) { return ++g_decode, hipSuccess; }
+                                int32_t, float, void*, float*, bool, hipStream_t) { return ++g_decode, hipSuccess; }
 hipError_t launch_chunk_rotary(const KvLayout&, const Plan&, void*, const NewRows&, const int32_t*,
                                int32_t, float, void*, float*, hipStream_t) { return ++g_chunk, hipSuccess; }
 }  // namespace libra
