@@ -114,6 +114,130 @@ struct ChunkRotaryArgs : ChunkArgs {
   int64_t q_row;
 };
 
+// Cosines and sines of a few tokens' pairs, in LDS: pairs 2 u and 2 u + 1 of token t lie
+// together at 16-byte unit u ^ t of its 512 bytes, so that the lanes of eight tokens, which
+// read the same pairs, read from different banks.
+constexpr int kTurnTokens = 8;
+struct TurnCosSin {
+  float2 cs[kTurnTokens][kRotaryPairs];
+  __device__ __forceinline__ void put(int t, int pair, float2 v) { cs[t][pair ^ 2 * t] = v; }
+  __device__ __forceinline__ float4 two(int t, int pair) const {  // pair even
+    return *reinterpret_cast<const float4*>(&cs[t][pair ^ 2 * t]);
+  }
+  __device__ __forceinline__ float2 one(int t, int pair) const { return cs[t][pair ^ 2 * t]; }
+};
+
+// Two turned values as bf16 and what that leaves of them (both parts hold 16 bits).
+__device__ __forceinline__ uint2 split_pair(float y0, float y1) {
+  const uint32_t h = pack_bf16x2(y0, y1);
+  return make_uint2(h, pack_bf16x2(y0 - __uint_as_float(h << 16), y1 - __uint_as_float(h & 0xFFFF0000u)));
+}
+
+// A value that bf16 makes infinite leaves a NaN; then nothing is left of the lane's channels.
+__device__ __forceinline__ void finite_low(float largest, bf16x8 (&low)[8]) {
+  if (largest < 3.3895e38f) return;  // the largest bf16
+#pragma unroll
+  for (int c = 0; c < 8; ++c) low[c] = as_bf16x8(make_uint4(0, 0, 0, 0));
+}
+
+// A lane's query, granules 2 c + hh of its row (c = 0 .. 7), turned by token t's pairs.  Half
+// pairing with R = 32 S: granules c and c + S (c < S) are eight pairs.
+template <int S>
+__device__ __forceinline__ void turn_half(const uint4 (&raw)[8], const TurnCosSin& cs, int t, int hh,
+                                          bf16x8 (&op)[8], bf16x8 (&low)[8]) {
+  float largest = 0.f;
+#pragma unroll
+  for (int c = 0; c < S; ++c) {
+    const uint32_t a[4] = {raw[c].x, raw[c].y, raw[c].z, raw[c].w};
+    const uint32_t b[4] = {raw[c + S].x, raw[c + S].y, raw[c + S].z, raw[c + S].w};
+    uint2 p[4], q[4];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      const float4 k = cs.two(t, 16 * c + 8 * hh + 2 * w);
+      const float x0 = bf16_to_f32(a[w] & 0xFFFF), x1 = __uint_as_float(a[w] & 0xFFFF0000u);
+      const float z0 = bf16_to_f32(b[w] & 0xFFFF), z1 = __uint_as_float(b[w] & 0xFFFF0000u);
+      const float f0 = turn_first(x0, z0, make_float2(k.x, k.y)), f1 = turn_first(x1, z1, make_float2(k.z, k.w));
+      const float s0 = turn_second(x0, z0, make_float2(k.x, k.y)), s1 = turn_second(x1, z1, make_float2(k.z, k.w));
+      largest = fmaxf(fmaxf(largest, fmaxf(fabsf(f0), fabsf(f1))), fmaxf(fabsf(s0), fabsf(s1)));
+      p[w] = split_pair(f0, f1);
+      q[w] = split_pair(s0, s1);
+    }
+    op[c] = as_bf16x8(make_uint4(p[0].x, p[1].x, p[2].x, p[3].x));
+    low[c] = as_bf16x8(make_uint4(p[0].y, p[1].y, p[2].y, p[3].y));
+    op[c + S] = as_bf16x8(make_uint4(q[0].x, q[1].x, q[2].x, q[3].x));
+    low[c + S] = as_bf16x8(make_uint4(q[0].y, q[1].y, q[2].y, q[3].y));
+  }
+#pragma unroll
+  for (int c = 2 * S; c < 8; ++c) op[c] = as_bf16x8(raw[c]), low[c] = as_bf16x8(make_uint4(0, 0, 0, 0));
+  finite_low(largest, low);
+}
+
+// Interleaved pairing, R a multiple of 16: a granule is four pairs.
+__device__ __forceinline__ void turn_interleaved(const uint4 (&raw)[8], const TurnCosSin& cs, int t,
+                                                 int hh, int rdim, bf16x8 (&op)[8], bf16x8 (&low)[8]) {
+  float largest = 0.f;
+#pragma unroll
+  for (int c = 0; c < 8; ++c) {
+    if (16 * c >= rdim) {
+      op[c] = as_bf16x8(raw[c]), low[c] = as_bf16x8(make_uint4(0, 0, 0, 0));
+      continue;
+    }
+    const uint32_t a[4] = {raw[c].x, raw[c].y, raw[c].z, raw[c].w};
+    uint2 p[4];
+#pragma unroll
+    for (int w = 0; w < 4; w += 2) {
+      const float4 k = cs.two(t, 8 * c + 4 * hh + w);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const float2 one = e ? make_float2(k.z, k.w) : make_float2(k.x, k.y);
+        const float x0 = bf16_to_f32(a[w + e] & 0xFFFF), x1 = __uint_as_float(a[w + e] & 0xFFFF0000u);
+        const float f = turn_first(x0, x1, one), s = turn_second(x0, x1, one);
+        largest = fmaxf(largest, fmaxf(fabsf(f), fabsf(s)));
+        p[w + e] = split_pair(f, s);
+      }
+    }
+    op[c] = as_bf16x8(make_uint4(p[0].x, p[1].x, p[2].x, p[3].x));
+    low[c] = as_bf16x8(make_uint4(p[0].y, p[1].y, p[2].y, p[3].y));
+  }
+  finite_low(largest, low);
+}
+
+// Any other R: channel by channel, in a loop.
+__device__ __forceinline__ void turn_any(const uint16_t* row, const TurnCosSin& cs, int t, int hh,
+                                         const RotaryArgs<kRotaryPairs>& rot, bf16x8 (&op)[8],
+                                         bf16x8 (&low)[8]) {
+  typedef uint32_t u32x32 __attribute__((ext_vector_type(32)));
+  u32x32 hi = 0, lo = 0;
+  const int h = rot.rdim / 2;
+  float largest = 0.f;
+#pragma unroll 1
+  for (int i = 0; i < 32; ++i) {
+    const int d0 = 16 * (i / 4) + 8 * hh + 2 * (i % 4);
+    const uint32_t raw = *reinterpret_cast<const uint32_t*>(row + d0);
+    float y[2];
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      const int d = d0 + e;
+      const bool first = rot.interleaved ? e == 0 : d < h, turned = d < rot.rdim;
+      const int other = !turned ? d : rot.interleaved ? d ^ 1 : first ? d + h : d - h;
+      const float2 k = cs.one(t, !turned ? 0 : rot.interleaved ? d / 2 : first ? d : d - h);
+      const float x = bf16_to_f32((raw >> (16 * e)) & 0xFFFF), o = bf16_to_f32(row[other]);
+      y[e] = first ? turn_first(x, o, k) : turn_second(o, x, k);
+      if (turned) largest = fmaxf(largest, fabsf(y[e]));
+    }
+    const uint2 p = split_pair(y[0], y[1]);
+    const uint32_t keep = (d0 < rot.rdim ? 0u : 0x0000FFFFu) | (d0 + 1 < rot.rdim ? 0u : 0xFFFF0000u);
+    hi[i] = (raw & keep) | (p.x & ~keep);
+    lo[i] = p.y & ~keep;
+  }
+#pragma unroll
+  for (int c = 0; c < 8; ++c) {
+    op[c] = as_bf16x8(make_uint4(hi[4 * c], hi[4 * c + 1], hi[4 * c + 2], hi[4 * c + 3]));
+    low[c] = as_bf16x8(make_uint4(lo[4 * c], lo[4 * c + 1], lo[4 * c + 2], lo[4 * c + 3]));
+  }
+  finite_low(largest, low);
+}
+
 template <int kWaves, bool kRotary>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void chunk_kernel(std::conditional_t<kRotary, ChunkRotaryArgs, ChunkArgs> A) {
@@ -208,11 +332,15 @@ void chunk_kernel(std::conditional_t<kRotary, ChunkRotaryArgs, ChunkArgs> A) {
   // 16 c + 8 hh .. + 7 of its row.
   bf16x8 qop[8];
   [[maybe_unused]] bf16x8 qlow[8];  // what bf16 leaves of turned queries
-  [[maybe_unused]] Granules<8> qin;
-  [[maybe_unused]] const int gq[8] = {hh, 2 + hh, 4 + hh, 6 + hh, 8 + hh, 10 + hh, 12 + hh, 14 + hh};
+  [[maybe_unused]] uint4 qraw[8];
+  [[maybe_unused]] const uint16_t* qrow = nullptr;
   if constexpr (kRotary) {
-    load_granules(qin, A.q + size_t(row0 + (ok ? t_tok : 0)) * A.q_row + (size_t(g) * G + head) * kDim,
-                  gq, A.rot.rdim, A.rot.interleaved);
+    qrow = A.q + size_t(row0 + (ok ? t_tok : 0)) * A.q_row + (size_t(g) * G + head) * kDim;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) {
+      qraw[c] = *reinterpret_cast<const uint4*>(qrow + 8 * (2 * c + hh));
+      qop[c] = qlow[c] = as_bf16x8(make_uint4(0, 0, 0, 0));
+    }
   } else {
     const uint4* qrow = reinterpret_cast<const uint4*>(
         A.q + (size_t(row0 + (ok ? t_tok : 0)) * A.hq + size_t(g) * G + head) * kDim);
@@ -291,39 +419,34 @@ void chunk_kernel(std::conditional_t<kRotary, ChunkRotaryArgs, ChunkArgs> A) {
   // shares them through its 4 KiB of the last K and V stage, which step 0 fills first, behind
   // the barrier below.
   if constexpr (kRotary) {
-    constexpr int kBatch = 8;
-    float2* const cs = reinterpret_cast<float2*>(
+    TurnCosSin* const cs = reinterpret_cast<TurnCosSin*>(
         (wave < kWaves / 2 ? &ldk3[0][0] : &ldv3[0][0]) + (wave % (kWaves / 2)) * 256);
     const int tok0 = q0 + (r_first + 32 * wave) / G;
     const int tok1 = min(q0 + (r_first + 32 * wave + 31) / G + 1, q1);  // the wave's tokens
-    uint4 hi[8], lo[8];
-#pragma unroll
-    for (int c = 0; c < 8; ++c) hi[c] = lo[c] = make_uint4(0, 0, 0, 0);
-    for (int base = tok0; base < tok1; base += kBatch) {
-      for (int i = 0; i < kBatch && base + i < tok1; ++i) {
+    const int rdim = A.rot.rdim;
+    for (int base = tok0; base < tok1; base += kTurnTokens) {
+      for (int i = 0; i < kTurnTokens && base + i < tok1; ++i) {
         const int32_t pos = A.positions ? A.positions[row0 + base + i] : prior + base + i;
-        if (lane < A.rot.rdim / 2)
-          cs[i * kRotaryPairs + lane] = rotary_cos_sin(A.rot.turn[lane], pos, A.rot.amplitude);
+        if (lane < rdim / 2) cs->put(i, lane, rotary_cos_sin(A.rot.turn[lane], pos, A.rot.amplitude));
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
-      if (ok && t_tok >= base && t_tok < base + kBatch) {
-        // Nothing that depends on these is worked out before the batches and held over them.
-        int rdim = A.rot.rdim;
-        asm volatile("" : "+s"(rdim));
+      if (ok && t_tok >= base && t_tok < base + kTurnTokens) {
+        const int t = t_tok - base;
+        // What depends on the queries is not worked out before the batches and held over them.
 #pragma unroll
         for (int c = 0; c < 8; ++c)
-          asm volatile("" : "+v"(qin.own[c].x), "+v"(qin.own[c].y), "+v"(qin.own[c].z),
-                       "+v"(qin.own[c].w), "+v"(qin.partner[c].x), "+v"(qin.partner[c].y),
-                       "+v"(qin.partner[c].z), "+v"(qin.partner[c].w));
-        turn_granules<8, true>(qin, gq, cs + (t_tok - base) * kRotaryPairs, rdim,
-                               A.rot.interleaved, hi, lo);
+          asm volatile("" : "+v"(qraw[c].x), "+v"(qraw[c].y), "+v"(qraw[c].z), "+v"(qraw[c].w));
+        if (A.rot.interleaved && rdim % 16 == 0) turn_interleaved(qraw, *cs, t, hh, rdim, qop, qlow);
+        else if (A.rot.interleaved || rdim % 32) turn_any(qrow, *cs, t, hh, A.rot, qop, qlow);
+        else if (rdim == 128) turn_half<4>(qraw, *cs, t, hh, qop, qlow);
+        else if (rdim == 96) turn_half<3>(qraw, *cs, t, hh, qop, qlow);
+        else if (rdim == 64) turn_half<2>(qraw, *cs, t, hh, qop, qlow);
+        else turn_half<1>(qraw, *cs, t, hh, qop, qlow);
       }
       __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
       __builtin_amdgcn_wave_barrier();
     }
-#pragma unroll
-    for (int c = 0; c < 8; ++c) qop[c] = as_bf16x8(hi[c]), qlow[c] = as_bf16x8(lo[c]);
   }
   __builtin_amdgcn_s_waitcnt(0);
   __syncthreads();

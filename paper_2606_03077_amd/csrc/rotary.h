@@ -188,7 +188,6 @@ __device__ __forceinline__ void turn_granules_as(const Granules<N>& in, const in
     }
     hi[i] = make_uint4(ho[0], ho[1], ho[2], ho[3]);
     if constexpr (kLow) lo[i] = make_uint4(lw[0], lw[1], lw[2], lw[3]);
-    if constexpr (N > 4) __builtin_amdgcn_sched_barrier(0);  // one granule's registers at a time
   }
 }
 
