@@ -1,5 +1,6 @@
 // Rotary positions of dense rows, and the cache append that turns keys on the way.
 #include <algorithm>
+#include <type_traits>
 
 #include "rotary_calls.h"
 
@@ -108,10 +109,32 @@ __device__ __forceinline__ int2 quads_of(int j, int R8) {
   return kInter || j >= R8 ? make_int2(2 * j, 2 * j + 1) : make_int2(j, j + R8);
 }
 
+template <bool kPastCaches, class Quad>
+__device__ __forceinline__ Quad load_quad(const Quad* p) {
+  typedef uint32_t V __attribute__((ext_vector_type(sizeof(Quad) / 4)));
+  if constexpr (kPastCaches)
+    return __builtin_bit_cast(Quad, __builtin_nontemporal_load(reinterpret_cast<const V*>(p)));
+  else
+    return *p;
+}
+template <bool kPastCaches, class Quad>
+__device__ __forceinline__ void store_quad(Quad* p, Quad v) {
+  typedef uint32_t V __attribute__((ext_vector_type(sizeof(Quad) / 4)));
+  if constexpr (kPastCaches)
+    __builtin_nontemporal_store(__builtin_bit_cast(V, v), reinterpret_cast<V*>(p));
+  else
+    *p = v;
+}
+
+constexpr int64_t kStreamBytes = int64_t(128) << 20;  // written by a call whose writes go past
+
+// What goes past the caches: nothing, the reads (each value is read once), or both.
+enum Streaming : int { kCached, kReads, kReadsWrites };
+
 // Wide form: R and the head size are multiples of 8, rows are aligned for four channels at a
 // time.  A thread owns two quads of a head (4 pairs, or 8 copied channels), computes their
 // cosines and sines once, and turns them in up to kHeads heads.
-template <class T, bool kInter, int kHeads, class Rot>
+template <class T, bool kInter, int kHeads, Streaming kStream, class Rot>
 __device__ __forceinline__ void turn_rows_wide(const Rot& rot, const RowsArgs<T>& A, int64_t bx,
                                                int by) {
   using Quad = typename T::Quad;
@@ -132,8 +155,8 @@ __device__ __forceinline__ void turn_rows_wide(const Rot& rot, const RowsArgs<T>
   for (int i = 0; i < kHeads; ++i) {
     const int h = head0 + i * A.head_slots;
     if (h < A.heads) {
-      a[i] = *reinterpret_cast<const Quad*>(x + h * A.x_head + 4 * qd.x);
-      b[i] = *reinterpret_cast<const Quad*>(x + h * A.x_head + 4 * qd.y);
+      a[i] = load_quad<kStream != kCached>(reinterpret_cast<const Quad*>(x + h * A.x_head + 4 * qd.x));
+      b[i] = load_quad<kStream != kCached>(reinterpret_cast<const Quad*>(x + h * A.x_head + 4 * qd.y));
     }
   }
   float2 cs[4];
@@ -150,8 +173,8 @@ __device__ __forceinline__ void turn_rows_wide(const Rot& rot, const RowsArgs<T>
     const int h = head0 + i * A.head_slots;
     if (h < A.heads) {
       if (turned) turn_quads<T, kInter>(a[i], b[i], cs);
-      *reinterpret_cast<Quad*>(out + h * A.out_head + 4 * qd.x) = a[i];
-      *reinterpret_cast<Quad*>(out + h * A.out_head + 4 * qd.y) = b[i];
+      store_quad<kStream == kReadsWrites>(reinterpret_cast<Quad*>(out + h * A.out_head + 4 * qd.x), a[i]);
+      store_quad<kStream == kReadsWrites>(reinterpret_cast<Quad*>(out + h * A.out_head + 4 * qd.y), b[i]);
     }
   }
 }
@@ -187,10 +210,10 @@ __device__ __forceinline__ void turn_rows_narrow(const Rot& rot, const RowsArgs<
   }
 }
 
-template <class T, bool kInter, int kHeads>
+template <class T, bool kInter, int kHeads, Streaming kStream>
 __global__ __launch_bounds__(kThreads) void rotary_wide_kernel(RotaryArgs<kMaxPairs> rot,
                                                                RowsArgs<T> A) {
-  turn_rows_wide<T, kInter, kHeads>(rot, A, blockIdx.x, blockIdx.y);
+  turn_rows_wide<T, kInter, kHeads, kStream>(rot, A, blockIdx.x, blockIdx.y);
 }
 template <class T>
 __global__ __launch_bounds__(kThreads) void rotary_narrow_kernel(RotaryArgs<kMaxPairs> rot,
@@ -204,7 +227,7 @@ constexpr int64_t kMaxBlocks = int64_t(1) << 22;  // per launch: 2^30 threads
 template <class T>
 struct RowsPlan {
   RowsArgs<T> args;
-  bool wide, many;
+  bool wide, many, stream;
   int threads;
   // Blocks along x for `rows` rows, and the rows that n of them take.
   int64_t blocks(int64_t rows) const {
@@ -232,16 +255,26 @@ RowsPlan<T> plan_rows(const Rotary& r, const RotaryRows& a) {
   p.wide = r.rotary_dim % 8 == 0 && r.head_dim % 8 == 0 &&
            (reinterpret_cast<uintptr_t>(a.x) | reinterpret_cast<uintptr_t>(a.out)) % quad == 0 &&
            ((a.x_row | a.x_head | a.out_row | a.out_head) & 3) == 0;
-  p.many = a.rows * a.heads * A.per_head >= int64_t(4) * 2048 * kThreads;
+  // Four heads to a thread share its cosines and sines, which pays once the chip is full and a
+  // row has heads enough: 40,960 rows of 40 heads (bf16) 168 us against 197 with one head each
+  // and 177 with two, of 28 heads 125 (143, 123); but 1,024 rows of 28 heads 9.0 us against 8.6,
+  // 16 rows 6.4 against 6.1, 40,960 rows of 8 heads 46 against 45 (cold caches, launch included).
+  p.many = a.heads >= 16 && a.rows * a.heads * A.per_head >= int64_t(2560) * kThreads;
+  // More than the last-level cache (256 MiB) would hold of both sides: the result goes past it
+  // too.  Turned and then copied, 16,384 rows of 40 heads (160 MiB a side) take 111 us so, 125
+  // through the caches, 40,960 rows 290 and 303; but 8,192 rows (80 MiB) 58 and 54.
+  p.stream = p.many && a.rows * a.heads * r.head_dim * int64_t(sizeof(typename T::Elem)) >= kStreamBytes;
   const int per_thread = p.many ? 4 : 1;
   p.threads = kThreads;
   A.y_blocks = (a.heads + kNarrowHeads - 1) / kNarrowHeads;
   p.half = r.rotary_dim / 2;
   if (p.wide) {
-    A.head_slots = std::min<int>((a.heads + per_thread - 1) / per_thread, kThreads / A.per_head);
+    // As few blocks to a row as its heads need, with even shares.
+    const int most = kThreads / A.per_head * per_thread;
+    A.y_blocks = (a.heads + most - 1) / most;
+    A.head_slots = (a.heads + A.y_blocks * per_thread - 1) / (A.y_blocks * per_thread);
     A.per_row = A.head_slots * A.per_head;
     A.block_rows = kThreads / A.per_row;
-    A.y_blocks = (a.heads + A.head_slots * per_thread - 1) / (A.head_slots * per_thread);
     p.threads = A.per_row * A.block_rows;
   }
   return p;
@@ -260,9 +293,15 @@ hipError_t apply(const Rotary& r, const RotaryRows& a, hipStream_t s) {
     A.positions += r0;
     const dim3 grid(unsigned(p.blocks(A.rows)), unsigned(A.y_blocks));
     const bool inter = r.pairing == LIBRA_ROTARY_INTERLEAVED;
+    auto wide_form = [&](auto pairing) {
+      constexpr bool kInter = decltype(pairing)::value;
+      return !p.many    ? rotary_wide_kernel<T, kInter, 1, kCached>
+             : p.stream ? rotary_wide_kernel<T, kInter, 4, kReadsWrites>
+                        : rotary_wide_kernel<T, kInter, 4, kReads>;
+    };
     auto k = !p.wide ? rotary_narrow_kernel<T>
-             : p.many ? (inter ? rotary_wide_kernel<T, true, 4> : rotary_wide_kernel<T, false, 4>)
-                      : (inter ? rotary_wide_kernel<T, true, 1> : rotary_wide_kernel<T, false, 1>);
+             : inter ? wide_form(std::true_type{})
+                     : wide_form(std::false_type{});
     hipLaunchKernelGGL(k, grid, dim3(unsigned(p.threads)), 0, s, rot, A);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
@@ -369,7 +408,7 @@ __device__ __forceinline__ void store_key(const WriteArgs& A, const Rot& rot, co
 // slots of one page form a run; the block writes the runs that begin among its rows, so a long
 // chunk's blocks write whole pages wherever its pages begin.  Whole pages go through LDS (V
 // tiles are transposed), single rows straight to their slots.  The other blocks turn queries.
-template <int kForm, int kHeads>
+template <int kForm, int kHeads, Streaming kStream>
 __global__ __launch_bounds__(kThreads) void kv_append_kernel(Rot rot, WriteArgs A,
                                                              RowsArgs<Bf16> Q) {
   __shared__ __align__(16) uint16_t vt[kTileElems];
@@ -380,7 +419,7 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(Rot rot, WriteArgs 
     if constexpr (kForm == kAnyPairs)
       turn_rows_narrow<Bf16>(rot, Q, bx, i - bx * Q.y_blocks);
     else
-      turn_rows_wide<Bf16, kForm == kInterQuads, kHeads>(rot, Q, bx, i - bx * Q.y_blocks);
+      turn_rows_wide<Bf16, kForm == kInterQuads, kHeads, kStream>(rot, Q, bx, i - bx * Q.y_blocks);
     return;
   }
   const int blk = int(blockIdx.x) / A.hkv, g = int(blockIdx.x) - blk * A.hkv;
@@ -488,9 +527,17 @@ hipError_t launch_kv_append(const KvLayout& L, const NewRows& n, const int64_t* 
   if (hq > 0)
     q = plan_rows<Bf16>(*n.rotary, {n.q, q_out, n.q_row, kDim, int64_t(hq) * kDim, kDim, n.positions,
                                     rows, hq, LIBRA_DTYPE_BF16, false});
-  auto k = form == kAnyPairs     ? kv_append_kernel<kAnyPairs, 1>
-           : form == kInterQuads ? (q.many ? kv_append_kernel<kInterQuads, 4> : kv_append_kernel<kInterQuads, 1>)
-                                 : (q.many ? kv_append_kernel<kHalfQuads, 4> : kv_append_kernel<kHalfQuads, 1>);
+  // The cache's rows take their share of the caches too.
+  q.stream = q.many && rows * (hq + 2 * L.desc.num_kv_heads) * kDim * 2 >= kStreamBytes;
+  auto quads = [&](auto key_form) {
+    constexpr int kForm = decltype(key_form)::value;
+    return !q.many    ? kv_append_kernel<kForm, 1, kCached>
+           : q.stream ? kv_append_kernel<kForm, 4, kReadsWrites>
+                      : kv_append_kernel<kForm, 4, kCached>;
+  };
+  auto k = form == kAnyPairs     ? kv_append_kernel<kAnyPairs, 1, kCached>
+           : form == kInterQuads ? quads(std::integral_constant<int, kInterQuads>{})
+                                 : quads(std::integral_constant<int, kHalfQuads>{});
   // Rows that one launch takes: at most kMaxBlocks blocks of either kind.
   WriteArgs A = write_args(L, n);
   A.slots = slots;
