@@ -238,9 +238,12 @@ __device__ __forceinline__ void turn_any(const uint16_t* row, const TurnCosSin& 
   finite_low(largest, low);
 }
 
-template <int kWaves, bool kRotary>
+// kLow: how many of the eight 16-channel products of a score a turned query's lower part
+// takes: all, or the first four if nothing turns beyond channel 64; 0 if queries come as they are.
+template <int kWaves, int kLow>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2)))
-void chunk_kernel(std::conditional_t<kRotary, ChunkRotaryArgs, ChunkArgs> A) {
+void chunk_kernel(std::conditional_t<kLow != 0, ChunkRotaryArgs, ChunkArgs> A) {
+  constexpr bool kRotary = kLow != 0;
   constexpr bool kWide = kWaves == kWideWaves;
   constexpr int kThreads = 64 * kWaves;
   constexpr int kRows = 32 * kWaves;
@@ -463,7 +466,7 @@ void chunk_kernel(std::conditional_t<kRotary, ChunkRotaryArgs, ChunkArgs> A) {
     for (int c = 0; c < 8; ++c) {
       const uint4 kr = kst(stage_tag)[j][(2 * c + hh) * 16 + (col & 15)];
       a = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kr), qop[c], a, 0, 0, 0);
-      if constexpr (kRotary)
+      if (c < kLow)
         a = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kr), qlow[c], a, 0, 0, 0);
     }
     s = a;
@@ -576,7 +579,7 @@ void chunk_kernel(std::conditional_t<kRotary, ChunkRotaryArgs, ChunkArgs> A) {
     for (int c = 0; c < 8; ++c) {
       if constexpr (!kLast) {
         qs = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kpre[c]), qop[c], qs, 0, 0, 0);
-        if constexpr (kRotary)
+        if (c < kLow)
           qs = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(kpre[c]), qlow[c], qs, 0, 0, 0);
       }
       const int jj = c >> 2, cb = c & 3;
@@ -759,13 +762,13 @@ ChunkArgs chunk_args(const KvLayout& L, const Plan& P, void* ws, const void* q,
   return A;
 }
 
-template <bool kRotary, class Args>
+template <int kLow, class Args>
 hipError_t launch_form(const Plan& P, const Args& A, hipStream_t s) {
   const dim3 grid{unsigned(P.chunk_grid)};
   if (P.chunk_form != kUnits)
-    hipLaunchKernelGGL((chunk_kernel<kNarrowWaves, kRotary>), grid, dim3(64 * kNarrowWaves), 0, s, A);
+    hipLaunchKernelGGL((chunk_kernel<kNarrowWaves, kLow>), grid, dim3(64 * kNarrowWaves), 0, s, A);
   else
-    hipLaunchKernelGGL((chunk_kernel<kWideWaves, kRotary>), grid, dim3(64 * kWideWaves), 0, s, A);
+    hipLaunchKernelGGL((chunk_kernel<kWideWaves, kLow>), grid, dim3(64 * kWideWaves), 0, s, A);
   return hipGetLastError();
 }
 
@@ -775,7 +778,7 @@ hipError_t launch_chunk(const KvLayout& L, const Plan& P, void* ws, const void* 
                         const int32_t* bt, int32_t stride, float scale, void* out, float* lse,
                         hipStream_t s) {
   if (P.info.n_chunk == 0) return hipSuccess;
-  return launch_form<false>(P, chunk_args(L, P, ws, q, bt, stride, scale, out, lse), s);
+  return launch_form<0>(P, chunk_args(L, P, ws, q, bt, stride, scale, out, lse), s);
 }
 
 hipError_t launch_chunk_rotary(const KvLayout& L, const Plan& P, void* ws, const NewRows& n,
@@ -787,7 +790,7 @@ hipError_t launch_chunk_rotary(const KvLayout& L, const Plan& P, void* ws, const
   A.rot = rotary_args<kRotaryPairs>(*n.rotary);
   A.positions = n.positions;
   A.q_row = n.q_row;
-  return launch_form<true>(P, A, s);
+  return n.rotary->rotary_dim <= 64 ? launch_form<4>(P, A, s) : launch_form<8>(P, A, s);
 }
 
 }  // namespace libra
