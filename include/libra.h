@@ -528,10 +528,13 @@ libra_status libra_kv_append(libra_kv_layout layout, libra_rotary rotary,
 
 /* libra_append_attn from unturned projections: keys are turned on their way into the cache
  * (to the bits libra_rotary_apply gives), queries where the attention kernels load them, and
- * neither is written out.  A turned query enters the scores as the sum of two bf16 numbers a
- * channel, 16 bits, so that scores and lse are float32's of the unrounded queries (within
- * 2^-17 of each product; turned queries rounded to bf16 would put 2^-8 into them).  q, k_new
- * and v_new are rows as in libra_kv_append, [sum C_b] of them in libra_append_attn's order.
+ * neither is written out.  With round_queries = 0 a turned query enters the scores as the sum
+ * of two bf16 numbers a channel, 16 bits, so that scores and lse are float32's of the
+ * unrounded queries (within 2^-17 of each product).  Otherwise it is rounded to bf16, which
+ * puts 2^-8 into the products and gives the bits of turning q and k_new with
+ * libra_rotary_apply and calling libra_append_attn; chunks, which the matrix cores bound,
+ * take 16-25% less time so, single rows the same.  q, k_new and v_new are rows as in
+ * libra_kv_append, [sum C_b] of them in libra_append_attn's order.
  * positions: device int32 [sum C_b], or NULL for each token's index in its sequence's cache
  * (P_b + i); positions need not follow the index, as where part of a context has been
  * dropped, but the causal order is the cache's.  A key that a row sees must be finite (an
@@ -543,8 +546,8 @@ libra_status libra_append_attn_rotary(libra_kv_layout layout, libra_plan plan,
                                       int64_t k_row_stride, const void* v_new,
                                       int64_t v_row_stride, const int32_t* block_table,
                                       int32_t bt_stride, int32_t batch, int32_t num_q_heads,
-                                      float scale, void* workspace, size_t ws_bytes, void* out,
-                                      float* lse, void* stream);
+                                      float scale, int32_t round_queries, void* workspace,
+                                      size_t ws_bytes, void* out, float* lse, void* stream);
 
 /* ------------------------------------------------------------------------------ */
 /* Per-kernel timing                                                               */

@@ -239,7 +239,9 @@ __device__ __forceinline__ void turn_any(const uint16_t* row, const TurnCosSin& 
 }
 
 // kLow: how many of the eight 16-channel products of a score a turned query's lower part
-// takes: all, or the first four if nothing turns beyond channel 64; 0 if queries come as they are.
+// takes: all, or the first four if nothing turns beyond channel 64, or none (kRounded).  0: queries
+// come as they are.
+constexpr int kRounded = -1;
 template <int kWaves, int kLow>
 __global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void chunk_kernel(std::conditional_t<kLow != 0, ChunkRotaryArgs, ChunkArgs> A) {
@@ -790,6 +792,7 @@ hipError_t launch_chunk_rotary(const KvLayout& L, const Plan& P, void* ws, const
   A.rot = rotary_args<kRotaryPairs>(*n.rotary);
   A.positions = n.positions;
   A.q_row = n.q_row;
+  if (n.round_queries) return launch_form<kRounded>(P, A, s);
   return n.rotary->rotary_dim <= 64 ? launch_form<4>(P, A, s) : launch_form<8>(P, A, s);
 }
 

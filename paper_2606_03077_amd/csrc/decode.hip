@@ -202,6 +202,7 @@ struct DecodeRotaryArgs : DecodeArgs {
   const uint16_t* k_new;
   const uint16_t* v_new;
   int64_t k_row, v_row;
+  int round_queries;
 };
 
 // Turned rows in LDS, 16 granules each.  kPaired: the heads' upper parts, and from kNewRow on
@@ -283,7 +284,7 @@ void decode_kernel(std::conditional_t<kForm == kPlain, DecodeArgs, DecodeRotaryA
     turn_granules<1, true>(in, gi, rows.cs, is_v ? 0 : rdim, inter, hi, lo);
     const bool unused = h >= G && !is_k && !is_v;
     rows.hi[h][gi[0]] = unused ? make_uint4(0, 0, 0, 0) : hi[0];
-    rows.lo[h][gi[0]] = unused ? make_uint4(0, 0, 0, 0) : lo[0];
+    rows.lo[h][gi[0]] = unused || A.round_queries ? make_uint4(0, 0, 0, 0) : lo[0];
     if (is_k || is_v) {
       const size_t page = size_t(A.bt[int64_t(b) * A.bt_stride + prior / kPage]);
       const size_t tile = (page * A.hkv + g) * kTileElems;
@@ -518,6 +519,7 @@ hipError_t launch_decode_rotary(const KvLayout& L, const Plan& P, void* ws, cons
   A.v_new = static_cast<const uint16_t*>(n.v);
   A.k_row = n.k_row;
   A.v_row = n.v_row;
+  A.round_queries = n.round_queries;
   auto k = P.group <= 8 ? decode_kernel<kPaired> : decode_kernel<kSplit>;
   hipLaunchKernelGGL(k, dim3(unsigned(units)), dim3(kThreads), 0, s, A);
   return hipGetLastError();

@@ -229,8 +229,8 @@ libra_status libra_append_attn_rotary(libra_kv_layout layout, libra_plan plan,
                                       int64_t k_row_stride, const void* v_new,
                                       int64_t v_row_stride, const int32_t* block_table,
                                       int32_t bt_stride, int32_t batch, int32_t num_q_heads,
-                                      float scale, void* workspace, size_t ws_bytes, void* out,
-                                      float* lse, void* stream) {
+                                      float scale, int32_t round_queries, void* workspace,
+                                      size_t ws_bytes, void* out, float* lse, void* stream) {
   libra_status st = check_call(layout, plan, LIBRA_MODE_APPEND, q, block_table, bt_stride, batch,
                                num_q_heads, scale, out);
   if (st != LIBRA_OK) return st;
@@ -252,7 +252,8 @@ libra_status libra_append_attn_rotary(libra_kv_layout layout, libra_plan plan,
   if (st != LIBRA_OK) return st;
   const Plan& P = *form;
   const KvLayout& L = *layout;
-  const NewRows n{rotary, positions, q, k_new, v_new, q_row_stride, k_row_stride, v_row_stride};
+  const NewRows n{rotary, positions, q, k_new, v_new, q_row_stride, k_row_stride, v_row_stride,
+                  round_queries != 0};
   // Decode units of up to 8 heads write their rows' tokens themselves, and without chunk rows
   // there are no others.
   const bool fused = P.info.n_chunk == 0 && P.group <= 8;

@@ -27,6 +27,7 @@ struct NewRows {
   const void* k;
   const void* v;
   int64_t q_row, k_row, v_row;  // row strides in elements; heads are 128 apart
+  bool round_queries = false;   // attention: to bf16, instead of two bf16 parts
 };
 // Rows to slots[row]; q (if given) turned to q_out.
 hipError_t launch_kv_append(const KvLayout& L, const NewRows& n, const int64_t* slots,

@@ -166,7 +166,8 @@ def load() -> ctypes.CDLL:
                                               P]),
         "libra_kv_append": (ctypes.c_int, [P, P, P, P, I64, P, I64, I32, P, I64, P, I64, P, P]),
         "libra_append_attn_rotary": (ctypes.c_int, [P, P, P, P, P, I64, P, I64, P, I64, P, I32,
-                                                    I32, I32, ctypes.c_float, P, SZ, P, P, P]),
+                                                    I32, I32, ctypes.c_float, I32, P, SZ, P, P,
+                                                    P]),
         "libra_profile_enable": (ctypes.c_int, [ctypes.c_int]),
         "libra_profile_collect": (ctypes.c_int, [ctypes.POINTER(KernelTimes)]),
         "libra_ce_fit": (ctypes.c_int, [DP, DP, I32, ctypes.POINTER(CePoly)]),
@@ -532,9 +533,11 @@ def libra_kv_append(layout: int, rotary: Optional[int], positions, slots, q, k_n
 
 def libra_append_attn_rotary(layout: int, plan: int, rotary: int, positions, q, k_new, v_new,
                              block_table, bt_stride: int, batch: int, num_q_heads: int,
-                             scale: float, workspace, out, lse=None, stream=None):
+                             scale: float, workspace, out, lse=None, stream=None,
+                             round_queries: bool = False):
     """libra_append_attn from unturned projections, whose rows may be slices of one tensor;
-    positions [rows] (int32), or None for each token's index in its cache."""
+    positions [rows] (int32), or None for each token's index in its cache.  round_queries:
+    turned queries as bf16, as from libra_rotary_apply, instead of in 16 bits."""
     ws_bytes = workspace.numel() * workspace.element_size()
     rows = q.shape[0]
     qp, qs, _ = _rows(q, rows, num_q_heads, "q")
@@ -543,9 +546,9 @@ def libra_append_attn_rotary(layout: int, plan: int, rotary: int, positions, q, 
     _check(load().libra_append_attn_rotary(layout, plan, rotary,
                                            _vector(positions, torch.int32, rows, "positions"), qp,
                                            qs, kp, ks, vp, vs, _ptr(block_table), bt_stride, batch,
-                                           num_q_heads, scale, _ptr(workspace), ws_bytes,
-                                           _ptr(out), _ptr(lse), _stream(stream)),
-           "libra_append_attn_rotary")
+                                           num_q_heads, scale, 1 if round_queries else 0,
+                                           _ptr(workspace), ws_bytes, _ptr(out), _ptr(lse),
+                                           _stream(stream)), "libra_append_attn_rotary")
 
 
 def libra_profile_enable(enable: bool = True) -> None:

@@ -101,7 +101,7 @@ int main() {
     CHECK(libra_kv_append(lay, rot, i32, i64, rows, p, 1024, hq, p, 1536, p, 1536, p, nullptr) ==
           LIBRA_OK);
     CHECK(libra_append_attn_rotary(lay, plan, rot, nullptr, p, 1536, p, 1536, p, 1536, i32, 200, B,
-                                   hq, 0.1f, ws, ws_bytes, p, nullptr, nullptr) == LIBRA_OK);
+                                   hq, 0.1f, i & 1, ws, ws_bytes, p, nullptr, nullptr) == LIBRA_OK);
     if (i == 0) copies = g_fake_hip.memcpy_async;
   }
   CHECK(g_rotary == 3 && g_append == 3 && g_write == 3 && g_decode == 3 && g_chunk == 3);

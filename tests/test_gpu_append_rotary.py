@@ -1,7 +1,8 @@
 """libra_append_attn_rotary on the GPU, in every launched form (decode units, wide and narrow
 chunk tiles, split keys).
 
-Where nothing turns (frequencies of zero) it gives libra_append_attn's bits.  Turned, the cache
+Where nothing turns (frequencies of zero) it gives libra_append_attn's bits, and with queries
+rounded to bf16 those of libra_rotary_apply and libra_append_attn.  Turned, the cache
 holds libra_rotary_apply's bits, and outputs are those of float64 attention of the exactly turned
 queries over that cache: queries enter the scores as two bf16 parts, so what is left of them is
 2^-17 of each channel (two halvings of 2^-8 and the turn's own error), and a score, a sum of 128
@@ -52,17 +53,29 @@ class Step:
         self.cache.k.copy_(self.k0)
         self.cache.v.copy_(self.v0)
 
-    def call(self, rope, out, lse, ws=None, stream=None):
+    def call(self, rope, out, lse, ws=None, stream=None, round_queries=False):
         libra.libra_append_attn_rotary(
             self.cache.layout, self.plan, rope.h, self.given, self.q, self.k, self.v, self.cache.bt,
             self.cache.bt_stride, len(self.lens), self.hq, self.batch.scale,
-            self.ws if ws is None else ws, out, lse, stream=stream)
+            self.ws if ws is None else ws, out, lse, stream=stream, round_queries=round_queries)
 
     def unturned(self):
         """libra_append_attn on the projections as they are."""
         out, lse = self.outputs()
         libra.libra_append_attn(self.cache.layout, self.plan, self.q.contiguous(),
                                 self.k.contiguous(), self.v.contiguous(), self.cache.bt,
+                                self.cache.bt_stride, len(self.lens), self.hq, self.batch.scale,
+                                self.ws, out, lse)
+        torch.cuda.synchronize()
+        return out, lse, self.cache.k.clone(), self.cache.v.clone()
+
+    def turned_first(self, rope):
+        """libra_append_attn on projections that libra_rotary_apply has turned."""
+        q, k = (torch.empty(t.shape, dtype=BF16, device="cuda") for t in (self.q, self.k))
+        libra.libra_rotary_apply(rope.h, self.q, self.pd, q)
+        libra.libra_rotary_apply(rope.h, self.k, self.pd, k)
+        out, lse = self.outputs()
+        libra.libra_append_attn(self.cache.layout, self.plan, q, k, self.v.contiguous(), self.cache.bt,
                                 self.cache.bt_stride, len(self.lens), self.hq, self.batch.scale,
                                 self.ws, out, lse)
         torch.cuda.synchronize()
@@ -140,6 +153,10 @@ CASES = [
     ("split keys", [2900, 700], [32, 1], 8, 2, dict(num_cus=4)),
     ("wide tiles", [2100, 1500, 900], [2100, 700, 900], 40, 8, dict(num_cus=16)),
     ("long prior", [70000], [40], 10, 2, {}),
+    ("decode, eight heads a group", [1, 16, 17, 900, 4097], [1] * 5, 16, 2, dict(num_cus=32, min_split_pages=2)),
+    ("decode, nine heads a group", [1, 16, 17, 900], [1] * 4, 18, 2, dict(num_cus=32, min_split_pages=2)),
+    ("decode, sixteen heads a group", [1, 700, 33, 48], [1] * 4, 16, 1, {}),
+    ("decode beside a chunk, sixteen heads", [700, 150], [1, 90], 32, 2, dict(num_cus=32)),
 ]
 ROPES = [dict(), dict(rdim=64, interleaved=True), dict(rdim=20), dict(rdim=96, amplitude=1.25),
          dict(interleaved=True), dict(rdim=32), dict(rdim=2, interleaved=True), dict(rdim=112)]
@@ -170,6 +187,10 @@ def test_cases(case, shift):
         rope = Handle(**kw)
         s.reset()
         s.check(rope, s.one_step(rope), f"{name} {kw}")
+        s.reset()
+        rounded = s.one_step(rope, round_queries=True)
+        s.reset()
+        same(rounded, s.turned_first(rope), f"{name} {kw} rounded")
         rope.close()
     s.close()
 
@@ -185,6 +206,83 @@ def test_random_batches(seed):
     rope = Handle(rdim=2 * int(rng.integers(1, 65)), interleaved=bool(rng.integers(2)))
     H.say(f"[case] append rotary random {seed}: G={G} hkv={hkv} lens={lens} news={news} R={rope.rdim}")
     s.check(rope, s.one_step(rope), f"random {seed}")
+    s.reset()
+    rounded = s.one_step(rope, round_queries=True)
+    s.reset()
+    same(rounded, s.turned_first(rope), f"random {seed} rounded")
+    rope.close()
+    s.close()
+
+
+@pytest.mark.parametrize("lens,news,hq,hkv", [([900, 1500], [1, 1], 8, 2), ([1500, 700], [400, 90], 10, 2),
+                                              ([3000], [20], 8, 2)])
+def test_scores_whose_maximum_moves(lens, news, hq, hkv):
+    """Scores of size 16, so that running maxima move by far more than a product's exponent."""
+    H.say(f"[case] append rotary large scores {lens} {news}")
+    s = Step(lens, news, hq, hkv, seed=60, num_cus=4)
+    s.qkv[:, :hq + hkv] *= 4
+    s.cache.k.view(BF16).mul_(4)
+    rope = Handle(rdim=96)
+    out, lse, _, _ = s.one_step(rope)
+    o, l = H.bf16_dev_to_f64(out), lse.double().cpu().numpy()
+    q = torch.from_numpy(rope.turn(f64(s.q), s.pos)).cuda()
+    G, r0 = hq // hkv, 0
+    for (k, v), n, c in zip(s.tokens(), lens, news):
+        seen = torch.arange(n, device="cuda")[None] <= torch.arange(n - c, n, device="cuda")[:, None]
+        for h in range(hq):
+            z = (q[r0:r0 + c, h] @ k[:, h // G].double().t()) * s.batch.scale
+            z.masked_fill_(~seen, -np.inf)
+            L = torch.logsumexp(z, dim=1)
+            p = torch.exp(z - L[:, None])
+            want = (p @ v[:, h // G].double()).cpu().numpy()
+            # A score is off by at most eps = scale |q| |k| (2^-17 + 2^-17), a probability by
+            # that and by bf16's 2^-8, the output by its own 2^-8.
+            eps = float(s.batch.scale * q[r0:r0 + c, h].norm(dim=-1).max() *
+                        k[:, h // G].double().norm(dim=-1).max()) * 2.0 ** -16
+            size = (p @ v[:, h // G].double().abs()).cpu().numpy()
+            assert (np.abs(o[r0:r0 + c, h] - want) <= (2 * eps + 2.0 ** -8) * size + 2.0 ** -8 * np.abs(want)).all()
+            L = L.cpu().numpy()
+            assert (np.abs(l[r0:r0 + c, h] - L) <= eps + 2.0 ** -20 * (4 + np.abs(L))).all()
+        r0 += c
+    rope.close()
+    s.close()
+
+
+@pytest.mark.parametrize("rdim,interleaved", [(128, False), (128, True), (20, False)])
+def test_other_rows_do_not_see_a_rows_infinities(rdim, interleaved):
+    """A query that is infinite, NaN, or turns past bf16's largest value, and a NaN new key: only
+    its own row, or its own sequence's rows that see it, go wrong.  The chunk kernel's running
+    maxima move by a vote of a wave's 32 rows, so that the others' probabilities are rounded to
+    bf16 against another maximum, which is 2^-8 of each, twice, and of the outputs."""
+    H.say(f"[case] append rotary non-finite R={rdim}")
+    s = Step([300, 200, 90], [1, 60, 40], 8, 2, seed=61)
+    rope = Handle(rdim=rdim, interleaved=interleaved, amplitude=2.0)
+    clean = s.one_step(rope)
+    q0 = s.qkv.clone()
+    most = max(float(v.abs().max()) for _, v in s.tokens())
+
+    def near(got, clean, keep):
+        a, b = (t[0].view(BF16).float()[keep] for t in (got, clean))
+        assert bool(((a - b).abs() <= 2 * 2.0 ** -8 * most + 2 * 2.0 ** -8 * b.abs()).all())
+        a, b = (t[1][keep] for t in (got, clean))
+        assert bool(((a - b).abs() <= 2.0 ** -20 * (4 + b.abs())).all())
+
+    for value in (float("inf"), float("nan"), 3.3e38):
+        s.qkv.copy_(q0)
+        s.qkv[0, 3, 1] = s.qkv[7, 5, 0] = s.qkv[30, 0, 9] = value
+        s.reset()
+        got = s.one_step(rope)
+        keep = torch.ones((s.rows, s.hq), dtype=torch.bool, device="cuda")
+        keep[0, 3] = keep[7, 5] = keep[30, 0] = False
+        near(got, clean, keep)
+    s.qkv.copy_(q0)
+    s.qkv[1 + 25, s.hq, 2] = float("nan")              # sequence 1, new token 25, KV head 0
+    s.reset()
+    got = s.one_step(rope)
+    keep = torch.ones((s.rows, s.hq), dtype=torch.bool, device="cuda")
+    keep[1 + 25:61, :4] = False
+    near(got, clean, keep)
+    assert not torch.isfinite(got[0][26:61, :4].view(BF16)).any()
     rope.close()
     s.close()
 
@@ -237,6 +335,52 @@ def test_replays_from_a_graph_with_new_positions():
     del g
     rope.close()
     s.close()
+
+
+def test_single_rows_replay_from_a_graph():
+    """A step of single rows is one launch (and a merge): the units write the new tokens.  Each
+    replay has other projections, and the page it writes still holds the last replay's token."""
+    H.say("[case] append rotary graph of single rows")
+    s = Step([600, 1, 16, 17, 5000], [1] * 5, 28, 4, shift=3, num_cus=64)
+    rope = Handle()
+    out, lse = s.outputs()
+    s.call(rope, out, lse)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        s.call(rope, out, lse)
+    for i in range(3):
+        s.qkv.copy_(randn(s.qkv.shape, BF16, 40 + i))
+        out.fill_(NAN)
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        got = out.clone(), lse.clone(), s.cache.k.clone(), s.cache.v.clone()
+        s.check(rope, got, f"replay {i}")
+        same(s.one_step(rope), got, f"replay {i}")
+    del g
+    rope.close()
+    s.close()
+
+
+def test_launches_of_a_step():
+    """Per-kernel timing sees one decode launch for single rows, a cache write beside chunks."""
+    H.say("[case] append rotary launches")
+    rope = Handle()
+    for news, kinds in (([1, 1], {"decode"}), ([1, 40], {"cache_write", "decode", "chunk"})):
+        s = Step([300, 200], news, 8, 2, num_cus=8, min_split_pages=64)
+        s.one_step(rope)
+        libra.libra_profile_enable(True)
+        try:
+            libra.libra_profile_collect()
+            s.one_step(rope)
+            libra.libra_rotary_apply(rope.h, s.k, s.pd, torch.empty_like(s.k))
+            seen = libra.libra_profile_collect()
+        finally:
+            libra.libra_profile_enable(False)
+        assert {k for k, (_, n) in seen.items() if n} == kinds | {"rotary"}, seen
+        s.close()
+    rope.close()
 
 
 def test_stale_nan_behind_the_last_token():

@@ -185,6 +185,28 @@ def test_slots_past_32_bits_of_elements():
     rope.close()
 
 
+def test_rows_of_several_launches():
+    """With 1,024 KV heads a launch takes 65,536 rows.  Only the rows around that are not
+    padding, so that only their projections exist."""
+    H.say("[case] kv append several launches")
+    hkv, per_launch, rows = 1024, 65536, 65536 + 50
+    cache, rope = Cache(8, hkv), Handle()
+    first = per_launch - 21                                 # a run across the two launches
+    k, v = randn((71, hkv, 128), BF16, 12), randn((71, hkv, 128), BF16, 13)
+    slots = np.full(rows, -1, np.int64)
+    slots[first:first + 71] = np.arange(5, 76)
+    pos = np.arange(rows, dtype=np.int32)
+    sd, pd = torch.from_numpy(slots).cuda(), torch.from_numpy(pos).cuda()
+    at = first * hkv * 128 * 2                              # the rows before are never read
+    status = libra.load().libra_kv_append(
+        cache.layout, rope.h, pd.data_ptr(), sd.data_ptr(), rows, None, 0, 0, k.data_ptr() - at,
+        hkv * 128, v.data_ptr() - at, hkv * 128, None, torch.cuda.current_stream().cuda_stream)
+    assert status == 0
+    check_cache(cache, rope, slots[first:first + 71], pos[first:first + 71], k, v, "launches")
+    rope.close()
+    cache.close()
+
+
 def _decode(cache, plan, q, table, batch, hq, scale, ws):
     out = torch.full((batch, hq, 128), 0x7FC0, dtype=torch.int16, device="cuda")
     lse = torch.full((batch, hq), float("nan"), device="cuda")

@@ -253,6 +253,26 @@ def test_offsets_past_32_bits():
     r.close()
 
 
+def test_rows_of_several_launches():
+    """More rows than one launch takes (2^22 blocks of 256 pieces in the narrow form)."""
+    H.say("[case] rotary several launches")
+    dim, rdim = 512, 20
+    per_launch = 2 ** 22 * 256 // (dim - rdim // 2)
+    rows = per_launch + 777
+    r = Handle(dim, rdim)
+    x = torch.zeros((rows, 1, dim), dtype=torch.bfloat16, device="cuda")
+    out = torch.full_like(x, 5.0)
+    look = torch.tensor([0, 1, per_launch - 2, per_launch - 1, per_launch, per_launch + 1, rows - 1],
+                        device="cuda")
+    x[look] = randn((len(look), 1, dim), torch.bfloat16, 25)
+    p = torch.arange(rows, dtype=torch.int32, device="cuda") % 5000
+    libra.libra_rotary_apply(r.h, x, p, out)
+    torch.cuda.synchronize()
+    r.check(f64(out[look]), f64(x[look]), p[look].cpu().numpy(), torch.bfloat16)
+    assert not bool((out == 5.0).any())
+    r.close()
+
+
 def test_other_stream_and_graph_with_new_positions():
     H.say("[case] rotary stream and graph")
     r = Handle(128, 128, True)

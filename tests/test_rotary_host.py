@@ -165,7 +165,7 @@ def test_refused_append_attn(rotary):
     def call(plan=plan, h=rotary, pos=None, q=P, qr=512, k=P, kr=256, v=P, vr=256, bt=P, stride=2,
              batch=2, hq=4, scale=0.1, ws=P, n=1 << 30, out=P):
         return _raw("libra_append_attn_rotary", lay, plan, h, pos, q, qr, k, kr, v, vr, bt, stride,
-                    batch, hq, scale, ws, n, out, None, None)
+                    batch, hq, scale, 0, ws, n, out, None, None)
 
     for kw, status in [(dict(plan=decode), INVAL), (dict(plan=None), INVAL), (dict(h=None), INVAL),
                        (dict(h=other), INVAL), (dict(q=None), INVAL), (dict(q=P + 8), INVAL),
