@@ -202,7 +202,7 @@ __device__ __forceinline__ void turn_interleaved(const uint4 (&raw)[8], const Tu
   finite_low(largest, low);
 }
 
-// Any other R: channel by channel, in a loop.
+// Any other R: channel by channel, a granule at a time.
 __device__ __forceinline__ void turn_any(const uint16_t* row, const TurnCosSin& cs, int t, int hh,
                                          const RotaryArgs<kRotaryPairs>& rot, bf16x8 (&op)[8],
                                          bf16x8 (&low)[8]) {
@@ -211,24 +211,34 @@ __device__ __forceinline__ void turn_any(const uint16_t* row, const TurnCosSin& 
   const int h = rot.rdim / 2;
   float largest = 0.f;
 #pragma unroll 1
-  for (int i = 0; i < 32; ++i) {
-    const int d0 = 16 * (i / 4) + 8 * hh + 2 * (i % 4);
-    const uint32_t raw = *reinterpret_cast<const uint32_t*>(row + d0);
-    float y[2];
+  for (int c = 0; c < 8; ++c) {
+    const int first_d = 16 * c + 8 * hh;
+    const uint4 r4 = *reinterpret_cast<const uint4*>(row + first_d);
+    const uint32_t raw[4] = {r4.x, r4.y, r4.z, r4.w};
+    uint16_t other[8];
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      const int d = d0 + e;
-      const bool first = rot.interleaved ? e == 0 : d < h, turned = d < rot.rdim;
-      const int other = !turned ? d : rot.interleaved ? d ^ 1 : first ? d + h : d - h;
-      const float2 k = cs.one(t, !turned ? 0 : rot.interleaved ? d / 2 : first ? d : d - h);
-      const float x = bf16_to_f32((raw >> (16 * e)) & 0xFFFF), o = bf16_to_f32(row[other]);
-      y[e] = first ? turn_first(x, o, k) : turn_second(o, x, k);
-      if (turned) largest = fmaxf(largest, fabsf(y[e]));
+    for (int e = 0; e < 8; ++e) {
+      const int d = first_d + e;
+      other[e] = row[d >= rot.rdim ? d : rot.interleaved ? d ^ 1 : d < h ? d + h : d - h];
     }
-    const uint2 p = split_pair(y[0], y[1]);
-    const uint32_t keep = (d0 < rot.rdim ? 0u : 0x0000FFFFu) | (d0 + 1 < rot.rdim ? 0u : 0xFFFF0000u);
-    hi[i] = (raw & keep) | (p.x & ~keep);
-    lo[i] = p.y & ~keep;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+      float y[2];
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        const int d = first_d + 2 * w + e;
+        const bool first = rot.interleaved ? e == 0 : d < h, turned = d < rot.rdim;
+        const float2 k = cs.one(t, !turned ? 0 : rot.interleaved ? d / 2 : first ? d : d - h);
+        const float x = bf16_to_f32((raw[w] >> (16 * e)) & 0xFFFF), o = bf16_to_f32(other[2 * w + e]);
+        y[e] = first ? turn_first(x, o, k) : turn_second(o, x, k);
+        if (turned) largest = fmaxf(largest, fabsf(y[e]));
+      }
+      const uint2 p = split_pair(y[0], y[1]);
+      const int d = first_d + 2 * w;
+      const uint32_t keep = (d < rot.rdim ? 0u : 0x0000FFFFu) | (d + 1 < rot.rdim ? 0u : 0xFFFF0000u);
+      hi[4 * c + w] = (raw[w] & keep) | (p.x & ~keep);
+      lo[4 * c + w] = p.y & ~keep;
+    }
   }
 #pragma unroll
   for (int c = 0; c < 8; ++c) {

@@ -127,6 +127,8 @@ __device__ __forceinline__ void load_granules(Granules<N>& in, const uint16_t* r
   } else {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
+      in.partner[i] = in.own[i];
+      if (8 * gi[i] >= rdim) continue;
       auto at = [&](int e) -> uint32_t {
         const int d = 8 * gi[i] + e;
         return row[d < h ? d + h : d < rdim ? d - h : d];

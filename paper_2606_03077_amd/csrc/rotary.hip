@@ -103,10 +103,11 @@ __device__ __forceinline__ void turn_quads(typename T::Quad& a, typename T::Quad
   b = T::pack(z);
 }
 
-// The quads of piece j of a head: pairs 4 j .. 4 j + 3 while j < R / 8, copied ones after.
+// The quads of piece j of a head of `pieces`: pairs 4 j .. 4 j + 3 while j < R / 8, copied ones
+// after.  Neighbours among the pieces read neighbouring quads.
 template <bool kInter>
-__device__ __forceinline__ int2 quads_of(int j, int R8) {
-  return kInter || j >= R8 ? make_int2(2 * j, 2 * j + 1) : make_int2(j, j + R8);
+__device__ __forceinline__ int2 quads_of(int j, int R8, int pieces) {
+  return kInter ? make_int2(2 * j, 2 * j + 1) : j < R8 ? make_int2(j, j + R8) : make_int2(j + R8, j + pieces);
 }
 
 template <bool kPastCaches, class Quad>
@@ -146,7 +147,7 @@ __device__ __forceinline__ void turn_rows_wide(const Rot& rot, const RowsArgs<T>
   const int R8 = rot.rdim / 8;
   const bool turned = j < R8;
   if (!turned && A.x == A.out) return;
-  const int2 qd = quads_of<kInter>(j, R8);
+  const int2 qd = quads_of<kInter>(j, R8, A.per_head);
   const int head0 = by * A.head_slots * kHeads + h0;
   const typename T::Elem* x = A.x + row * A.x_row;
   typename T::Elem* out = A.out + row * A.out_row;
@@ -193,20 +194,28 @@ __device__ __forceinline__ void turn_rows_narrow(const Rot& rot, const RowsArgs<
   if (row >= A.rows || skipped(A, row)) return;
   const typename T::Elem* x = A.x + row * A.x_row;
   typename T::Elem* out = A.out + row * A.out_row;
-  const int h0 = by * kNarrowHeads, h1 = min(A.heads, h0 + kNarrowHeads);
-  if (j >= half) {
-    if (A.x == A.out) return;
-    const int d = j + half;
-    for (int h = h0; h < h1; ++h) out[h * A.out_head + d] = x[h * A.x_head + d];
-    return;
+  const int h0 = by * kNarrowHeads;
+  const bool turned = j < half;
+  if (!turned && A.x == A.out) return;
+  const int d1 = !turned ? j + half : rot.interleaved ? 2 * j : j;
+  const int d2 = !turned ? d1 : rot.interleaved ? 2 * j + 1 : j + half;
+  typename T::Elem e1[kNarrowHeads], e2[kNarrowHeads];
+#pragma unroll
+  for (int i = 0; i < kNarrowHeads; ++i) {
+    const int64_t h = min(h0 + i, A.heads - 1);
+    e1[i] = x[h * A.x_head + d1];
+    e2[i] = x[h * A.x_head + d2];
   }
-  const int d1 = rot.interleaved ? 2 * j : j, d2 = rot.interleaved ? 2 * j + 1 : j + half;
-  float2 cs = rotary_cos_sin(rot.turn[j], A.positions[row], rot.amplitude);
+  float2 cs = make_float2(1.f, 0.f);
+  if (turned) cs = rotary_cos_sin(rot.turn[j], A.positions[row], rot.amplitude);
   if (A.backward) cs.y = -cs.y;
-  for (int h = h0; h < h1; ++h) {
-    const float x1 = T::get(x[h * A.x_head + d1]), x2 = T::get(x[h * A.x_head + d2]);
-    out[h * A.out_head + d1] = T::put(turn_first(x1, x2, cs));
-    out[h * A.out_head + d2] = T::put(turn_second(x1, x2, cs));
+#pragma unroll
+  for (int i = 0; i < kNarrowHeads; ++i) {
+    const int64_t h = h0 + i;
+    if (h >= A.heads) break;
+    const float x1 = T::get(e1[i]), x2 = T::get(e2[i]);
+    out[h * A.out_head + d1] = turned ? T::put(turn_first(x1, x2, cs)) : e1[i];
+    if (turned) out[h * A.out_head + d2] = T::put(turn_second(x1, x2, cs));
   }
 }
 
@@ -361,7 +370,7 @@ __device__ __forceinline__ NewPiece load_piece(const WriteArgs& A, const Rot& ro
   NewPiece p;
   const uint16_t* k = A.k_new + row * A.k_row + g * kDim;
   if constexpr (kForm != kAnyPairs) {
-    const int2 qd = quads_of<kForm == kInterQuads>(j, rot.rdim / 8);
+    const int2 qd = quads_of<kForm == kInterQuads>(j, rot.rdim / 8, kDim / 8);
     p.a = *reinterpret_cast<const uint2*>(k + 4 * qd.x);
     p.b = *reinterpret_cast<const uint2*>(k + 4 * qd.y);
   }
@@ -370,28 +379,45 @@ __device__ __forceinline__ NewPiece load_piece(const WriteArgs& A, const Rot& ro
   return p;
 }
 
-// Turns the piece's key and stores it to slot s of the K tile.  kAnyPairs: the 16 threads of
-// a row, in one wave, share the row's cosines and sines through cs.
+// Granule j of a bf16 row whose pairs may lie anywhere.  The 16 threads of a row, in one wave,
+// share the row's cosines and sines through cs; all of them read before any of them writes.
+__device__ __forceinline__ uint4 turn_any_granule(const Rot& rot, const uint16_t* row, int j,
+                                                  int32_t pos, float2* cs) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (4 * j + i < rot.rdim / 2)
+      cs[4 * j + i] = rotary_cos_sin(rot.turn[4 * j + i], pos, rot.amplitude);
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  const int gi[1] = {j};
+  Granules<1> in;
+  uint4 out[1], none[1];
+  load_granules(in, row, gi, rot.rdim, rot.interleaved);
+  turn_granules<1, false>(in, gi, cs, rot.rdim, rot.interleaved, out, none);
+  return out[0];
+}
+
+// 16 rows of one query head, any pairs.
+__device__ __forceinline__ void turn_queries_any(const Rot& rot, const RowsArgs<Bf16>& A, int64_t bx,
+                                                 int head, float2 (*cs)[kRotaryPairs]) {
+  const int s = threadIdx.x >> 4, j = threadIdx.x & 15;
+  const int64_t row = bx * kPage + s;
+  if (row >= A.rows || skipped(A, row)) return;
+  const uint4 y = turn_any_granule(rot, A.x + row * A.x_row + int64_t(head) * kDim, j, A.positions[row], cs[s]);
+  *reinterpret_cast<uint4*>(A.out + row * A.out_row + int64_t(head) * kDim + 8 * j) = y;
+}
+
+// Turns the piece's key and stores it to slot s of the K tile.
 template <int kForm>
 __device__ __forceinline__ void store_key(const WriteArgs& A, const Rot& rot, const NewPiece& p,
                                           int64_t row, int g, int j, int s, uint16_t* tile,
                                           float2* cs) {
   if constexpr (kForm == kAnyPairs) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (4 * j + i < rot.rdim / 2)
-        cs[4 * j + i] = rotary_cos_sin(rot.turn[4 * j + i], p.pos, rot.amplitude);
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    const int gi[1] = {j};
-    Granules<1> in;
-    uint4 k[1], none[1];
-    load_granules(in, A.k_new + row * A.k_row + g * kDim, gi, rot.rdim, rot.interleaved);
-    turn_granules<1, false>(in, gi, cs, rot.rdim, rot.interleaved, k, none);
-    *reinterpret_cast<uint4*>(tile + k_off(s, 8 * j)) = k[0];
+    *reinterpret_cast<uint4*>(tile + k_off(s, 8 * j)) =
+        turn_any_granule(rot, A.k_new + row * A.k_row + g * kDim, j, p.pos, cs);
   } else {
     constexpr bool kInter = kForm == kInterQuads;
-    const int2 qd = quads_of<kInter>(j, rot.rdim / 8);
+    const int2 qd = quads_of<kInter>(j, rot.rdim / 8, kDim / 8);
     uint2 a = p.a, b = p.b;
     if (j < rot.rdim / 8) {
       float2 t[4];
@@ -417,7 +443,7 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(Rot rot, WriteArgs 
     const int i = int(blockIdx.x) - A.kv_blocks;
     const int bx = i / Q.y_blocks;
     if constexpr (kForm == kAnyPairs)
-      turn_rows_narrow<Bf16>(rot, Q, bx, i - bx * Q.y_blocks);
+      turn_queries_any(rot, Q, bx, i - bx * Q.y_blocks, cs);
     else
       turn_rows_wide<Bf16, kForm == kInterQuads, kHeads, kStream>(rot, Q, bx, i - bx * Q.y_blocks);
     return;
@@ -527,6 +553,11 @@ hipError_t launch_kv_append(const KvLayout& L, const NewRows& n, const int64_t* 
   if (hq > 0)
     q = plan_rows<Bf16>(*n.rotary, {n.q, q_out, n.q_row, kDim, int64_t(hq) * kDim, kDim, n.positions,
                                     rows, hq, LIBRA_DTYPE_BF16, false});
+  if (form == kAnyPairs && hq > 0) {  // blocks of 16 rows of a head
+    q.wide = true, q.many = false;
+    q.args.block_rows = kPage;
+    q.args.y_blocks = hq;
+  }
   // The cache's rows take their share of the caches too.
   q.stream = q.many && rows * (hq + 2 * L.desc.num_kv_heads) * kDim * 2 >= kStreamBytes;
   auto quads = [&](auto key_form) {
