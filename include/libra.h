@@ -495,7 +495,7 @@ void libra_rotary_destroy(libra_rotary rotary);
 libra_status libra_rotary_get(libra_rotary rotary, int32_t* head_dim, int32_t* rotary_dim,
                               double* frequencies, double* amplitude);
 
-/* Turns rows x num_heads vectors of head_dim elements.  Element (r, h, d) of x lies at
+/* Turns rows x num_heads vectors of head_dim (the rotary's) elements.  Element (r, h, d) of x lies at
  * x + r * x_row_stride + h * x_head_stride + d, of out likewise (strides in elements; any
  * order of rows and heads; x's strides may be 0, out's vectors must not overlap).  positions:
  * device int32 [rows], any value.  backward != 0 gives the gradient's pass, the turn by the
@@ -505,8 +505,8 @@ libra_status libra_rotary_get(libra_rotary rotary, int32_t* head_dim, int32_t* r
 libra_status libra_rotary_apply(libra_rotary rotary, int32_t dtype, const void* x,
                                 int64_t x_row_stride, int64_t x_head_stride,
                                 const int32_t* positions, int64_t rows, int32_t num_heads,
-                                int32_t backward, void* out, int64_t out_row_stride,
-                                int64_t out_head_stride, void* stream);
+                                int32_t head_dim, int32_t backward, void* out,
+                                int64_t out_row_stride, int64_t out_head_stride, void* stream);
 
 /* Writes new rows into the cache, keys turned on the way: row r goes to slots[r] = page * 16
  * + slot (device int64 [rows]).  A row whose slot lies outside [0, 16 num_pages) is padding:
@@ -519,7 +519,8 @@ libra_status libra_rotary_apply(libra_rotary rotary, int32_t dtype, const void* 
  * multiples of 8, pointers 16-byte aligned.  rotary NULL: keys are written as they are and
  * positions is not read; else positions: device int32 [rows].
  * q (may be NULL, with q_out): device bf16 rows of num_q_heads heads at q_row_stride; turned
- * to q_out, [rows][num_q_heads][128], which may be q if its rows are dense.  Needs a rotary. */
+ * to q_out, [rows][num_q_heads][128], which may be q if its rows are dense and must not
+ * overlap anything else here.  Needs a rotary. */
 libra_status libra_kv_append(libra_kv_layout layout, libra_rotary rotary,
                              const int32_t* positions, const int64_t* slots, int64_t rows,
                              const void* q, int64_t q_row_stride, int32_t num_q_heads,
@@ -534,14 +535,14 @@ libra_status libra_kv_append(libra_kv_layout layout, libra_rotary rotary,
  * puts 2^-8 into the products and gives the bits of turning q and k_new with
  * libra_rotary_apply and calling libra_append_attn; chunks, which the matrix cores bound,
  * take 16-25% less time so, single rows the same.  q, k_new and v_new are rows as in
- * libra_kv_append, [sum C_b] of them in libra_append_attn's order.
- * positions: device int32 [sum C_b], or NULL for each token's index in its sequence's cache
+ * libra_kv_append, rows = sum C_b of them in libra_append_attn's order.
+ * positions: device int32 [rows], or NULL for each token's index in its sequence's cache
  * (P_b + i); positions need not follow the index, as where part of a context has been
  * dropped, but the causal order is the cache's.  A key that a row sees must be finite (an
  * infinite channel makes the row NaN); what lies behind a sequence's end may be anything.
  * Plans, workspaces, streams and graph capture are as for libra_append_attn. */
 libra_status libra_append_attn_rotary(libra_kv_layout layout, libra_plan plan,
-                                      libra_rotary rotary, const int32_t* positions,
+                                      libra_rotary rotary, const int32_t* positions, int64_t rows,
                                       const void* q, int64_t q_row_stride, const void* k_new,
                                       int64_t k_row_stride, const void* v_new,
                                       int64_t v_row_stride, const int32_t* block_table,

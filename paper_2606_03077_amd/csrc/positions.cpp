@@ -151,9 +151,11 @@ libra_status libra_rotary_get(libra_rotary rotary, int32_t* head_dim, int32_t* r
 libra_status libra_rotary_apply(libra_rotary rotary, int32_t dtype, const void* x,
                                 int64_t x_row_stride, int64_t x_head_stride,
                                 const int32_t* positions, int64_t rows, int32_t num_heads,
-                                int32_t backward, void* out, int64_t out_row_stride,
-                                int64_t out_head_stride, void* stream) {
+                                int32_t head_dim, int32_t backward, void* out,
+                                int64_t out_row_stride, int64_t out_head_stride, void* stream) {
   if (!rotary) return set_error(LIBRA_E_INVAL, "rotary is NULL");
+  if (head_dim != rotary->head_dim)
+    return set_error(LIBRA_E_INVAL, "head_dim differs from the rotary's");
   if (dtype != LIBRA_DTYPE_BF16 && dtype != LIBRA_DTYPE_FP16 && dtype != LIBRA_DTYPE_FP32)
     return set_error(LIBRA_E_UNSUPPORTED, "dtype must be bf16, fp16 or fp32");
   if (rows < 0 || num_heads < 0) return set_error(LIBRA_E_INVAL, "rows / num_heads < 0");
@@ -224,7 +226,7 @@ libra_status libra_kv_append(libra_kv_layout layout, libra_rotary rotary,
 }
 
 libra_status libra_append_attn_rotary(libra_kv_layout layout, libra_plan plan,
-                                      libra_rotary rotary, const int32_t* positions,
+                                      libra_rotary rotary, const int32_t* positions, int64_t rows,
                                       const void* q, int64_t q_row_stride, const void* k_new,
                                       int64_t k_row_stride, const void* v_new,
                                       int64_t v_row_stride, const int32_t* block_table,
@@ -237,8 +239,10 @@ libra_status libra_append_attn_rotary(libra_kv_layout layout, libra_plan plan,
   if (!rotary) return set_error(LIBRA_E_INVAL, "rotary is NULL");
   st = check_cached(*layout, *rotary);
   if (st != LIBRA_OK) return st;
-  if (plan->info.n_rows > 0) {
-    const int64_t hkv = layout->desc.num_kv_heads, rows = plan->info.n_rows;
+  if (rows != plan->info.n_rows)
+    return set_error(LIBRA_E_INVAL, "rows differ from the plan's new tokens");
+  if (rows > 0) {
+    const int64_t hkv = layout->desc.num_kv_heads;
     st = check_rows(q, rows, q_row_stride, num_q_heads, "q");
     if (st == LIBRA_OK) st = check_rows(k_new, rows, k_row_stride, hkv, "k_new");
     if (st == LIBRA_OK) st = check_rows(v_new, rows, v_row_stride, hkv, "v_new");

@@ -162,10 +162,10 @@ def load() -> ctypes.CDLL:
         "libra_rotary_create": (ctypes.c_int, [ctypes.POINTER(RotaryDesc), ctypes.POINTER(P)]),
         "libra_rotary_destroy": (None, [P]),
         "libra_rotary_get": (ctypes.c_int, [P, P, P, DP, DP]),
-        "libra_rotary_apply": (ctypes.c_int, [P, I32, P, I64, I64, P, I64, I32, I32, P, I64, I64,
-                                              P]),
+        "libra_rotary_apply": (ctypes.c_int, [P, I32, P, I64, I64, P, I64, I32, I32, I32, P, I64,
+                                              I64, P]),
         "libra_kv_append": (ctypes.c_int, [P, P, P, P, I64, P, I64, I32, P, I64, P, I64, P, P]),
-        "libra_append_attn_rotary": (ctypes.c_int, [P, P, P, P, P, I64, P, I64, P, I64, P, I32,
+        "libra_append_attn_rotary": (ctypes.c_int, [P, P, P, P, I64, P, I64, P, I64, P, I64, P, I32,
                                                     I32, I32, ctypes.c_float, I32, P, SZ, P, P,
                                                     P]),
         "libra_profile_enable": (ctypes.c_int, [ctypes.c_int]),
@@ -429,7 +429,6 @@ def libra_append_attn(layout: int, plan: int, q, k_new, v_new, block_table, bt_s
 _ROTARY_DTYPES = {torch.bfloat16: LIBRA_DTYPE_BF16, torch.float16: LIBRA_DTYPE_FP16,
                   torch.float32: LIBRA_DTYPE_FP32}
 _BF16_BITS = (torch.bfloat16, torch.int16)
-_rotary_head_dims = {}   # of the live handles made here
 
 
 def libra_rotary_create(head_dim: int = HEAD_DIM, rotary_dim: int = 0,
@@ -448,12 +447,10 @@ def libra_rotary_create(head_dim: int = HEAD_DIM, rotary_dim: int = 0,
                    slow, amplitude, None if f is None else _dp(f))
     h = ctypes.c_void_p()
     _check(load().libra_rotary_create(ctypes.byref(d), ctypes.byref(h)), "libra_rotary_create")
-    _rotary_head_dims[h.value] = head_dim
     return h.value
 
 
 def libra_rotary_destroy(rotary: int) -> None:
-    _rotary_head_dims.pop(rotary, None)
     load().libra_rotary_destroy(rotary)
 
 
@@ -501,15 +498,13 @@ def libra_rotary_apply(rotary: int, x, positions, out, backward: bool = False, s
     if out.dtype is not x.dtype or out.shape != x.shape or out.device != x.device:
         raise ValueError("out must be of x's shape, type and device")
     rows, heads, dim = x.shape
-    if dim != (_rotary_head_dims.get(rotary) or libra_rotary_get(rotary)["head_dim"]):
-        raise ValueError("x's head size differs from the rotary's")
     (xr, xh, xd), (outr, outh, outd) = x.stride(), out.stride()
     if dim > 1 and (xd != 1 or outd != 1):
         raise ValueError("the channels of a head must be contiguous")
     _check(load().libra_rotary_apply(rotary, dtype, x.data_ptr(), xr, xh,
                                      _vector(positions, torch.int32, rows, "positions"), rows,
-                                     heads, 1 if backward else 0, out.data_ptr(), outr, outh,
-                                     _stream(stream)), "libra_rotary_apply")
+                                     heads, dim, 1 if backward else 0, out.data_ptr(), outr,
+                                     outh, _stream(stream)), "libra_rotary_apply")
 
 
 def libra_kv_append(layout: int, rotary: Optional[int], positions, slots, q, k_new, v_new, q_out,
@@ -544,11 +539,12 @@ def libra_append_attn_rotary(layout: int, plan: int, rotary: int, positions, q, 
     kp, ks, hkv = _rows(k_new, rows, None, "k_new")
     vp, vs, _ = _rows(v_new, rows, hkv, "v_new")
     _check(load().libra_append_attn_rotary(layout, plan, rotary,
-                                           _vector(positions, torch.int32, rows, "positions"), qp,
-                                           qs, kp, ks, vp, vs, _ptr(block_table), bt_stride, batch,
-                                           num_q_heads, scale, 1 if round_queries else 0,
-                                           _ptr(workspace), ws_bytes, _ptr(out), _ptr(lse),
-                                           _stream(stream)), "libra_append_attn_rotary")
+                                           _vector(positions, torch.int32, rows, "positions"),
+                                           rows, qp, qs, kp, ks, vp, vs, _ptr(block_table),
+                                           bt_stride, batch, num_q_heads, scale,
+                                           1 if round_queries else 0, _ptr(workspace), ws_bytes,
+                                           _ptr(out), _ptr(lse), _stream(stream)),
+           "libra_append_attn_rotary")
 
 
 def libra_profile_enable(enable: bool = True) -> None:

@@ -100,12 +100,14 @@ def rotary():
     libra.libra_rotary_destroy(h)
 
 
-def _apply(h, dtype=0, x=P, xr=256, xh=128, pos=P, rows=3, heads=2, out=2 * P, outr=256, outh=128):
-    return _raw("libra_rotary_apply", h, dtype, x, xr, xh, pos, rows, heads, 0, out, outr, outh, None)
+def _apply(h, dtype=0, x=P, xr=256, xh=128, pos=P, rows=3, heads=2, dim=128, out=2 * P, outr=256,
+           outh=128):
+    return _raw("libra_rotary_apply", h, dtype, x, xr, xh, pos, rows, heads, dim, 0, out, outr, outh,
+                None)
 
 
 @pytest.mark.parametrize("kw,status", [
-    (dict(dtype=3), UNSUPPORTED), (dict(dtype=-1), UNSUPPORTED), (dict(rows=-1), INVAL),
+    (dict(dim=64), INVAL), (dict(dim=256), INVAL), (dict(dtype=3), UNSUPPORTED), (dict(dtype=-1), UNSUPPORTED), (dict(rows=-1), INVAL),
     (dict(heads=-1), INVAL), (dict(rows=2 ** 31), UNSUPPORTED), (dict(heads=65536), UNSUPPORTED),
     (dict(x=None), INVAL), (dict(out=None), INVAL), (dict(pos=None), INVAL),
     (dict(x=P + 1), INVAL), (dict(dtype=2, out=P + 2), INVAL), (dict(xr=-128), INVAL),
@@ -162,13 +164,14 @@ def test_refused_append_attn(rotary):
     decode = libra.libra_splitkv_plan(libra.LIBRA_MODE_DECODE, 2, 4, 2, [20, 5], None, num_cus=8)
     other = libra.libra_rotary_create(head_dim=64)
 
-    def call(plan=plan, h=rotary, pos=None, q=P, qr=512, k=P, kr=256, v=P, vr=256, bt=P, stride=2,
+    def call(plan=plan, h=rotary, pos=None, rows=4, q=P, qr=512, k=P, kr=256, v=P, vr=256, bt=P, stride=2,
              batch=2, hq=4, scale=0.1, ws=P, n=1 << 30, out=P):
-        return _raw("libra_append_attn_rotary", lay, plan, h, pos, q, qr, k, kr, v, vr, bt, stride,
+        return _raw("libra_append_attn_rotary", lay, plan, h, pos, rows, q, qr, k, kr, v, vr, bt, stride,
                     batch, hq, scale, 0, ws, n, out, None, None)
 
     for kw, status in [(dict(plan=decode), INVAL), (dict(plan=None), INVAL), (dict(h=None), INVAL),
-                       (dict(h=other), INVAL), (dict(q=None), INVAL), (dict(q=P + 8), INVAL),
+                       (dict(h=other), INVAL), (dict(rows=3), INVAL), (dict(rows=0), INVAL),
+                       (dict(q=None), INVAL), (dict(q=P + 8), INVAL),
                        (dict(qr=511), INVAL), (dict(qr=256), INVAL), (dict(k=None), INVAL),
                        (dict(kr=128), INVAL), (dict(v=P + 4), INVAL), (dict(vr=300), INVAL),
                        (dict(bt=None), INVAL), (dict(stride=1), INVAL), (dict(batch=1), INVAL),
