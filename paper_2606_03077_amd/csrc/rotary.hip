@@ -103,11 +103,19 @@ __device__ __forceinline__ void turn_quads(typename T::Quad& a, typename T::Quad
   b = T::pack(z);
 }
 
-// The quads of piece j of a head of `pieces`: pairs 4 j .. 4 j + 3 while j < R / 8, copied ones
-// after.  Neighbours among the pieces read neighbouring quads.
-template <bool kInter>
+// The quads of piece j of a head of `pieces`, turned ones while j < R / 8, copied ones after.
+// Neighbouring threads take neighbouring quads, so that an instruction covers whole lines; two
+// quads of 8 bytes that are neighbours themselves make one access of 16.
+template <class T, bool kInter>
 __device__ __forceinline__ int2 quads_of(int j, int R8, int pieces) {
-  return kInter ? make_int2(2 * j, 2 * j + 1) : j < R8 ? make_int2(j, j + R8) : make_int2(j + R8, j + pieces);
+  if (kInter && sizeof(typename T::Quad) == 8) return make_int2(2 * j, 2 * j + 1);
+  return j < R8 ? make_int2(j, j + R8) : make_int2(j + R8, j + pieces);
+}
+
+// Pair i of the four that a turned piece's quads hold.
+template <bool kInter>
+__device__ __forceinline__ int pair_of(int2 quads, int j, int i) {
+  return !kInter ? 4 * j + i : i < 2 ? 2 * quads.x + i : 2 * quads.y + i - 2;
 }
 
 template <bool kPastCaches, class Quad>
@@ -147,7 +155,7 @@ __device__ __forceinline__ void turn_rows_wide(const Rot& rot, const RowsArgs<T>
   const int R8 = rot.rdim / 8;
   const bool turned = j < R8;
   if (!turned && A.x == A.out) return;
-  const int2 qd = quads_of<kInter>(j, R8, A.per_head);
+  const int2 qd = quads_of<T, kInter>(j, R8, A.per_head);
   const int head0 = by * A.head_slots * kHeads + h0;
   const typename T::Elem* x = A.x + row * A.x_row;
   typename T::Elem* out = A.out + row * A.out_row;
@@ -165,7 +173,7 @@ __device__ __forceinline__ void turn_rows_wide(const Rot& rot, const RowsArgs<T>
     const int32_t pos = A.positions[row];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      cs[i] = rotary_cos_sin(rot.turn[4 * j + i], pos, rot.amplitude);
+      cs[i] = rotary_cos_sin(rot.turn[pair_of<kInter>(qd, j, i)], pos, rot.amplitude);
       if (A.backward) cs[i].y = -cs[i].y;
     }
   }
@@ -236,7 +244,7 @@ constexpr int64_t kMaxBlocks = int64_t(1) << 22;  // per launch: 2^30 threads
 template <class T>
 struct RowsPlan {
   RowsArgs<T> args;
-  bool wide, many, stream;
+  bool wide, many, lines, stream;
   int threads;
   // Blocks along x for `rows` rows, and the rows that n of them take.
   int64_t blocks(int64_t rows) const {
@@ -269,10 +277,15 @@ RowsPlan<T> plan_rows(const Rotary& r, const RotaryRows& a) {
   // and 177 with two, of 28 heads 125 (143, 123); but 1,024 rows of 28 heads 9.0 us against 8.6,
   // 16 rows 6.4 against 6.1, 40,960 rows of 8 heads 46 against 45 (cold caches, launch included).
   p.many = a.heads >= 16 && a.rows * a.heads * A.per_head >= int64_t(2560) * kThreads;
+  // Nothing goes past the caches where an instruction covers half lines (128 bytes), as half
+  // pairing of 64 16-bit channels does: 40,960 rows of 40 heads 168 us so, 151 through them.
+  p.lines = (r.pairing == LIBRA_ROTARY_INTERLEAVED && quad == 8) ||
+            r.rotary_dim / 2 * sizeof(typename T::Elem) % 128 == 0;
   // More than the last-level cache (256 MiB) would hold of both sides: the result goes past it
   // too.  Turned and then copied, 16,384 rows of 40 heads (160 MiB a side) take 111 us so, 125
   // through the caches, 40,960 rows 290 and 303; but 8,192 rows (80 MiB) 58 and 54.
-  p.stream = p.many && a.rows * a.heads * r.head_dim * int64_t(sizeof(typename T::Elem)) >= kStreamBytes;
+  p.stream = p.many && p.lines &&
+             a.rows * a.heads * r.head_dim * int64_t(sizeof(typename T::Elem)) >= kStreamBytes;
   const int per_thread = p.many ? 4 : 1;
   p.threads = kThreads;
   A.y_blocks = (a.heads + kNarrowHeads - 1) / kNarrowHeads;
@@ -306,7 +319,8 @@ hipError_t apply(const Rotary& r, const RotaryRows& a, hipStream_t s) {
       constexpr bool kInter = decltype(pairing)::value;
       return !p.many    ? rotary_wide_kernel<T, kInter, 1, kCached>
              : p.stream ? rotary_wide_kernel<T, kInter, 4, kReadsWrites>
-                        : rotary_wide_kernel<T, kInter, 4, kReads>;
+             : p.lines  ? rotary_wide_kernel<T, kInter, 4, kReads>
+                        : rotary_wide_kernel<T, kInter, 4, kCached>;
     };
     auto k = !p.wide ? rotary_narrow_kernel<T>
              : inter ? wide_form(std::true_type{})
@@ -370,7 +384,7 @@ __device__ __forceinline__ NewPiece load_piece(const WriteArgs& A, const Rot& ro
   NewPiece p;
   const uint16_t* k = A.k_new + row * A.k_row + g * kDim;
   if constexpr (kForm != kAnyPairs) {
-    const int2 qd = quads_of<kForm == kInterQuads>(j, rot.rdim / 8, kDim / 8);
+    const int2 qd = quads_of<Bf16, kForm == kInterQuads>(j, rot.rdim / 8, kDim / 8);
     p.a = *reinterpret_cast<const uint2*>(k + 4 * qd.x);
     p.b = *reinterpret_cast<const uint2*>(k + 4 * qd.y);
   }
@@ -417,12 +431,13 @@ __device__ __forceinline__ void store_key(const WriteArgs& A, const Rot& rot, co
         turn_any_granule(rot, A.k_new + row * A.k_row + g * kDim, j, p.pos, cs);
   } else {
     constexpr bool kInter = kForm == kInterQuads;
-    const int2 qd = quads_of<kInter>(j, rot.rdim / 8, kDim / 8);
+    const int2 qd = quads_of<Bf16, kInter>(j, rot.rdim / 8, kDim / 8);
     uint2 a = p.a, b = p.b;
     if (j < rot.rdim / 8) {
       float2 t[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) t[i] = rotary_cos_sin(rot.turn[4 * j + i], p.pos, rot.amplitude);
+      for (int i = 0; i < 4; ++i)
+        t[i] = rotary_cos_sin(rot.turn[pair_of<kInter>(qd, j, i)], p.pos, rot.amplitude);
       turn_quads<Bf16, kInter>(a, b, t);
     }
     *reinterpret_cast<uint2*>(tile + k_off(s, 4 * qd.x)) = a;
@@ -559,7 +574,7 @@ hipError_t launch_kv_append(const KvLayout& L, const NewRows& n, const int64_t* 
     q.args.y_blocks = hq;
   }
   // The cache's rows take their share of the caches too.
-  q.stream = q.many && rows * (hq + 2 * L.desc.num_kv_heads) * kDim * 2 >= kStreamBytes;
+  q.stream = q.many && q.lines && rows * (hq + 2 * L.desc.num_kv_heads) * kDim * 2 >= kStreamBytes;
   auto quads = [&](auto key_form) {
     constexpr int kForm = decltype(key_form)::value;
     return !q.many    ? kv_append_kernel<kForm, 1, kCached>
