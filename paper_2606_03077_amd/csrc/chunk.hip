@@ -46,6 +46,18 @@
 // ids and storing whole rows through LDS took 32 prompts of 64-2,048 tokens (40/8 heads) as
 // whole units from 893 us to 858 us on one card, cache write included; the narrow form takes
 // 857 us on them.
+//
+// Unturned queries (libra_append_attn_rotary): a wave turns its 32 rows in registers before the
+// first step, while the first copies land.  A turned query is not a bf16 number; it enters the
+// scores as hi + lo, the nearest bf16 and what that leaves, in 8 products more per page pair on
+// the K operands that are there anyway, since rounding it puts 2^-8 into every product: the
+// log-sum-exp of long rows is then off by 2-3e-5, of short ones by 1e-4, against 1e-7 so.
+// (lo in fp8 or fp6 would take a quarter or an eighth of the products' time, but leaves 2e-6 to
+// 4e-5.)  The lower products bound the kernel further by the matrix cores: 16,385-token prefill
+// (40/8 heads) 2.32 ms rounded, 3.08 ms with them (1.33 PFLOP/s of products, MFMA busy 71%, the
+// clock at 1.8 GHz), the prompts above 872 and 1,085 us, of which turning takes 70.  Orders of
+// the lower products (after the others, beside the PV products) and wave priorities as in the
+// narrow form are within 1% or slower.
 #include <cfloat>
 #include <cmath>
 #include <type_traits>

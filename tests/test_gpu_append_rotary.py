@@ -383,6 +383,31 @@ def test_launches_of_a_step():
     rope.close()
 
 
+def test_two_streams_share_plan_and_rotary():
+    """Calls of one plan and one rotary at once, on two streams, each with its own cache,
+    workspace and outputs."""
+    H.say("[case] append rotary two streams")
+    lens, news = [600, 1500, 300], [1, 200, 64]
+    a, b = (Step(lens, news, 8, 2, seed=70 + i, num_cus=32) for i in (0, 1))
+    rope = Handle(rdim=64)
+    want = [s.one_step(rope) for s in (a, b)]
+    for s in (a, b):
+        s.reset()
+    libra.libra_plan_destroy(b.plan)
+    b.plan, streams = a.plan, [torch.cuda.Stream() for _ in range(2)]
+    outs = [s.outputs() for s in (a, b)]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for s, o, st in zip((a, b), outs, streams):
+            s.call(rope, *o, stream=st)
+    torch.cuda.synchronize()
+    for s, o, w, label in zip((a, b), outs, want, "ab"):
+        same((*o, s.cache.k, s.cache.v), w, label)
+    rope.close()
+    b.cache.close()
+    a.close()
+
+
 def test_stale_nan_behind_the_last_token():
     """Slots behind a sequence's end hold NaN: nothing of them comes out."""
     H.say("[case] append rotary stale slots")
