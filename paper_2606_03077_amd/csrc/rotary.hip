@@ -415,6 +415,8 @@ __device__ __forceinline__ uint4 turn_any_granule(const Rot& rot, const uint16_t
   uint4 out[1], none[1];
   load_granules(in, row, gi, rot.rdim, rot.interleaved);
   turn_granules<1, false>(in, gi, cs, rot.rdim, rot.interleaved, out, none);
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
   return out[0];
 }
 
