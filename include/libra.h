@@ -514,8 +514,8 @@ libra_status libra_rotary_apply(libra_rotary rotary, int32_t dtype, const void* 
  * No plan is needed, so a captured call serves every later step whose slots and positions
  * are written to the same memory; libra_decode_attn reads what it wrote.
  *
- * k_new, v_new: device bf16, row r's heads at r * k_row_stride (v_row_stride) elements, 128
- * apart, so that slices of one projection can be given: strides >= num_kv_heads * 128 and
+ * k_new, v_new: device bf16, row r's num_kv_heads (the layout's) heads at r * k_row_stride
+ * (v_row_stride) elements, 128 apart, so that slices of one projection can be given: strides >= num_kv_heads * 128 and
  * multiples of 8, pointers 16-byte aligned.  rotary NULL: keys are written as they are and
  * positions is not read; else positions: device int32 [rows].
  * q (may be NULL, with q_out): device bf16 rows of num_q_heads heads at q_row_stride; turned
@@ -525,7 +525,8 @@ libra_status libra_kv_append(libra_kv_layout layout, libra_rotary rotary,
                              const int32_t* positions, const int64_t* slots, int64_t rows,
                              const void* q, int64_t q_row_stride, int32_t num_q_heads,
                              const void* k_new, int64_t k_row_stride, const void* v_new,
-                             int64_t v_row_stride, void* q_out, void* stream);
+                             int64_t v_row_stride, int32_t num_kv_heads, void* q_out,
+                             void* stream);
 
 /* libra_append_attn from unturned projections: keys are turned on their way into the cache
  * (to the bits libra_rotary_apply gives), queries where the attention kernels load them, and
@@ -545,9 +546,10 @@ libra_status libra_append_attn_rotary(libra_kv_layout layout, libra_plan plan,
                                       libra_rotary rotary, const int32_t* positions, int64_t rows,
                                       const void* q, int64_t q_row_stride, const void* k_new,
                                       int64_t k_row_stride, const void* v_new,
-                                      int64_t v_row_stride, const int32_t* block_table,
-                                      int32_t bt_stride, int32_t batch, int32_t num_q_heads,
-                                      float scale, int32_t round_queries, void* workspace,
+                                      int64_t v_row_stride, int32_t num_kv_heads,
+                                      const int32_t* block_table, int32_t bt_stride,
+                                      int32_t batch, int32_t num_q_heads, float scale,
+                                      int32_t round_queries, void* workspace,
                                       size_t ws_bytes, void* out, float* lse, void* stream);
 
 /* ------------------------------------------------------------------------------ */

@@ -110,9 +110,11 @@ libra_status check_rows(const void* p, int64_t rows, int64_t row, int64_t heads,
   return LIBRA_OK;
 }
 
-libra_status check_cached(const KvLayout& L, const Rotary& r) {
-  if (r.head_dim != L.desc.head_dim)
+libra_status check_cached(const KvLayout& L, const Rotary* r, int32_t num_kv_heads) {
+  if (r && r->head_dim != L.desc.head_dim)
     return set_error(LIBRA_E_INVAL, "rotary and layout disagree on head_dim");
+  if (num_kv_heads != L.desc.num_kv_heads)
+    return set_error(LIBRA_E_INVAL, "num_kv_heads differs from the layout's");
   return LIBRA_OK;
 }
 
@@ -189,22 +191,20 @@ libra_status libra_kv_append(libra_kv_layout layout, libra_rotary rotary,
                              const int32_t* positions, const int64_t* slots, int64_t rows,
                              const void* q, int64_t q_row_stride, int32_t num_q_heads,
                              const void* k_new, int64_t k_row_stride, const void* v_new,
-                             int64_t v_row_stride, void* q_out, void* stream) {
+                             int64_t v_row_stride, int32_t num_kv_heads, void* q_out,
+                             void* stream) {
   if (!layout) return set_error(LIBRA_E_INVAL, "layout is NULL");
   if (rows < 0) return set_error(LIBRA_E_INVAL, "rows < 0");
   if (rows > INT32_MAX) return set_error(LIBRA_E_UNSUPPORTED, "rows must be < 2^31");
   if (!q != !q_out) return set_error(LIBRA_E_INVAL, "q and q_out come together");
   if (q && !rotary) return set_error(LIBRA_E_INVAL, "q needs a rotary");
-  if (rotary) {
-    const libra_status st = check_cached(*layout, *rotary);
-    if (st != LIBRA_OK) return st;
-  }
+  libra_status st = check_cached(*layout, rotary, num_kv_heads);
+  if (st != LIBRA_OK) return st;
   if (rows == 0) return LIBRA_OK;
   if (!slots || (rotary && !positions))
     return set_error(LIBRA_E_INVAL, "slots or positions is NULL");
-  const int64_t hkv = layout->desc.num_kv_heads;
-  libra_status st = check_rows(k_new, rows, k_row_stride, hkv, "k_new");
-  if (st == LIBRA_OK) st = check_rows(v_new, rows, v_row_stride, hkv, "v_new");
+  st = check_rows(k_new, rows, k_row_stride, num_kv_heads, "k_new");
+  if (st == LIBRA_OK) st = check_rows(v_new, rows, v_row_stride, num_kv_heads, "v_new");
   if (st != LIBRA_OK) return st;
   if (q) {
     if (num_q_heads <= 0 || num_q_heads > 65535)
@@ -229,23 +229,23 @@ libra_status libra_append_attn_rotary(libra_kv_layout layout, libra_plan plan,
                                       libra_rotary rotary, const int32_t* positions, int64_t rows,
                                       const void* q, int64_t q_row_stride, const void* k_new,
                                       int64_t k_row_stride, const void* v_new,
-                                      int64_t v_row_stride, const int32_t* block_table,
-                                      int32_t bt_stride, int32_t batch, int32_t num_q_heads,
-                                      float scale, int32_t round_queries, void* workspace,
-                                      size_t ws_bytes, void* out, float* lse, void* stream) {
+                                      int64_t v_row_stride, int32_t num_kv_heads,
+                                      const int32_t* block_table, int32_t bt_stride,
+                                      int32_t batch, int32_t num_q_heads, float scale,
+                                      int32_t round_queries, void* workspace, size_t ws_bytes,
+                                      void* out, float* lse, void* stream) {
   libra_status st = check_call(layout, plan, LIBRA_MODE_APPEND, q, block_table, bt_stride, batch,
                                num_q_heads, scale, out);
   if (st != LIBRA_OK) return st;
   if (!rotary) return set_error(LIBRA_E_INVAL, "rotary is NULL");
-  st = check_cached(*layout, *rotary);
+  st = check_cached(*layout, rotary, num_kv_heads);
   if (st != LIBRA_OK) return st;
   if (rows != plan->info.n_rows)
     return set_error(LIBRA_E_INVAL, "rows differ from the plan's new tokens");
   if (rows > 0) {
-    const int64_t hkv = layout->desc.num_kv_heads;
     st = check_rows(q, rows, q_row_stride, num_q_heads, "q");
-    if (st == LIBRA_OK) st = check_rows(k_new, rows, k_row_stride, hkv, "k_new");
-    if (st == LIBRA_OK) st = check_rows(v_new, rows, v_row_stride, hkv, "v_new");
+    if (st == LIBRA_OK) st = check_rows(k_new, rows, k_row_stride, num_kv_heads, "k_new");
+    if (st == LIBRA_OK) st = check_rows(v_new, rows, v_row_stride, num_kv_heads, "v_new");
     if (st != LIBRA_OK) return st;
   }
   if (ws_bytes < plan->ws_bytes)

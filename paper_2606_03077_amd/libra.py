@@ -164,10 +164,11 @@ def load() -> ctypes.CDLL:
         "libra_rotary_get": (ctypes.c_int, [P, P, P, DP, DP]),
         "libra_rotary_apply": (ctypes.c_int, [P, I32, P, I64, I64, P, I64, I32, I32, I32, P, I64,
                                               I64, P]),
-        "libra_kv_append": (ctypes.c_int, [P, P, P, P, I64, P, I64, I32, P, I64, P, I64, P, P]),
-        "libra_append_attn_rotary": (ctypes.c_int, [P, P, P, P, I64, P, I64, P, I64, P, I64, P, I32,
-                                                    I32, I32, ctypes.c_float, I32, P, SZ, P, P,
-                                                    P]),
+        "libra_kv_append": (ctypes.c_int, [P, P, P, P, I64, P, I64, I32, P, I64, P, I64, I32, P,
+                                           P]),
+        "libra_append_attn_rotary": (ctypes.c_int, [P, P, P, P, I64, P, I64, P, I64, P, I64, I32, P,
+                                                    I32, I32, I32, ctypes.c_float, I32, P, SZ, P,
+                                                    P, P]),
         "libra_profile_enable": (ctypes.c_int, [ctypes.c_int]),
         "libra_profile_collect": (ctypes.c_int, [ctypes.POINTER(KernelTimes)]),
         "libra_ce_fit": (ctypes.c_int, [DP, DP, I32, ctypes.POINTER(CePoly)]),
@@ -244,10 +245,11 @@ def _run_ptr(t) -> Optional[int]:
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
-def _stream(stream) -> Optional[int]:
+def _stream(stream, device: Optional[int] = None) -> Optional[int]:
+    """The handle of stream, or of the current one (of the current device, if it is known)."""
     if stream is None:
         if _raw_stream is not None:
-            return _raw_stream(torch.cuda.current_device())
+            return _raw_stream(torch.cuda.current_device() if device is None else device)
         return torch.cuda.current_stream().cuda_stream
     if isinstance(stream, torch.cuda.Stream):
         return stream.cuda_stream
@@ -465,21 +467,24 @@ def libra_rotary_get(rotary: int) -> dict:
     return {"head_dim": dims[0], "rotary_dim": dims[1], "frequencies": f, "amplitude": a.value}
 
 
-def _vector(t, dtype, n: int, what: str) -> Optional[int]:
-    """A contiguous device vector of n elements."""
+def _vector(t, dtype, n: int, what: str, device: int) -> Optional[int]:
+    """A contiguous vector of n elements on the current device."""
     if t is None:
         return None
-    if not t.is_cuda or t.dtype is not dtype or not t.is_contiguous() or t.numel() != n:
-        raise ValueError(f"{what}: contiguous {dtype} device tensor of {n} elements expected")
+    if t.get_device() != device or t.dtype is not dtype or not t.is_contiguous() or t.numel() != n:
+        raise ValueError(f"{what}: contiguous {dtype} tensor of {n} elements on the current "
+                         "device expected")
     return t.data_ptr()
 
 
-def _rows(t, rows: int, heads: Optional[int], what: str):
-    """(pointer, row stride, heads) of a projection's bf16 rows [rows, heads, 128], 128 apart."""
+def _rows(t, rows: int, heads: Optional[int], what: str, device: int):
+    """(pointer, row stride, heads) of a projection's bf16 rows [rows, heads, 128], 128 apart,
+    on the current device."""
     if t is None:
         return None, 0, 0
-    if not t.is_cuda or t.dtype not in _BF16_BITS or t.dim() != 3:
-        raise ValueError(f"{what}: [rows, heads, {HEAD_DIM}] bf16 device tensor expected")
+    if t.get_device() != device or t.dtype not in _BF16_BITS or t.dim() != 3:
+        raise ValueError(f"{what}: [rows, heads, {HEAD_DIM}] bf16 tensor on the current device "
+                         "expected")
     n, h, d = t.shape
     if n != rows or d != HEAD_DIM or (heads is not None and h != heads):
         raise ValueError(f"{what}: [{rows}, {heads or 'heads'}, {HEAD_DIM}] expected")
@@ -493,8 +498,10 @@ def libra_rotary_apply(rotary: int, x, positions, out, backward: bool = False, s
     """Turns x [rows, heads, head_dim] (bf16, fp16 or fp32; any row and head strides) by
     positions [rows] (int32) into out, of the same shape and type, which may be x."""
     dtype = _ROTARY_DTYPES.get(x.dtype)
-    if dtype is None or not x.is_cuda or x.dim() != 3:
-        raise ValueError("[rows, heads, head_dim] bf16, fp16 or fp32 device tensor expected")
+    device = torch.cuda.current_device()
+    if dtype is None or x.get_device() != device or x.dim() != 3:
+        raise ValueError("[rows, heads, head_dim] bf16, fp16 or fp32 tensor on the current device "
+                         "expected")
     if out.dtype is not x.dtype or out.shape != x.shape or out.device != x.device:
         raise ValueError("out must be of x's shape, type and device")
     rows, heads, dim = x.shape
@@ -502,9 +509,9 @@ def libra_rotary_apply(rotary: int, x, positions, out, backward: bool = False, s
     if dim > 1 and (xd != 1 or outd != 1):
         raise ValueError("the channels of a head must be contiguous")
     _check(load().libra_rotary_apply(rotary, dtype, x.data_ptr(), xr, xh,
-                                     _vector(positions, torch.int32, rows, "positions"), rows,
-                                     heads, dim, 1 if backward else 0, out.data_ptr(), outr,
-                                     outh, _stream(stream)), "libra_rotary_apply")
+                                     _vector(positions, torch.int32, rows, "positions", device),
+                                     rows, heads, dim, 1 if backward else 0, out.data_ptr(), outr,
+                                     outh, _stream(stream, device)), "libra_rotary_apply")
 
 
 def libra_kv_append(layout: int, rotary: Optional[int], positions, slots, q, k_new, v_new, q_out,
@@ -512,18 +519,20 @@ def libra_kv_append(layout: int, rotary: Optional[int], positions, slots, q, k_n
     """Writes k_new (turned) and v_new [rows, Hkv, 128] to slots [rows] (int64; outside the
     cache: padding), and q [rows, Hq, 128] turned to q_out.  Rows may be slices of one
     projection.  rotary None: keys as they are; q and q_out may be None."""
+    device = torch.cuda.current_device()
     rows = slots.numel()
-    qp, qs, hq = _rows(q, rows, None, "q")
-    kp, ks, hkv = _rows(k_new, rows, None, "k_new")
-    vp, vs, _ = _rows(v_new, rows, hkv, "v_new")
+    qp, qs, hq = _rows(q, rows, None, "q", device)
+    kp, ks, hkv = _rows(k_new, rows, None, "k_new", device)
+    vp, vs, _ = _rows(v_new, rows, hkv, "v_new", device)
     qo = None
     if q_out is not None:
-        qo, stride, _ = _rows(q_out, rows, hq, "q_out")
+        qo, stride, _ = _rows(q_out, rows, hq, "q_out", device)
         if stride != hq * HEAD_DIM:
             raise ValueError("q_out: dense rows expected")
-    _check(load().libra_kv_append(layout, rotary, _vector(positions, torch.int32, rows, "positions"),
-                                  _vector(slots, torch.int64, rows, "slots"), rows, qp, qs, hq, kp,
-                                  ks, vp, vs, qo, _stream(stream)), "libra_kv_append")
+    _check(load().libra_kv_append(layout, rotary,
+                                  _vector(positions, torch.int32, rows, "positions", device),
+                                  _vector(slots, torch.int64, rows, "slots", device), rows, qp, qs,
+                                  hq, kp, ks, vp, vs, hkv, qo, _stream(stream, device)), "libra_kv_append")
 
 
 def libra_append_attn_rotary(layout: int, plan: int, rotary: int, positions, q, k_new, v_new,
@@ -534,16 +543,18 @@ def libra_append_attn_rotary(layout: int, plan: int, rotary: int, positions, q, 
     positions [rows] (int32), or None for each token's index in its cache.  round_queries:
     turned queries as bf16, as from libra_rotary_apply, instead of in 16 bits."""
     ws_bytes = workspace.numel() * workspace.element_size()
+    device = torch.cuda.current_device()
     rows = q.shape[0]
-    qp, qs, _ = _rows(q, rows, num_q_heads, "q")
-    kp, ks, hkv = _rows(k_new, rows, None, "k_new")
-    vp, vs, _ = _rows(v_new, rows, hkv, "v_new")
+    qp, qs, _ = _rows(q, rows, num_q_heads, "q", device)
+    kp, ks, hkv = _rows(k_new, rows, None, "k_new", device)
+    vp, vs, _ = _rows(v_new, rows, hkv, "v_new", device)
     _check(load().libra_append_attn_rotary(layout, plan, rotary,
-                                           _vector(positions, torch.int32, rows, "positions"),
-                                           rows, qp, qs, kp, ks, vp, vs, _ptr(block_table),
-                                           bt_stride, batch, num_q_heads, scale,
+                                           _vector(positions, torch.int32, rows, "positions",
+                                                   device),
+                                           rows, qp, qs, kp, ks, vp, vs, hkv,
+                                           _ptr(block_table), bt_stride, batch, num_q_heads, scale,
                                            1 if round_queries else 0, _ptr(workspace), ws_bytes,
-                                           _ptr(out), _ptr(lse), _stream(stream)),
+                                           _ptr(out), _ptr(lse), _stream(stream, device)),
            "libra_append_attn_rotary")
 
 

@@ -96,11 +96,11 @@ int main() {
   for (int i = 0; i < 3; ++i) {
     CHECK(libra_rotary_apply(rot, LIBRA_DTYPE_FP32, p, 1024, 128, i32, rows, hq, 128, i & 1, p, 1024, 128,
                              nullptr) == LIBRA_OK);
-    CHECK(libra_kv_append(lay, rot, i32, i64, rows, p, 1536, hq, p, 1536, p, 1536, p, nullptr) ==
+    CHECK(libra_kv_append(lay, rot, i32, i64, rows, p, 1536, hq, p, 1536, p, 1536, hkv, p, nullptr) ==
           LIBRA_E_INVAL);  // in place, but q's rows are not dense
-    CHECK(libra_kv_append(lay, rot, i32, i64, rows, p, 1024, hq, p, 1536, p, 1536, p, nullptr) ==
+    CHECK(libra_kv_append(lay, rot, i32, i64, rows, p, 1024, hq, p, 1536, p, 1536, hkv, p, nullptr) ==
           LIBRA_OK);
-    CHECK(libra_append_attn_rotary(lay, plan, rot, nullptr, rows, p, 1536, p, 1536, p, 1536, i32, 200, B,
+    CHECK(libra_append_attn_rotary(lay, plan, rot, nullptr, rows, p, 1536, p, 1536, p, 1536, hkv, i32, 200, B,
                                    hq, 0.1f, i & 1, ws, ws_bytes, p, nullptr, nullptr) == LIBRA_OK);
     if (i == 0) copies = g_fake_hip.memcpy_async;
   }

@@ -200,9 +200,40 @@ def test_rows_of_several_launches():
     at = first * hkv * 128 * 2                              # the rows before are never read
     status = libra.load().libra_kv_append(
         cache.layout, rope.h, pd.data_ptr(), sd.data_ptr(), rows, None, 0, 0, k.data_ptr() - at,
-        hkv * 128, v.data_ptr() - at, hkv * 128, None, torch.cuda.current_stream().cuda_stream)
+        hkv * 128, v.data_ptr() - at, hkv * 128, hkv, None, torch.cuda.current_stream().cuda_stream)
     assert status == 0
     check_cache(cache, rope, slots[first:first + 71], pos[first:first + 71], k, v, "launches")
+    rope.close()
+    cache.close()
+
+
+def test_refusals_of_the_binding(monkeypatch):
+    """Wrong heads in rows far enough apart to pass by their stride, lengths, and a device that is
+    not the current one; the cache stays as it was."""
+    hkv, rows = 2, 4
+    cache, rope = Cache(3, hkv), Handle()
+    saved = cache.k.clone(), cache.v.clone()
+    qkv = randn((rows, 10, 128), BF16, 31)
+    pos = torch.arange(rows, dtype=torch.int32, device="cuda")
+    slots = pos.long()
+
+    def call(q=qkv[:, :4], k=qkv[:, 4:6], v=qkv[:, 6:8], q_out=None, p=pos, s=slots):
+        libra.libra_kv_append(cache.layout, rope.h, p, s, q, k, v,
+                              torch.empty(rows, 4, 128, dtype=BF16, device="cuda") if q_out is None else q_out)
+
+    for bad in (dict(k=qkv[:, 4:5], v=qkv[:, 6:7]), dict(k=qkv[:, 4:7], v=qkv[:, 7:10]),
+                dict(v=qkv[:, 6:7]), dict(k=qkv[:3, 4:6]), dict(q=qkv[:3, :4]), dict(p=pos[:3]),
+                dict(s=slots[:3]), dict(p=slots), dict(s=pos), dict(k=qkv[:, 4:6, :64]),
+                dict(q_out=qkv[:, 6:10]), dict(q_out=qkv[:, 6:8].contiguous()),
+                dict(k=qkv[:, 4:8:2]), dict(v=qkv[:, 6:8].cpu())):
+        with pytest.raises((ValueError, libra.LibraError)):
+            call(**bad)
+    with monkeypatch.context() as m:
+        m.setattr(torch.cuda, "current_device", lambda: 1)
+        with pytest.raises(ValueError, match="current device"):
+            call()
+    torch.cuda.synchronize()
+    assert torch.equal(cache.k, saved[0]) and torch.equal(cache.v, saved[1])
     rope.close()
     cache.close()
 

@@ -7,6 +7,7 @@ import subprocess
 
 import numpy as np
 import pytest
+import torch
 
 from oracle import rotary as ref
 from paper_2606_03077_amd import libra
@@ -129,12 +130,13 @@ def _layout(hkv=2):
     return libra.libra_kv_layout_create(P, P, 10, hkv)
 
 
-def _append(layout, h, pos=P, slots=P, rows=3, q=None, qr=0, hq=0, k=P, kr=256, v=P, vr=256, q_out=None):
-    return _raw("libra_kv_append", layout, h, pos, slots, rows, q, qr, hq, k, kr, v, vr, q_out, None)
+def _append(layout, h, pos=P, slots=P, rows=3, q=None, qr=0, hq=0, k=P, kr=256, v=P, vr=256, hkv=2, q_out=None):
+    return _raw("libra_kv_append", layout, h, pos, slots, rows, q, qr, hq, k, kr, v, vr, hkv, q_out, None)
 
 
 @pytest.mark.parametrize("kw,status", [
     (dict(rows=-1), INVAL), (dict(rows=2 ** 31), UNSUPPORTED), (dict(slots=None), INVAL),
+    (dict(hkv=1), INVAL), (dict(hkv=4, kr=512, vr=512), INVAL),
     (dict(pos=None), INVAL), (dict(k=None), INVAL), (dict(v=None), INVAL), (dict(k=P + 8), INVAL),
     (dict(v=P + 2), INVAL), (dict(kr=255), INVAL), (dict(kr=248), INVAL), (dict(vr=0), INVAL),
     (dict(vr=-256), INVAL), (dict(vr=2 ** 60), INVAL), (dict(q=P, qr=512, hq=4), INVAL),
@@ -165,9 +167,9 @@ def test_refused_append_attn(rotary):
     other = libra.libra_rotary_create(head_dim=64)
 
     def call(plan=plan, h=rotary, pos=None, rows=4, q=P, qr=512, k=P, kr=256, v=P, vr=256, bt=P, stride=2,
-             batch=2, hq=4, scale=0.1, ws=P, n=1 << 30, out=P):
-        return _raw("libra_append_attn_rotary", lay, plan, h, pos, rows, q, qr, k, kr, v, vr, bt, stride,
-                    batch, hq, scale, 0, ws, n, out, None, None)
+             batch=2, hq=4, hkv=2, scale=0.1, ws=P, n=1 << 30, out=P):
+        return _raw("libra_append_attn_rotary", lay, plan, h, pos, rows, q, qr, k, kr, v, vr, hkv, bt,
+                    stride, batch, hq, scale, 0, ws, n, out, None, None)
 
     for kw, status in [(dict(plan=decode), INVAL), (dict(plan=None), INVAL), (dict(h=None), INVAL),
                        (dict(h=other), INVAL), (dict(rows=3), INVAL), (dict(rows=0), INVAL),
@@ -175,13 +177,28 @@ def test_refused_append_attn(rotary):
                        (dict(qr=511), INVAL), (dict(qr=256), INVAL), (dict(k=None), INVAL),
                        (dict(kr=128), INVAL), (dict(v=P + 4), INVAL), (dict(vr=300), INVAL),
                        (dict(bt=None), INVAL), (dict(stride=1), INVAL), (dict(batch=1), INVAL),
-                       (dict(hq=8), INVAL), (dict(scale=0.0), INVAL), (dict(scale=float("nan")), INVAL),
+                       (dict(hq=8), INVAL), (dict(hkv=1), INVAL), (dict(hkv=4, kr=512, vr=512), INVAL), (dict(scale=0.0), INVAL), (dict(scale=float("nan")), INVAL),
                        (dict(ws=None), INVAL), (dict(ws=P + 16), INVAL), (dict(n=16), WORKSPACE),
                        (dict(out=P + 2), INVAL), (dict(out=None), INVAL)]:
         assert call(**kw) == status, (kw, libra.libra_last_error())
     libra.libra_rotary_destroy(other)
     libra.libra_plan_destroy(decode)
     libra.libra_plan_destroy(plan)
+    libra.libra_kv_layout_destroy(lay)
+
+
+def test_tensors_of_another_device_are_refused(rotary, monkeypatch):
+    """The binding refuses what does not lie on the current device, before the library is called."""
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(libra, "_stream", lambda *a: None)
+    x, pos = torch.zeros(3, 2, 128, dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int32)
+    lay = _layout()
+    for bad in (lambda: libra.libra_rotary_apply(rotary, x, pos, x),
+                lambda: libra.libra_kv_append(lay, rotary, pos, pos.long(), None, x, x, None),
+                lambda: libra.libra_append_attn_rotary(lay, None, rotary, pos, x, x, x, pos, 1, 1, 2,
+                                                       0.1, pos, x)):
+        with pytest.raises(ValueError, match="current device"):
+            bad()
     libra.libra_kv_layout_destroy(lay)
 
 
