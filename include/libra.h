@@ -459,7 +459,8 @@ libra_status libra_append_attn(libra_kv_layout layout, libra_plan plan, const vo
  *                        frequency, those with fewer than `slow` are interpolated.
  *
  * Frequencies are taken in extended precision and angles kept modulo one turn in 64-bit
- * fixed point, so the angle of a position of 2^31 is still good to 1e-9 turns.  Cosine and
+ * fixed point, so the angle of a position of 2^31 is still good to 1e-9 turns (where
+ * theta_j > 1 is not given but computed, or given and scaled: to theta_j times that).  Cosine and
  * sine are float32 (within 1.2e-7 of the exact ones, times A), the products too, and the
  * result is rounded once to the output's type.
  */

@@ -6,6 +6,7 @@
 
 #include "calls.h"
 #include "rotary_calls.h"
+#include "turns.h"
 
 using namespace libra;
 
@@ -17,14 +18,6 @@ constexpr long double kTwoPi = 6.283185307179586476925286766559005768L;
 constexpr int64_t kMaxOffset = int64_t(1) << 56;  // elements
 
 bool positive(double x) { return std::isfinite(x) && x > 0; }
-
-// theta / 2 pi mod 1 in units of 2^-64 (nearest).
-uint64_t turns(long double theta) {
-  long double t = theta / kTwoPi;
-  t -= std::floor(t);
-  t = std::round(t * 18446744073709551616.0L);
-  return t >= 18446744073709551616.0L ? 0 : uint64_t(t);
-}
 
 libra_status fill(const libra_rotary_desc& d, Rotary* r) {
   if (d.head_dim < 2 || d.head_dim > kMaxRotaryHead)
@@ -80,7 +73,7 @@ libra_status fill(const libra_rotary_desc& d, Rotary* r) {
     if (!(std::fabs(th) <= 1e6L))
       return set_error(LIBRA_E_INVAL, "a frequency is not finite or beyond 1e6 radians");
     r->theta[j] = double(th);
-    r->turn[j] = turns(th);
+    r->turn[j] = rotary_turns(th);
   }
   return LIBRA_OK;
 }

@@ -8,7 +8,8 @@
 //
 // Angles are kept in turns, as 64-bit fixed point: turn_j = theta_j / 2 pi mod 1 in units of
 // 2^-64, and p turn_j mod 2^64 is the angle mod one turn, exact but for turn_j's own rounding
-// (p 2^-65 turns), whatever the position; float32 angles lose 2^-24 p theta.  The fraction's
+// (p 2^-65 turns), whatever the position and the frequency; float32 angles lose 2^-24 p theta.
+// theta_j itself is a given double, or computed in long double (64 bits).  The fraction's
 // top 32 bits give the quadrant and an angle in [-pi / 4, pi / 4] for the sine's and cosine's
 // Taylor polynomials (truncated below 2e-9; with float32 rounding within 1.2e-7).
 #pragma once
