@@ -22,7 +22,8 @@
 //
 // Unturned queries (libra_append_attn_rotary): the workgroup turns its heads through LDS first.
 // A turned query is the sum of two bf16 parts: of at most 8 heads, the parts are two halves of
-// the products' 16 columns, so the scores take no product more, and one cross-lane add.  Where
+// the products' 16 columns, so the scores take no product more, and one cross-lane add.  Rounded
+// to bf16 it is the plain operand.  Where
 // a unit ends with its row's new token, it writes the token to the cache too, which saves a
 // step of single rows its write launch (3-5 us of 19 for 8 short rows, of 104 for 64 long ones).
 #include <cmath>
@@ -208,11 +209,11 @@ struct DecodeRotaryArgs : DecodeArgs {
   const uint16_t* k_new;
   const uint16_t* v_new;
   int64_t k_row, v_row;
-  int round_queries;
 };
 
-// Turned rows in LDS, 16 granules each.  kPaired: the heads' upper parts, and from kNewRow on
-// the new token's key and value; the heads' lower parts are further rows.
+// Turned rows in LDS, 16 granules each: the heads' upper parts (all there is of rounded queries),
+// of at most 8 heads, and from kNewRow on the new token's key and value; the heads' lower parts
+// are further rows.
 struct TurnedRows {
   float2 cs[kRotaryPairs];
   uint4 hi[16][kDim / 8], lo[16][kDim / 8];
@@ -239,13 +240,13 @@ __device__ __forceinline__ void patch_page(PageRegs& r, const TurnedRows& n, int
   }
 }
 
-// How queries enter the scores: as they are, or turned, as two parts.
-enum QueryForm : int { kPlain, kPaired, kSplit };
+// How queries enter the scores: as they are, turned and rounded to bf16, or turned as two parts.
+enum QueryForm : int { kPlain, kRounded, kPaired, kSplit };
 
 template <int kForm>
 __global__ __launch_bounds__(kThreads) __attribute__((amdgpu_waves_per_eu(LIBRA_DECODE_WAVES_PER_EU, 8)))
 void decode_kernel(std::conditional_t<kForm == kPlain, DecodeArgs, DecodeRotaryArgs> A) {
-  constexpr bool kRotary = kForm != kPlain;
+  constexpr bool kRotary = kForm != kPlain, kTwoParts = kForm == kPaired || kForm == kSplit;
   __shared__ float red_m[kWaves][16];
   __shared__ float red_l[kWaves][16];
   __shared__ __align__(16) float red_o[kWaves][16][kRedStride];
@@ -273,7 +274,7 @@ void decode_kernel(std::conditional_t<kForm == kPlain, DecodeArgs, DecodeRotaryA
     static_assert(sizeof(TurnedRows) <= sizeof(red_o), "turned rows lie in the waves' exchange");
     TurnedRows& rows = *reinterpret_cast<TurnedRows*>(&red_o[0][0][0]);
     const int prior = u[U_PRIOR], rdim = A.rot.rdim, inter = A.rot.interleaved;
-    const bool owner = kForm == kPaired && A.k_new && kv1 == prior + 1;
+    const bool owner = kForm != kSplit && A.k_new && kv1 == prior + 1;
     const int h = tid >> 4, gi[1] = {tid & 15};
     const bool is_k = owner && h == kNewRow, is_v = owner && h == kNewRow + 1;
     const uint16_t* src = is_k   ? A.k_new + size_t(row) * A.k_row + size_t(g) * kDim
@@ -287,10 +288,10 @@ void decode_kernel(std::conditional_t<kForm == kPlain, DecodeArgs, DecodeRotaryA
     }
     __syncthreads();
     uint4 hi[1], lo[1];
-    turn_granules<1, true>(in, gi, rows.cs, is_v ? 0 : rdim, inter, hi, lo);
+    turn_granules<1, kTwoParts>(in, gi, rows.cs, is_v ? 0 : rdim, inter, hi, lo);
     const bool unused = h >= G && !is_k && !is_v;
     rows.hi[h][gi[0]] = unused ? make_uint4(0, 0, 0, 0) : hi[0];
-    rows.lo[h][gi[0]] = unused || A.round_queries ? make_uint4(0, 0, 0, 0) : lo[0];
+    if constexpr (kTwoParts) rows.lo[h][gi[0]] = unused ? make_uint4(0, 0, 0, 0) : lo[0];
     if (is_k || is_v) {
       const size_t page = size_t(A.bt[int64_t(b) * A.bt_stride + prior / kPage]);
       const size_t tile = (page * A.hkv + g) * kTileElems;
@@ -311,6 +312,8 @@ void decode_kernel(std::conditional_t<kForm == kPlain, DecodeArgs, DecodeRotaryA
     for (int i = 0; i < 4; ++i) {
       if constexpr (kForm == kPaired) {
         qop.part[i] = as_bf16x8((col < 8 ? rows.hi : rows.lo)[col & 7][4 * i + quad]);
+      } else if constexpr (kForm == kRounded) {
+        qop[i] = as_bf16x8(col < G ? rows.hi[col][4 * i + quad] : make_uint4(0, 0, 0, 0));
       } else {
         qop.hi[i] = as_bf16x8(rows.hi[col][4 * i + quad]);
         qop.lo[i] = as_bf16x8(rows.lo[col][4 * i + quad]);
@@ -361,7 +364,7 @@ void decode_kernel(std::conditional_t<kForm == kPlain, DecodeArgs, DecodeRotaryA
     auto consume = [&](PageRegs& r, int k) {
       const int valid = min(kPage, kv1 - (w0 + k) * kPage);
       if (valid < kPage) clear_v_slots(r, quad, valid);
-      if constexpr (kForm == kPaired) {
+      if constexpr (kForm == kRounded || kForm == kPaired) {
         if (new_slot >= 0 && k == nw - 1)
           patch_page(r, *reinterpret_cast<const TurnedRows*>(&red_o[0][0][0]), new_slot, lane);
       }
@@ -525,8 +528,9 @@ hipError_t launch_decode_rotary(const KvLayout& L, const Plan& P, void* ws, cons
   A.v_new = static_cast<const uint16_t*>(n.v);
   A.k_row = n.k_row;
   A.v_row = n.v_row;
-  A.round_queries = n.round_queries;
-  auto k = P.group <= 8 ? decode_kernel<kPaired> : decode_kernel<kSplit>;
+  auto k = n.round_queries ? decode_kernel<kRounded>
+           : P.group <= 8  ? decode_kernel<kPaired>
+                           : decode_kernel<kSplit>;
   hipLaunchKernelGGL(k, dim3(unsigned(units)), dim3(kThreads), 0, s, A);
   return hipGetLastError();
 }
