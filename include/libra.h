@@ -540,8 +540,10 @@ libra_status libra_kv_append(libra_kv_layout layout, libra_rotary rotary,
  * libra_kv_append, rows = sum C_b of them in libra_append_attn's order.
  * positions: device int32 [rows], or NULL for each token's index in its sequence's cache
  * (P_b + i); positions need not follow the index, as where part of a context has been
- * dropped, but the causal order is the cache's.  A key that a row sees must be finite (an
- * infinite channel makes the row NaN); what lies behind a sequence's end may be anything.
+ * dropped, but the causal order is the cache's.  What lies behind a sequence's end may be
+ * anything.  A key with an infinite channel gives a row that sees it what it gives the unrounded
+ * query, or makes the row NaN with lse -inf (the parts differ in sign, or one is 0); rounded
+ * queries give over such keys, too, what the two calls give.
  * Plans, workspaces, streams and graph capture are as for libra_append_attn. */
 libra_status libra_append_attn_rotary(libra_kv_layout layout, libra_plan plan,
                                       libra_rotary rotary, const int32_t* positions, int64_t rows,

@@ -450,7 +450,20 @@ void decode_kernel(std::conditional_t<kForm == kPlain, DecodeArgs, DecodeRotaryA
     for (int w = 0; w < kWaves; ++w) s += red_o[w][hcol][c8 + i];
     o[i] = Lh > 0.f ? s / Lh : 0.f;
   }
-  const float lse2 = Lh > 0.f ? Mh + log2f(Lh) : -INFINITY;
+  float lse2 = Lh > 0.f ? Mh + log2f(Lh) : -INFINITY;
+  if constexpr (kTwoParts) {
+    // An infinite key channel can meet the parts as 0 x inf or inf - inf.  Maxima ignore such a
+    // score, a wave's sum does not; the row is NaN then, its LSE -inf.  A split's LSE is +inf,
+    // whose weight against any maximum, its own or a finite one, makes the merged row the same.
+    bool none = false;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) none |= __builtin_isnan(red_l[w][hcol]);
+    if (none) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[i] = __builtin_nanf("");
+      lse2 = nsplit == 1 ? -INFINITY : INFINITY;
+    }
+  }
   const size_t head = size_t(g) * G + hcol;
 
   if (nsplit == 1) {
