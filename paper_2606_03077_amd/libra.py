@@ -431,6 +431,7 @@ def libra_append_attn(layout: int, plan: int, q, k_new, v_new, block_table, bt_s
 _ROTARY_DTYPES = {torch.bfloat16: LIBRA_DTYPE_BF16, torch.float16: LIBRA_DTYPE_FP16,
                   torch.float32: LIBRA_DTYPE_FP32}
 _BF16_BITS = (torch.bfloat16, torch.int16)
+_INT32, _FLOAT32 = (torch.int32,), (torch.float32,)
 
 
 def libra_rotary_create(head_dim: int = HEAD_DIM, rotary_dim: int = 0,
@@ -474,6 +475,19 @@ def _vector(t, dtype, n: int, what: str, device: int) -> Optional[int]:
     if t.get_device() != device or t.dtype is not dtype or not t.is_contiguous() or t.numel() != n:
         raise ValueError(f"{what}: contiguous {dtype} tensor of {n} elements on the current "
                          "device expected")
+    return t.data_ptr()
+
+
+def _buffer(t, dtypes, n: int, what: str, device: int) -> Optional[int]:
+    """A contiguous buffer of at least n elements on the current device (any type if dtypes is
+    None), or an address as it is."""
+    if not isinstance(t, torch.Tensor):
+        return None if t is None else int(t)
+    if (t.get_device() != device or (dtypes is not None and t.dtype not in dtypes)
+            or not t.is_contiguous() or t.numel() < n):
+        kind = "" if dtypes is None else f"{dtypes[0]} "
+        raise ValueError(f"{what}: contiguous {kind}tensor of {n} elements on the current device "
+                         "expected")
     return t.data_ptr()
 
 
@@ -541,7 +555,8 @@ def libra_append_attn_rotary(layout: int, plan: int, rotary: int, positions, q, 
                              round_queries: bool = False):
     """libra_append_attn from unturned projections, whose rows may be slices of one tensor;
     positions [rows] (int32), or None for each token's index in its cache.  round_queries:
-    turned queries as bf16, as from libra_rotary_apply, instead of in 16 bits."""
+    turned queries as bf16, as from libra_rotary_apply, instead of in 16 bits.  block_table: int32
+    [batch, bt_stride]; out: [rows, num_q_heads, 128] bf16; lse: float32 [rows, num_q_heads]."""
     ws_bytes = workspace.numel() * workspace.element_size()
     device = torch.cuda.current_device()
     rows = q.shape[0]
@@ -552,10 +567,15 @@ def libra_append_attn_rotary(layout: int, plan: int, rotary: int, positions, q, 
                                            _vector(positions, torch.int32, rows, "positions",
                                                    device),
                                            rows, qp, qs, kp, ks, vp, vs, hkv,
-                                           _ptr(block_table), bt_stride, batch, num_q_heads, scale,
-                                           1 if round_queries else 0, _ptr(workspace), ws_bytes,
-                                           _ptr(out), _ptr(lse), _stream(stream, device)),
-           "libra_append_attn_rotary")
+                                           _buffer(block_table, _INT32, batch * bt_stride,
+                                                   "block_table", device),
+                                           bt_stride, batch, num_q_heads, scale,
+                                           1 if round_queries else 0,
+                                           _buffer(workspace, None, 0, "workspace", device), ws_bytes,
+                                           _buffer(out, _BF16_BITS, rows * num_q_heads * HEAD_DIM,
+                                                   "out", device),
+                                           _buffer(lse, _FLOAT32, rows * num_q_heads, "lse", device),
+                                           _stream(stream, device)), "libra_append_attn_rotary")
 
 
 def libra_profile_enable(enable: bool = True) -> None:
