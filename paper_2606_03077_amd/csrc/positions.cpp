@@ -85,7 +85,14 @@ bool disjoint(int64_t rows, int64_t heads, int64_t n, int64_t row, int64_t head)
   if (rows > 1 && row < n) return false;
   if (heads > 1 && head < n) return false;
   if (rows == 1 || heads == 1) return true;
-  return row >= (heads - 1) * head + n || head >= (rows - 1) * row + n;
+  if (row >= (heads - 1) * head + n || head >= (rows - 1) * row + n) return true;
+  // Vectors (r, h + j) and (r + i, h) lie j head - i row apart; the nearest to j head are two.
+  for (int64_t j = 1; j < heads; ++j) {
+    const int64_t i = j * head / row;
+    if (i >= 1 && i < rows && j * head - i * row < n) return false;
+    if (i + 1 < rows && (i + 1) * row - j * head < n) return false;
+  }
+  return true;
 }
 
 // Whether an element's offset stays well inside 64 bits of bytes.
