@@ -38,10 +38,7 @@ namespace {
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-#ifndef LIBRA_DECODE_WAVES
-#define LIBRA_DECODE_WAVES 4
-#endif
-constexpr int kWaves = LIBRA_DECODE_WAVES;
+constexpr int kWaves = 4;
 constexpr int kThreads = 64 * kWaves;
 #ifndef LIBRA_DECODE_DEPTH
 #define LIBRA_DECODE_DEPTH 2
@@ -271,6 +268,7 @@ void decode_kernel(std::conditional_t<kForm == kPlain, DecodeArgs, DecodeRotaryA
     // Where the unit ends with the new token, the same pass turns its key, stores key and value
     // to the cache, and keeps them for the last wave, which alone reads that page for this head:
     // the page as loaded may or may not have them, and to wait for the stores takes longer.
+    static_assert(kThreads == 256, "a thread turns one of 16 granules of one of 16 rows");
     static_assert(sizeof(TurnedRows) <= sizeof(red_o), "turned rows lie in the waves' exchange");
     TurnedRows& rows = *reinterpret_cast<TurnedRows*>(&red_o[0][0][0]);
     const int prior = u[U_PRIOR], rdim = A.rot.rdim, inter = A.rot.interleaved;
