@@ -511,7 +511,8 @@ libra_status libra_rotary_apply(libra_rotary rotary, int32_t dtype, const void* 
 
 /* Writes new rows into the cache, keys turned on the way: row r goes to slots[r] = page * 16
  * + slot (device int64 [rows]).  A row whose slot lies outside [0, 16 num_pages) is padding:
- * nothing of it is written, here or in q_out.  Slots must be distinct (repeated slots race).
+ * nothing of it is read or written, here or in q and q_out, and its position may be anything.
+ * Slots must be distinct (repeated slots race).
  * No plan is needed, so a captured call serves every later step whose slots and positions
  * are written to the same memory; libra_decode_attn reads what it wrote.
  *
