@@ -456,7 +456,10 @@ libra_status libra_append_attn(libra_kv_layout layout, libra_plan plan, const vo
  *   LIBRA_ROTARY_BANDS   theta_j (w + (1 - w) / s), w = clamp((n_j - slow) / (fast - slow),
  *                        0, 1), n_j = original_length * |theta_j| / 2 pi: pairs that make
  *                        more than `fast` turns over the original context keep their
- *                        frequency, those with fewer than `slow` are interpolated.
+ *                        frequency, those with fewer than `slow` are interpolated.  The
+ *                        weight w is linear in a pair's turns; a model whose weight is linear
+ *                        in the pair's index j, under the same parameters' names, is given
+ *                        by its frequencies.
  *
  * Frequencies are taken in extended precision and angles kept modulo one turn in 64-bit
  * fixed point, so the angle of a position of 2^31 is still good to 1e-9 turns (where

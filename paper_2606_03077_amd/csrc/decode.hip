@@ -22,10 +22,11 @@
 //
 // Unturned queries (libra_append_attn_rotary): the workgroup turns its heads through LDS first.
 // A turned query is the sum of two bf16 parts: of at most 8 heads, the parts are two halves of
-// the products' 16 columns, so the scores take no product more, and one cross-lane add.  Rounded
-// to bf16 it is the plain operand.  Where
-// a unit ends with its row's new token, it writes the token to the cache too, which saves a
-// step of single rows its write launch (3-5 us of 19 for 8 short rows, of 104 for 64 long ones).
+// the products' 16 columns, so the scores take no product more, and one cross-lane add; of more
+// heads they take products of their own (64 rows of 16 heads over one KV head 33 us, 2 registers
+// spilled).  Rounded to bf16 a turned query is the plain operand (32 us).  Where a unit of at most
+// 8 heads ends with its row's new token, it writes the token to the cache too, which saves a step
+// of such rows its write launch (3-5 us of 19 for 8 short rows, of 104 for 64 long ones).
 #include <cmath>
 #include <type_traits>
 
@@ -151,7 +152,9 @@ __device__ __forceinline__ bf16x4_bits as_bf16x4(uint32_t lo, uint32_t hi) {
 //   S^T[16 slots x 16 heads]: 4 x mfma 16x16x32 (k = channels);
 //   O^T[128 x 16 heads] += V^T[128 x 16 slots] . P^T: 8 x mfma 16x16x16 (k = slots),
 // whose B operand (lane = head + 16 * quad, slots 4 quad .. + 3) is exactly the score
-// tile's accumulator layout, so probabilities never leave registers.
+// tile's accumulator layout, so probabilities never leave registers.  They are rounded to bf16,
+// the operand's type: at most 2^-8 of each, independently, which is 1.2e-3 (rms) of an output of a
+// 7B-class step beside 1.7e-3 of its own rounding; the sum l takes them in float32.
 template <class Query>
 __device__ __forceinline__ void process_page(const PageRegs& r, int valid, int quad,
                                              const Query& qop, float sl2, Softmax& sm,
