@@ -6,10 +6,11 @@ As in test_gpu_append_rotary.py, whose bounds these are: the cache holds libra_r
 outputs are those of float64 attention of the exactly turned queries, and rounded queries give the
 bits of the two calls."""
 import pytest
+import torch
 
 import gpu_harness as H
-from test_gpu_append_rotary import Step, same
-from test_gpu_rotary import Handle
+from test_gpu_append_rotary import NAN, Step, same
+from test_gpu_rotary import Handle, randn
 from test_launched_forms import driver, forms, line, pytestmark as needs_compiler  # noqa: F401
 
 BATCHES = {  # lens, news, hq, hkv, CUs, form, whether keys are split
@@ -43,5 +44,35 @@ def test_form_and_turn(name, kw):
     rounded = s.one_step(rope, round_queries=True)
     s.reset()
     same(rounded, s.turned_first(rope), f"{name} {kw} rounded")
+    rope.close()
+    s.close()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv", [(28, 4), (16, 1)])
+def test_rounded_single_rows_replay_from_a_graph(hq, hkv):
+    """Each replay has other projections, positions and a cache whose last tokens are the former
+    replay's, and gives the bits of the two calls."""
+    H.say(f"[case] append rotary graph of rounded single rows {hq}/{hkv}")
+    s = Step([600, 1, 16, 17, 5000], [1] * 5, hq, hkv, seed=91, shift=3, num_cus=64)
+    rope = Handle(rdim=96)
+    out, lse = s.outputs()
+    s.call(rope, out, lse, round_queries=True)
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        s.call(rope, out, lse, round_queries=True)
+    for i in range(3):
+        s.qkv.copy_(randn(s.qkv.shape, torch.bfloat16, 92 + i))
+        s.pd.add_(500)
+        out.fill_(NAN)
+        lse.fill_(float("nan"))
+        torch.cuda.synchronize()
+        g.replay()
+        torch.cuda.synchronize()
+        got = out.clone(), lse.clone(), s.cache.k.clone(), s.cache.v.clone()
+        same(s.one_step(rope, round_queries=True), got, f"replay {i}, eager")
+        same(s.turned_first(rope), got, f"replay {i}")
+    del g
     rope.close()
     s.close()
