@@ -66,7 +66,8 @@ enum {
   LIBRA_MAX_GROUP = 16,     /* largest supported num_q_heads / num_kv_heads */
   LIBRA_MAX_KV_HEADS = 1024, /* largest supported num_kv_heads (a page's K or V, all heads,
                                 stays under 4 GiB of byte offsets) */
-  LIBRA_UNIT_INTS = 12      /* int32 fields per plan unit */
+  LIBRA_UNIT_INTS = 12,     /* int32 fields per plan unit */
+  LIBRA_MAX_MASK_WORDS = 8  /* 32-bit mask words of a drafted node: 256 nodes */
 };
 
 enum {
@@ -560,6 +561,141 @@ libra_status libra_append_attn_rotary(libra_kv_layout layout, libra_plan plan,
                                       size_t ws_bytes, void* out, float* lse, void* stream);
 
 /* ------------------------------------------------------------------------------ */
+/* Drafted steps                                                                   */
+/* ------------------------------------------------------------------------------ */
+/*
+ * A step that verifies drafted tokens (a tree of candidates per request, or a chain), with the
+ * requests' lengths on the GPU: none of these calls needs a plan, so captured calls serve every
+ * later step whose lengths, masks, slots and positions are written to the same memory.
+ *
+ *   libra_kv_map           pages for every request's new tokens; their slots and positions
+ *   libra_kv_append_norm   (or libra_kv_append) the nodes' keys and values to their slots
+ *   libra_tree_attn        every node over its request's cached tokens and its own ancestors
+ *   libra_kv_accept        the accepted path's keys and values behind the cached tokens
+ *   libra_kv_map           with the new lengths: gives back the rejected nodes' pages
+ */
+
+/* Makes the block tables follow the requests' lengths.  Request b has prior_lens[b] cached tokens,
+ * adds new_lens[b], and holds held_pages[b] pages, the first entries of its block-table row.  It
+ * wants ceil((prior + new) / 16) of them.  First, surplus pages go on top of the stack free_pages
+ * (num_free[0] entries, in order of request, then column); then missing pages are taken from its
+ * top (likewise) and written to the table.  A request that needs pages when those that it and all
+ * requests before it ask for exceed the stack is refused: its pages and table row stay as they are.
+ * A request with a negative length or page count, or more pages than bt_stride, is refused too.
+ *
+ * New tokens are rows, requests in order.  row_starts[b] is the sum of the new_lens before b (of
+ * negative ones: 0), at most `rows`; rows past `rows` are not mapped.  Row r = row_starts[b] + i is
+ * token prior + i: slots[r] = page * 16 + token % 16 (-1 if b is refused), positions[r] = prior + i,
+ * or prior + depths[r] (a node's depth in its tree) with depths.  Rows past the last request's are
+ * padding: slot -1, position 0.  libra_kv_append and libra_kv_append_norm skip slots of -1.
+ *
+ * All arrays are device memory: int32 [batch] prior_lens, new_lens, held_pages, held_out (the pages
+ * held now), refused (0 or 1); block_table int32 [batch][bt_stride]; free_pages int32
+ * [free_capacity]; num_free, num_free_out int32 [1]; depths int32 [rows] or NULL; slots int64
+ * [rows]; positions int32 [rows]; row_starts int32 [batch + 1].  held_out may be held_pages,
+ * num_free_out num_free; nothing else may overlap.  free_capacity >= every page that may come back
+ * (num_pages is enough); what does not fit is lost.  num_free outside [0, free_capacity] is taken as
+ * the nearer end.  Calls that share these arrays must be ordered. */
+libra_status libra_kv_map(int32_t batch, const int32_t* prior_lens, const int32_t* new_lens,
+                          const int32_t* held_pages, int32_t* block_table, int32_t bt_stride,
+                          int32_t* free_pages, int64_t free_capacity, const int32_t* num_free,
+                          const int32_t* depths, int64_t rows, int64_t* slots, int32_t* positions,
+                          int32_t* row_starts, int32_t* held_out, int32_t* num_free_out,
+                          int32_t* refused, void* stream);
+
+/* Moves accepted nodes' keys and values: request b's node accepted[b][i] (cached as token
+ * prior_lens[b] + accepted[b][i]) becomes token prior_lens[b] + i, for i < counts[b].  accepted:
+ * device int32 [batch][max_accepted], ascending in each row (a path's nodes are, where every node
+ * comes after its parent); an entry below its own index is skipped.  counts: device int32 [batch],
+ * at most max_accepted of which are read.  Moves whose tokens lie outside the block table, or
+ * whose pages outside the cache, are skipped.  No two requests may share a page that is written. */
+libra_status libra_kv_accept(libra_kv_layout layout, int32_t batch, const int32_t* prior_lens,
+                             const int32_t* accepted, int32_t max_accepted, const int32_t* counts,
+                             const int32_t* block_table, int32_t bt_stride, void* stream);
+
+/* A call's queries or keys: rows x num_heads vectors of head_dim elements; vector (r, h) of x lies
+ * at x + r * x_row_stride + h * x_head_stride elements, of out and grad likewise.  Strides are >= 0;
+ * those of inputs may be 0, out's vectors must not overlap. */
+typedef struct libra_norm_heads {
+  const void* x;             /* device */
+  int64_t x_row_stride, x_head_stride;
+  int32_t num_heads;         /* 0: none, and nothing else is read */
+  const void* weight;        /* device, head_dim values of weight_dtype */
+  void* out;                 /* device: y, or in the backward pass dx */
+  int64_t out_row_stride, out_head_stride;
+  const void* grad;          /* device: dy (backward only) */
+  int64_t grad_row_stride, grad_head_stride;
+  float* weight_grad;        /* device, head_dim values, written (backward only), or NULL */
+} libra_norm_heads;
+
+/* Norms of queries and keys, head by head, with their rotary positions in the same pass:
+ *
+ *   n = x / sqrt(mean(x^2) + eps) over the head's channels,  u = weight n,  y = u turned as by
+ *   libra_rotary_apply (channels past R: y = u),
+ *
+ * in float32 (a head whose squares exceed float32 gives 0), rounded once to y's type.  eps > 0.
+ * dtype: LIBRA_DTYPE_BF16, _FP16 or _FP32, of x and out, which are aligned to it; weight_dtype: any
+ * of these.  positions: device int32 [rows].  out may be x (the same strides), otherwise they must
+ * not overlap.  q or k may be NULL. */
+libra_status libra_qk_norm_rotary(libra_rotary rotary, int32_t dtype, int32_t weight_dtype, float eps,
+                                  const int32_t* positions, int64_t rows, int32_t head_dim,
+                                  const libra_norm_heads* q, const libra_norm_heads* k, void* stream);
+
+/* Its gradient's pass.  With dy turned back (the negative angle, the same amplitude) to du:
+ *
+ *   dx = (weight du - n mean(weight du n)) / sqrt(mean(x^2) + eps),
+ *   weight_grad = sum over rows and heads of du n (float32, overwritten; 0 where there are no rows).
+ *
+ * The sums' order is fixed by the sizes, so equal calls give equal bits.  out may be x or grad (the
+ * same strides).  workspace: device, 16-byte aligned, libra_qk_norm_rotary_workspace_bytes of it
+ * for weight gradients (not read without); calls that may overlap need one each. */
+size_t libra_qk_norm_rotary_workspace_bytes(int64_t rows, int32_t num_q_heads, int32_t num_k_heads,
+                                            int32_t head_dim);
+libra_status libra_qk_norm_rotary_backward(libra_rotary rotary, int32_t dtype, int32_t weight_dtype,
+                                           float eps, const int32_t* positions, int64_t rows,
+                                           int32_t head_dim, const libra_norm_heads* q,
+                                           const libra_norm_heads* k, void* workspace, size_t ws_bytes,
+                                           void* stream);
+
+/* libra_kv_append with keys and queries normalised (as above, q_weight and k_weight: device, 128
+ * values of weight_dtype) before they are turned: the bits that libra_qk_norm_rotary gives (for
+ * tensors of such rows).  A rotary is needed; q, q_weight and q_out may be NULL together. */
+libra_status libra_kv_append_norm(libra_kv_layout layout, libra_rotary rotary, int32_t weight_dtype,
+                                  float eps, const int32_t* positions, const int64_t* slots, int64_t rows,
+                                  const void* q, int64_t q_row_stride, int32_t num_q_heads,
+                                  const void* q_weight, const void* k_new, int64_t k_row_stride,
+                                  const void* k_weight, const void* v_new, int64_t v_row_stride,
+                                  int32_t num_kv_heads, void* q_out, void* stream);
+
+/* Attention of drafted nodes.  Request b's nodes are the query rows [row_starts[b], row_starts[b +
+ * 1]) (device int32 [batch + 1], ascending, as libra_kv_map writes them), its node i is cached as
+ * token prior_lens[b] + i, and each of its query heads h attends, with the formula of
+ * libra_decode_attn, the tokens [0, prior_lens[b]) and the nodes j < its request's node count whose
+ * bit is set in the row's mask: bit j % 32 of mask[r * mask_words + j / 32] (device uint32
+ * [rows][mask_words], mask_words in [1, LIBRA_MAX_MASK_WORDS]; nodes past the last word are seen by
+ * none).  Bits need not form a tree.  mask NULL (mask_words 0): nodes 0 .. i, a chain.  A row that
+ * sees nothing gives out = 0, lse = -inf.  Keys and values that a row does not see may be
+ * anything, infinities and NaN too, and so may slots past the last node.
+ *
+ * q, out: device bf16 [rows][num_q_heads][128], lse: device float32 [rows][num_q_heads] or NULL.  Rows
+ * outside every request's are neither read nor written.  Lengths are read on the device, by the
+ * kernels: tokens past bt_stride * 16 are not seen, and block-table ids of the tokens in [0,
+ * prior + nodes) that lie outside the cache read another page of it, so that a request that
+ * libra_kv_map refused gives meaningless rows but no fault.
+ *
+ * workspace: device, 256-byte aligned, at least libra_tree_attn_workspace_bytes(rows, batch,
+ * num_q_heads, num_kv_heads) bytes (0: bad arguments), of any contents; calls and graphs may share
+ * one if they are ordered.  Results depend on how a launch divides the work (their last bits change
+ * with the other requests' lengths), and are the same for the same call. */
+size_t libra_tree_attn_workspace_bytes(int64_t rows, int32_t batch, int32_t num_q_heads,
+                                       int32_t num_kv_heads);
+libra_status libra_tree_attn(libra_kv_layout layout, const void* q, int64_t rows,
+                             const int32_t* prior_lens, const int32_t* row_starts, const uint32_t* mask,
+                             int32_t mask_words, const int32_t* block_table, int32_t bt_stride,
+                             int32_t batch, int32_t num_q_heads, float scale, void* workspace,
+                             size_t ws_bytes, void* out, float* lse, void* stream);
+
+/* ------------------------------------------------------------------------------ */
 /* Per-kernel timing                                                               */
 /* ------------------------------------------------------------------------------ */
 /*
@@ -582,7 +718,10 @@ enum {
   LIBRA_KERNEL_COPY_OUT = 8,
   LIBRA_KERNEL_COPY_IN = 9,
   LIBRA_KERNEL_ROTARY = 10,
-  LIBRA_KERNEL_KINDS = 11
+  LIBRA_KERNEL_TABLES = 11,
+  LIBRA_KERNEL_TREE = 12,
+  LIBRA_KERNEL_ACCEPT = 13,
+  LIBRA_KERNEL_KINDS = 14
 };
 
 typedef struct libra_kernel_times {

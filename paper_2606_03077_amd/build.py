@@ -23,11 +23,13 @@ LIB = os.path.join(PKG, "liblibra.so")
 ARCH = "gfx950"
 
 SOURCES = ["api.cpp", "plan.cpp", "migrate.cpp", "cost_model.cpp", "scheduler.cpp", "kv_layout.hip", "decode.hip", "merge.hip",
-           "chunk.hip", "xcd_weights.hip", "scratch.hip", "positions.cpp", "rotary.hip"]
+           "chunk.hip", "xcd_weights.hip", "scratch.hip", "positions.cpp", "rotary.hip",
+           "drafts.cpp", "norm.hip", "kv_map.hip", "tree.hip"]
 
 # Packed-fp32 VALU forms are disabled for all device code (the host pass warns that it
-# does not know the feature; that is harmless).
-COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function", f"-I{INCLUDE}",
+# does not know the feature; that is harmless).  -Wno-inline-asm: the copies to LDS name m0,
+# which they set, as clobbered, and each would be warned of.
+COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function", "-Wno-inline-asm", f"-I{INCLUDE}",
           f"-I{CSRC}", f"--offload-arch={ARCH}",
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
 

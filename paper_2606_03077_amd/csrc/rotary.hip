@@ -14,57 +14,14 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "rotary_calls.h"
+#include "drafts.h"
+#include "row_types.h"
 
 namespace libra {
 namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxPairs = kMaxRotaryDim / 2;
-
-// Element types: four channels as loaded, to and from float32 (rounded to nearest even).
-struct Bf16 {
-  using Elem = uint16_t;
-  using Quad = uint2;
-  static __device__ __forceinline__ float get(Elem e) { return bf16_to_f32(e); }
-  static __device__ __forceinline__ Elem put(float f) { return Elem(rotary_pack_bf16(f, f)); }
-  static __device__ __forceinline__ void unpack(Quad q, float (&f)[4]) {
-    f[0] = bf16_to_f32(q.x & 0xFFFF), f[1] = bf16_to_f32(q.x >> 16);
-    f[2] = bf16_to_f32(q.y & 0xFFFF), f[3] = bf16_to_f32(q.y >> 16);
-  }
-  static __device__ __forceinline__ Quad pack(const float (&f)[4]) {
-    return make_uint2(rotary_pack_bf16(f[0], f[1]), rotary_pack_bf16(f[2], f[3]));
-  }
-};
-struct Fp16 {
-  using Elem = uint16_t;
-  using Quad = uint2;
-  static __device__ __forceinline__ float get(Elem e) {
-    return float(__builtin_bit_cast(_Float16, e));
-  }
-  static __device__ __forceinline__ Elem put(float f) {
-    return __builtin_bit_cast(Elem, _Float16(f));
-  }
-  static __device__ __forceinline__ void unpack(Quad q, float (&f)[4]) {
-    f[0] = get(Elem(q.x)), f[1] = get(Elem(q.x >> 16));
-    f[2] = get(Elem(q.y)), f[3] = get(Elem(q.y >> 16));
-  }
-  static __device__ __forceinline__ Quad pack(const float (&f)[4]) {
-    return make_uint2(put(f[0]) | uint32_t(put(f[1])) << 16, put(f[2]) | uint32_t(put(f[3])) << 16);
-  }
-};
-struct Fp32 {
-  using Elem = float;
-  using Quad = float4;
-  static __device__ __forceinline__ float get(Elem e) { return e; }
-  static __device__ __forceinline__ Elem put(float f) { return f; }
-  static __device__ __forceinline__ void unpack(Quad q, float (&f)[4]) {
-    f[0] = q.x, f[1] = q.y, f[2] = q.z, f[3] = q.w;
-  }
-  static __device__ __forceinline__ Quad pack(const float (&f)[4]) {
-    return make_float4(f[0], f[1], f[2], f[3]);
-  }
-};
 
 // Rows x heads to turn, for both forms below.
 template <class T>
@@ -88,63 +45,27 @@ __device__ __forceinline__ bool skipped(const RowsArgs<T>& A, int64_t row) {
   return A.slots && uint64_t(A.slots[row]) >= uint64_t(A.slot_end);
 }
 
-// Four pairs in two quads, which is what a thread turns: half pairing takes channel e of both
-// quads as a pair, interleaved pairing two neighbours of one.
+// Two quads of a head normalised over its `lanes` threads' quads, and turned if they are.
 template <class T, bool kInter>
-__device__ __forceinline__ void turn_quads(typename T::Quad& a, typename T::Quad& b,
-                                           const float2 (&cs)[4]) {
-  float f[4], g[4], y[4], z[4];
+__device__ __forceinline__ void norm_quads(typename T::Quad& a, typename T::Quad& b,
+                                           const float (&wa)[4], const float (&wb)[4], int lanes,
+                                           int dim, float eps, bool turned, const float2 (&cs)[4]) {
+  float f[4], g[4], y[4], z[4], squares = 0.f;
   T::unpack(a, f);
   T::unpack(b, g);
-  if (kInter) {
 #pragma unroll
-    for (int e = 0; e < 2; ++e) {
-      y[2 * e] = turn_first(f[2 * e], f[2 * e + 1], cs[e]);
-      y[2 * e + 1] = turn_second(f[2 * e], f[2 * e + 1], cs[e]);
-      z[2 * e] = turn_first(g[2 * e], g[2 * e + 1], cs[2 + e]);
-      z[2 * e + 1] = turn_second(g[2 * e], g[2 * e + 1], cs[2 + e]);
-    }
+  for (int e = 0; e < 4; ++e) squares = __builtin_fmaf(f[e], f[e], squares);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) squares = __builtin_fmaf(g[e], g[e], squares);
+  const float r = norm_scale(group_sum(squares, lanes), dim, eps);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) f[e] = f[e] * r * wa[e], g[e] = g[e] * r * wb[e];
+  if (turned) {
+    turn_values<kInter>(f, g, cs, y, z);
+    a = T::pack(y), b = T::pack(z);
   } else {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      y[e] = turn_first(f[e], g[e], cs[e]);
-      z[e] = turn_second(f[e], g[e], cs[e]);
-    }
+    a = T::pack(f), b = T::pack(g);
   }
-  a = T::pack(y);
-  b = T::pack(z);
-}
-
-// The quads of piece j of a head of `pieces`, turned ones while j < R / 8, copied ones after.
-// Neighbouring threads take neighbouring quads, so that an instruction covers whole lines; two
-// quads of 8 bytes that are neighbours themselves make one access of 16.
-template <class T, bool kInter>
-__device__ __forceinline__ int2 quads_of(int j, int R8, int pieces) {
-  if (kInter && sizeof(typename T::Quad) == 8) return make_int2(2 * j, 2 * j + 1);
-  return j < R8 ? make_int2(j, j + R8) : make_int2(j + R8, j + pieces);
-}
-
-// Pair i of the four that a turned piece's quads hold.
-template <bool kInter>
-__device__ __forceinline__ int pair_of(int2 quads, int j, int i) {
-  return !kInter ? 4 * j + i : i < 2 ? 2 * quads.x + i : 2 * quads.y + i - 2;
-}
-
-template <bool kPastCaches, class Quad>
-__device__ __forceinline__ Quad load_quad(const Quad* p) {
-  typedef uint32_t V __attribute__((ext_vector_type(sizeof(Quad) / 4)));
-  if constexpr (kPastCaches)
-    return __builtin_bit_cast(Quad, __builtin_nontemporal_load(reinterpret_cast<const V*>(p)));
-  else
-    return *p;
-}
-template <bool kPastCaches, class Quad>
-__device__ __forceinline__ void store_quad(Quad* p, Quad v) {
-  typedef uint32_t V __attribute__((ext_vector_type(sizeof(Quad) / 4)));
-  if constexpr (kPastCaches)
-    __builtin_nontemporal_store(__builtin_bit_cast(V, v), reinterpret_cast<V*>(p));
-  else
-    *p = v;
 }
 
 constexpr int64_t kStreamBytes = int64_t(128) << 20;  // written by a call whose writes go past
@@ -155,9 +76,11 @@ enum Streaming : int { kCached, kReads, kReadsWrites };
 // Wide form: R and the head size are multiples of 8, rows are aligned for four channels at a
 // time.  A thread owns two quads of a head (4 pairs, or 8 copied channels), computes their
 // cosines and sines once, and turns them in up to kHeads heads.
-template <class T, bool kInter, int kHeads, Streaming kStream, class Rot>
+// kNorm: the heads are normalised first (their size is a power of two then, so that a head's
+// threads are an aligned group of lanes, of which all take part or none).
+template <class T, bool kInter, int kHeads, Streaming kStream, bool kNorm = false, class Rot>
 __device__ __forceinline__ void turn_rows_wide(const Rot& rot, const RowsArgs<T>& A, int64_t bx,
-                                               int by) {
+                                               int by, [[maybe_unused]] const HeadNorm& norm = {}) {
   using Quad = typename T::Quad;
   const int t = threadIdx.x;
   const int r = t / A.per_row, in_row = t - r * A.per_row;
@@ -166,7 +89,7 @@ __device__ __forceinline__ void turn_rows_wide(const Rot& rot, const RowsArgs<T>
   if (r >= A.block_rows || row >= A.rows || skipped(A, row)) return;
   const int R8 = rot.rdim / 8;
   const bool turned = j < R8;
-  if (!turned && A.x == A.out) return;
+  if (!kNorm && !turned && A.x == A.out) return;
   const int2 qd = quads_of<T, kInter>(j, R8, A.per_head);
   const int head0 = by * A.head_slots * kHeads + h0;
   const typename T::Elem* x = A.x + row * A.x_row;
@@ -179,6 +102,12 @@ __device__ __forceinline__ void turn_rows_wide(const Rot& rot, const RowsArgs<T>
       a[i] = load_quad<kStream != kCached>(reinterpret_cast<const Quad*>(x + h * A.x_head + 4 * qd.x));
       b[i] = load_quad<kStream != kCached>(reinterpret_cast<const Quad*>(x + h * A.x_head + 4 * qd.y));
     }
+  }
+  [[maybe_unused]] float wa[4], wb[4];
+  if constexpr (kNorm) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      wa[e] = norm_weight(norm, 4 * qd.x + e), wb[e] = norm_weight(norm, 4 * qd.y + e);
   }
   float2 cs[4];
   if (turned) {
@@ -193,7 +122,8 @@ __device__ __forceinline__ void turn_rows_wide(const Rot& rot, const RowsArgs<T>
   for (int i = 0; i < kHeads; ++i) {
     const int h = head0 + i * A.head_slots;
     if (h < A.heads) {
-      if (turned) turn_quads<T, kInter>(a[i], b[i], cs);
+      if constexpr (kNorm) norm_quads<T, kInter>(a[i], b[i], wa, wb, A.per_head, A.dim, norm.eps, turned, cs);
+      else if (turned) turn_quads<T, kInter>(a[i], b[i], cs);
       store_quad<kStream == kReadsWrites>(reinterpret_cast<Quad*>(out + h * A.out_head + 4 * qd.x), a[i]);
       store_quad<kStream == kReadsWrites>(reinterpret_cast<Quad*>(out + h * A.out_head + 4 * qd.y), b[i]);
     }
@@ -250,6 +180,63 @@ __global__ __launch_bounds__(kThreads) void rotary_narrow_kernel(RotaryArgs<kMax
   turn_rows_narrow(rot, A, blockIdx.x, blockIdx.y);
 }
 
+// Queries' rows, then keys', both normalised: q_blocks blocks for the first.
+template <class T, bool kInter, int kHeads, Streaming kStream>
+__global__ __launch_bounds__(kThreads) void norm_rotary_wide_kernel(RotaryArgs<kMaxPairs> rot, RowsArgs<T> Q,
+                                                                    RowsArgs<T> K, RowNorms norms, int q_blocks) {
+  const int i = int(blockIdx.x);
+  if (i < q_blocks)
+    turn_rows_wide<T, kInter, kHeads, kStream, true>(rot, Q, i / Q.y_blocks, i % Q.y_blocks, norms.q);
+  else
+    turn_rows_wide<T, kInter, kHeads, kStream, true>(rot, K, (i - q_blocks) / K.y_blocks, (i - q_blocks) % K.y_blocks, norms.k);
+}
+
+// Any head size, R, alignment: a wave per head.  Its values go through LDS, where a channel finds
+// its partner; all are read before one is written, so in place is fine.
+template <class T>
+__device__ __forceinline__ void norm_rows_any(const RotaryArgs<kMaxPairs>& rot, const RowsArgs<T>& A,
+                                              int64_t vector, const HeadNorm& norm, float* u) {
+  const int lane = threadIdx.x & 63;
+  const int64_t row = vector / A.heads;
+  const int h = int(vector - row * A.heads);
+  if (row >= A.rows) return;
+  const typename T::Elem* x = A.x + row * A.x_row + h * A.x_head;
+  for (int d = lane; d < A.dim; d += 64) u[d] = T::get(x[d]);
+  auto wave_sync = [] {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  };
+  wave_sync();
+  float squares = 0.f;  // eight channels a lane, as the cache append adds them
+#pragma unroll
+  for (int e = 0; e < kMaxRotaryHead / 64; ++e)
+    if (8 * lane + e < A.dim) squares = __builtin_fmaf(u[8 * lane + e], u[8 * lane + e], squares);
+  const float r = norm_scale(group_sum(squares, 64), A.dim, norm.eps);
+  wave_sync();
+  for (int d = lane; d < A.dim; d += 64) u[d] = u[d] * r * norm_weight(norm, d);
+  wave_sync();
+  const int32_t pos = A.positions[row];
+  typename T::Elem* out = A.out + row * A.out_row + h * A.out_head;
+  for (int d = lane; d < A.dim; d += 64) {
+    float y = u[d];
+    if (d < rot.rdim) {
+      const bool first = rot.interleaved ? !(d & 1) : d < rot.rdim / 2;
+      const int o = rot.interleaved ? d ^ 1 : first ? d + rot.rdim / 2 : d - rot.rdim / 2;
+      const float2 cs = rotary_cos_sin(rot.turn[rot.interleaved ? d / 2 : first ? d : o], pos, rot.amplitude);
+      y = first ? turn_first(y, u[o], cs) : turn_second(u[o], y, cs);
+    }
+    out[d] = T::put(y);
+  }
+}
+template <class T>
+__global__ __launch_bounds__(kThreads) void norm_rotary_any_kernel(RotaryArgs<kMaxPairs> rot, RowsArgs<T> Q,
+                                                                   RowsArgs<T> K, RowNorms norms, int q_blocks) {
+  __shared__ float u[kThreads / 64][kMaxRotaryHead];
+  const int wave = threadIdx.x >> 6, i = int(blockIdx.x);
+  const int64_t at = i < q_blocks ? i : i - q_blocks;
+  norm_rows_any<T>(rot, i < q_blocks ? Q : K, at * (kThreads / 64) + wave, i < q_blocks ? norms.q : norms.k, u[wave]);
+}
+
 constexpr int64_t kMaxBlocks = int64_t(1) << 22;  // per launch: 2^30 threads
 
 // How rows x heads are cut: the form, heads per thread, rows per block.
@@ -268,8 +255,9 @@ struct RowsPlan {
   int half;
 };
 
+// many: whether threads take several heads (-1: by the rule below).
 template <class T>
-RowsPlan<T> plan_rows(const Rotary& r, const RotaryRows& a) {
+RowsPlan<T> plan_rows(const Rotary& r, const RotaryRows& a, int many = -1) {
   RowsPlan<T> p{};
   RowsArgs<T>& A = p.args;
   A.x = static_cast<const typename T::Elem*>(a.x);
@@ -288,7 +276,7 @@ RowsPlan<T> plan_rows(const Rotary& r, const RotaryRows& a) {
   // row has heads enough: 40,960 rows of 40 heads (bf16) 168 us against 197 with one head each
   // and 177 with two, of 28 heads 125 (143, 123); but 1,024 rows of 28 heads 9.0 us against 8.6,
   // 16 rows 6.4 against 6.1, 40,960 rows of 8 heads 46 against 45 (cold caches, launch included).
-  p.many = a.heads >= 16 && a.rows * a.heads * A.per_head >= int64_t(2560) * kThreads;
+  p.many = many >= 0 ? many != 0 : a.heads >= 16 && a.rows * a.heads * A.per_head >= int64_t(2560) * kThreads;
   // Nothing goes past the caches where an instruction covers half lines (128 bytes), as half
   // pairing of 64 16-bit channels does: 40,960 rows of 40 heads 168 us so, 151 through them.
   p.lines = (r.pairing == LIBRA_ROTARY_INTERLEAVED && quad == 8) ||
@@ -344,6 +332,49 @@ hipError_t apply(const Rotary& r, const RotaryRows& a, hipStream_t s) {
   return hipSuccess;
 }
 
+// Queries and keys in one launch (a tensor without heads takes no blocks).
+template <class T>
+hipError_t apply_norm(const Rotary& r, const RotaryRows& q, const RotaryRows& k, const RowNorms& norms,
+                      hipStream_t s) {
+  const int dim = r.head_dim, heads = q.heads + k.heads;
+  const bool many = heads >= 16 && q.rows * heads * (dim / 8) >= int64_t(2560) * kThreads;
+  // A tensor without heads is planned as the other, and gets no blocks.
+  const RowsPlan<T> pq = plan_rows<T>(r, q.heads ? q : k, many), pk = plan_rows<T>(r, k.heads ? k : q, many);
+  const bool wide = (dim & (dim - 1)) == 0 && pq.wide && pk.wide;
+  const bool inter = r.pairing == LIBRA_ROTARY_INTERLEAVED;
+  const bool lines = pq.lines;
+  const bool stream = many && lines && q.rows * heads * dim * int64_t(sizeof(typename T::Elem)) >= kStreamBytes;
+  auto wide_form = [&](auto pairing) {
+    constexpr bool kInter = decltype(pairing)::value;
+    return !many    ? norm_rotary_wide_kernel<T, kInter, 1, kCached>
+           : stream ? norm_rotary_wide_kernel<T, kInter, 4, kReadsWrites>
+           : lines  ? norm_rotary_wide_kernel<T, kInter, 4, kReads>
+                    : norm_rotary_wide_kernel<T, kInter, 4, kCached>;
+  };
+  auto form = !wide ? norm_rotary_any_kernel<T> : inter ? wide_form(std::true_type{}) : wide_form(std::false_type{});
+  const RotaryArgs<kMaxPairs> rot = rotary_args<kMaxPairs>(r);
+  auto blocks = [&](const RowsPlan<T>& p, int of, int64_t rows) -> int64_t {
+    if (!of) return 0;
+    return wide ? p.blocks(rows) * p.args.y_blocks : (rows * p.args.heads + kThreads / 64 - 1) / (kThreads / 64);
+  };
+  // Both tensors' blocks of a launch stay in 32 bits: a row has at most 2 * 65,535 heads.
+  const int64_t step = std::max<int64_t>(1, kMaxBlocks * (kThreads / 64) / heads);
+  for (int64_t r0 = 0; r0 < q.rows; r0 += step) {
+    RowsArgs<T> A[2] = {pq.args, pk.args};
+    for (RowsArgs<T>& a : A) {
+      a.rows = std::min(step, q.rows - r0);
+      a.x += r0 * a.x_row;
+      a.out += r0 * a.out_row;
+      a.positions += r0;
+    }
+    const int64_t nq = blocks(pq, q.heads, A[0].rows), nk = blocks(pk, k.heads, A[0].rows);
+    hipLaunchKernelGGL(form, dim3(unsigned(nq + nk)), dim3(kThreads), 0, s, rot, A[0], A[1], norms, int(nq));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
 // --- cache append ------------------------------------------------------------------------
 
 struct WriteArgs {
@@ -370,17 +401,6 @@ using Rot = RotaryArgs<kRotaryPairs>;  // rdim 0: keys are copied
 // How a key is turned: quads in half or interleaved pairing (R a multiple of 8; copies are
 // interleaved quads of which none turns), or granules whose pairs may lie anywhere.
 enum KeyForm : int { kHalfQuads, kInterQuads, kAnyPairs };
-
-// Element offsets inside a tile (kv_layout.hip has the layout).
-__device__ __forceinline__ int k_off(int s, int d) { return ((d >> 3) * 16 + s) * 8 + (d & 7); }
-__device__ __forceinline__ int v_off(int s, int d) {
-  return (128 * ((s >> 2) & 1) + d) * 8 + (s >> 3) * 4 + (s & 3);
-}
-__device__ __forceinline__ void v_scatter8(uint16_t* tile, int s, int d0, uint4 val) {
-  const uint32_t w[4] = {val.x, val.y, val.z, val.w};
-#pragma unroll
-  for (int i = 0; i < 8; ++i) tile[v_off(s, d0 + i)] = uint16_t(w[i / 2] >> (16 * (i & 1)));
-}
 
 // What thread j of a row's 16 holds of it, for one KV head: eight channels of the key (two
 // quads; not used by kAnyPairs, which reads them when it turns them) and of the value.
@@ -425,7 +445,53 @@ __device__ __forceinline__ uint4 turn_any_granule(const Rot& rot, const uint16_t
   return out[0];
 }
 
+// Granule j of a row that is normalised before it is turned, its pairs anywhere; u: the row.
+__device__ __forceinline__ uint4 norm_any_granule(const Rot& rot, const uint16_t* row, int j, int32_t pos,
+                                                  const HeadNorm& norm, float* u) {
+  const uint4 x = *reinterpret_cast<const uint4*>(row + 8 * j);
+  float f[4], g[4], squares = 0.f;
+  Bf16::unpack(make_uint2(x.x, x.y), f);
+  Bf16::unpack(make_uint2(x.z, x.w), g);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) squares = __builtin_fmaf(f[e], f[e], squares);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) squares = __builtin_fmaf(g[e], g[e], squares);
+  const float r = norm_scale(group_sum(squares, kDim / 8), kDim, norm.eps);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    u[8 * j + e] = f[e] * r * norm_weight(norm, 8 * j + e);
+    u[8 * j + 4 + e] = g[e] * r * norm_weight(norm, 8 * j + 4 + e);
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  float y[8];
+  const int half = rot.rdim / 2;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const int d = 8 * j + e;
+    y[e] = u[d];
+    if (d < rot.rdim) {
+      const bool first = rot.interleaved ? !(d & 1) : d < half;
+      const int o = rot.interleaved ? d ^ 1 : first ? d + half : d - half;
+      const float2 cs = rotary_cos_sin(rot.turn[rot.interleaved ? d / 2 : first ? d : o], pos, rot.amplitude);
+      y[e] = first ? turn_first(y[e], u[o], cs) : turn_second(u[o], y[e], cs);
+    }
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  return make_uint4(rotary_pack_bf16(y[0], y[1]), rotary_pack_bf16(y[2], y[3]),
+                    rotary_pack_bf16(y[4], y[5]), rotary_pack_bf16(y[6], y[7]));
+}
+
 // 16 rows of one query head, any pairs.
+__device__ __forceinline__ void norm_queries_any(const Rot& rot, const RowsArgs<Bf16>& A, int64_t bx,
+                                                 int head, const HeadNorm& norm, float (*u)[kDim]) {
+  const int s = threadIdx.x >> 4, j = threadIdx.x & 15;
+  const int64_t row = bx * kPage + s;
+  if (row >= A.rows || skipped(A, row)) return;
+  const uint4 y = norm_any_granule(rot, A.x + row * A.x_row + int64_t(head) * kDim, j, A.positions[row], norm, u[s]);
+  *reinterpret_cast<uint4*>(A.out + row * A.out_row + int64_t(head) * kDim + 8 * j) = y;
+}
 __device__ __forceinline__ void turn_queries_any(const Rot& rot, const RowsArgs<Bf16>& A, int64_t bx,
                                                  int head, float2 (*cs)[kRotaryPairs]) {
   const int s = threadIdx.x >> 4, j = threadIdx.x & 15;
@@ -435,23 +501,36 @@ __device__ __forceinline__ void turn_queries_any(const Rot& rot, const RowsArgs<
   *reinterpret_cast<uint4*>(A.out + row * A.out_row + int64_t(head) * kDim + 8 * j) = y;
 }
 
-// Turns the piece's key and stores it to slot s of the K tile.
-template <int kForm>
+// Turns the piece's key (normalised first if kNorm: all 16 threads of the row take part) and stores
+// it to slot s of the K tile.  cs: the row's part of LDS (kAnyPairs).
+template <int kForm, bool kNorm = false>
 __device__ __forceinline__ void store_key(const WriteArgs& A, const Rot& rot, const NewPiece& p,
                                           int64_t row, int g, int j, int s, uint16_t* tile,
-                                          float2* cs) {
-  if constexpr (kForm == kAnyPairs) {
+                                          float2* cs, [[maybe_unused]] const HeadNorm& norm = {}) {
+  if constexpr (kForm == kAnyPairs && kNorm) {
+    *reinterpret_cast<uint4*>(tile + k_off(s, 8 * j)) = norm_any_granule(
+        rot, A.k_new + row * A.k_row + g * kDim, j, p.pos, norm, reinterpret_cast<float*>(cs));
+  } else if constexpr (kForm == kAnyPairs) {
     *reinterpret_cast<uint4*>(tile + k_off(s, 8 * j)) =
         turn_any_granule(rot, A.k_new + row * A.k_row + g * kDim, j, p.pos, cs);
   } else {
     constexpr bool kInter = kForm == kInterQuads;
     const int2 qd = quads_of<Bf16, kInter>(j, rot.rdim / 8, kDim / 8);
     uint2 a = p.a, b = p.b;
-    if (j < rot.rdim / 8) {
-      float2 t[4];
+    const bool turned = j < rot.rdim / 8;
+    float2 t[4];
+    if (turned) {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
         t[i] = rotary_cos_sin(rot.turn[pair_of<kInter>(qd, j, i)], p.pos, rot.amplitude);
+    }
+    if constexpr (kNorm) {
+      float wa[4], wb[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        wa[e] = norm_weight(norm, 4 * qd.x + e), wb[e] = norm_weight(norm, 4 * qd.y + e);
+      norm_quads<Bf16, kInter>(a, b, wa, wb, kDim / 8, kDim, norm.eps, turned, t);
+    } else if (turned) {
       turn_quads<Bf16, kInter>(a, b, t);
     }
     *reinterpret_cast<uint2*>(tile + k_off(s, 4 * qd.x)) = a;
@@ -463,18 +542,25 @@ __device__ __forceinline__ void store_key(const WriteArgs& A, const Rot& rot, co
 // slots of one page form a run; the block writes the runs that begin among its rows, so a long
 // chunk's blocks write whole pages wherever its pages begin.  Whole pages go through LDS (V
 // tiles are transposed), single rows straight to their slots.  The other blocks turn queries.
-template <int kForm, int kHeads, Streaming kStream>
+struct NoNorms {
+  HeadNorm q, k;  // not read
+};
+template <int kForm, int kHeads, Streaming kStream, class Norms = NoNorms>
 __global__ __launch_bounds__(kThreads) void kv_append_kernel(Rot rot, WriteArgs A,
-                                                             RowsArgs<Bf16> Q) {
+                                                             RowsArgs<Bf16> Q, Norms norms) {
+  constexpr bool kNorm = std::is_same_v<Norms, RowNorms>;
+  static_assert(sizeof(float2[kRotaryPairs]) == sizeof(float[kDim]), "a row of either in LDS");
   __shared__ __align__(16) uint16_t vt[kTileElems];
   __shared__ __align__(16) float2 cs[kForm == kAnyPairs ? kPage : 1][kRotaryPairs];
   if (int(blockIdx.x) >= A.kv_blocks) {
     const int i = int(blockIdx.x) - A.kv_blocks;
     const int bx = i / Q.y_blocks;
-    if constexpr (kForm == kAnyPairs)
+    if constexpr (kForm == kAnyPairs && kNorm)
+      norm_queries_any(rot, Q, bx, i - bx * Q.y_blocks, norms.q, reinterpret_cast<float(*)[kDim]>(cs));
+    else if constexpr (kForm == kAnyPairs)
       turn_queries_any(rot, Q, bx, i - bx * Q.y_blocks, cs);
     else
-      turn_rows_wide<Bf16, kForm == kInterQuads, kHeads, kStream>(rot, Q, bx, i - bx * Q.y_blocks);
+      turn_rows_wide<Bf16, kForm == kInterQuads, kHeads, kStream, kNorm>(rot, Q, bx, i - bx * Q.y_blocks, norms.q);
     return;
   }
   const int blk = int(blockIdx.x) / A.hkv, g = int(blockIdx.x) - blk * A.hkv;
@@ -500,7 +586,7 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(Rot rot, WriteArgs 
     const size_t base = (size_t(first >> 4) * A.hkv + g) * kTileElems;
     const NewPiece p = load_piece<kForm>(A, rot, row, g, j);
     v_scatter8(vt, s, 8 * j, p.v);
-    store_key<kForm>(A, rot, p, row, g, j, s, A.k_cache + base, cs[kForm == kAnyPairs ? s : 0]);
+    store_key<kForm, kNorm>(A, rot, p, row, g, j, s, A.k_cache + base, cs[kForm == kAnyPairs ? s : 0], norms.k);
     __syncthreads();
     *reinterpret_cast<uint4*>(A.v_cache + base + t * 8) = *reinterpret_cast<const uint4*>(vt + t * 8);
     return;
@@ -513,7 +599,7 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(Rot rot, WriteArgs 
     const int sl = int(at & 15);
     const NewPiece p = load_piece<kForm>(A, rot, row, g, j);
     v_scatter8(A.v_cache + base, sl, 8 * j, p.v);
-    store_key<kForm>(A, rot, p, row, g, j, sl, A.k_cache + base, cs[kForm == kAnyPairs ? s : 0]);
+    store_key<kForm, kNorm>(A, rot, p, row, g, j, sl, A.k_cache + base, cs[kForm == kAnyPairs ? s : 0], norms.k);
   }
 }
 
@@ -573,8 +659,11 @@ hipError_t launch_rotary(const Rotary& r, const RotaryRows& a, hipStream_t s) {
   }
 }
 
-hipError_t launch_kv_append(const KvLayout& L, const NewRows& n, const int64_t* slots,
-                            int64_t rows, int32_t hq, void* q_out, hipStream_t s) {
+namespace {
+
+template <class Norms>
+hipError_t append_rows(const KvLayout& L, const NewRows& n, const int64_t* slots, int64_t rows,
+                       int32_t hq, void* q_out, const Norms& norms, hipStream_t s) {
   Rot rot{};
   if (n.rotary) rot = rotary_args<kRotaryPairs>(*n.rotary);
   const KeyForm form = key_form(n.rotary);
@@ -591,11 +680,11 @@ hipError_t launch_kv_append(const KvLayout& L, const NewRows& n, const int64_t* 
   q.stream = q.many && q.lines && rows * (hq + 2 * L.desc.num_kv_heads) * kDim * 2 >= kStreamBytes;
   auto quads = [&](auto key_form) {
     constexpr int kForm = decltype(key_form)::value;
-    return !q.many    ? kv_append_kernel<kForm, 1, kCached>
-           : q.stream ? kv_append_kernel<kForm, 4, kReadsWrites>
-                      : kv_append_kernel<kForm, 4, kCached>;
+    return !q.many    ? kv_append_kernel<kForm, 1, kCached, Norms>
+           : q.stream ? kv_append_kernel<kForm, 4, kReadsWrites, Norms>
+                      : kv_append_kernel<kForm, 4, kCached, Norms>;
   };
-  auto k = form == kAnyPairs     ? kv_append_kernel<kAnyPairs, 1, kCached>
+  auto k = form == kAnyPairs     ? kv_append_kernel<kAnyPairs, 1, kCached, Norms>
            : form == kInterQuads ? quads(std::integral_constant<int, kInterQuads>{})
                                  : quads(std::integral_constant<int, kHalfQuads>{});
   // Rows that one launch takes: at most kMaxBlocks blocks of either kind.
@@ -620,11 +709,32 @@ hipError_t launch_kv_append(const KvLayout& L, const NewRows& n, const int64_t* 
       Q.slot_end = A.slot_end;
       blocks += q.blocks(n_rows) * Q.y_blocks;
     }
-    hipLaunchKernelGGL(k, dim3(unsigned(blocks)), dim3(kThreads), 0, s, rot, A, Q);
+    hipLaunchKernelGGL(k, dim3(unsigned(blocks)), dim3(kThreads), 0, s, rot, A, Q, norms);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
+}
+
+}  // namespace
+
+hipError_t launch_kv_append(const KvLayout& L, const NewRows& n, const int64_t* slots,
+                            int64_t rows, int32_t hq, void* q_out, hipStream_t s) {
+  return append_rows(L, n, slots, rows, hq, q_out, NoNorms{}, s);
+}
+
+hipError_t launch_kv_append_norm(const KvLayout& L, const NewRows& n, const RowNorms& norms, const int64_t* slots,
+                                 int64_t rows, int32_t hq, void* q_out, hipStream_t s) {
+  return append_rows(L, n, slots, rows, hq, q_out, norms, s);
+}
+
+hipError_t launch_norm_rotary(const Rotary& r, const RotaryRows& q, const RotaryRows& k, const RowNorms& norms,
+                              hipStream_t s) {
+  switch (q.dtype) {
+    case LIBRA_DTYPE_BF16: return apply_norm<Bf16>(r, q, k, norms, s);
+    case LIBRA_DTYPE_FP16: return apply_norm<Fp16>(r, q, k, norms, s);
+    default: return apply_norm<Fp32>(r, q, k, norms, s);
+  }
 }
 
 hipError_t launch_cache_write_rotary(const KvLayout& L, const Plan& P, const void* ws,

@@ -46,13 +46,16 @@ EXPORTS = ("libra_status_string", "libra_last_error", "libra_alloc_calls",
            "libra_decode_attn", "libra_decode_attn_noalloc", "libra_append_attn",
            "libra_rotary_create", "libra_rotary_destroy", "libra_rotary_get",
            "libra_rotary_apply", "libra_kv_append", "libra_append_attn_rotary",
+           "libra_kv_map", "libra_kv_accept", "libra_qk_norm_rotary",
+           "libra_qk_norm_rotary_workspace_bytes", "libra_qk_norm_rotary_backward",
+           "libra_kv_append_norm", "libra_tree_attn_workspace_bytes", "libra_tree_attn",
            "libra_profile_enable",
            "libra_profile_collect", "libra_ce_fit", "libra_ce_mape", "libra_ce_poly_sum",
            "libra_rollout_dp", "libra_trie_create", "libra_trie_destroy", "libra_trie_insert",
            "libra_trie_lookup", "libra_route_bucket")
 TP_SLOTS = {1: 0, 2: 1, 4: 2, 8: 3}
 KERNEL_KINDS = ("pack", "unpack", "gather", "cache_write", "decode", "merge", "chunk", "upload",
-                "copy_out", "copy_in", "rotary")
+                "copy_out", "copy_in", "rotary", "tables", "tree", "accept")
 
 
 class LibraError(RuntimeError):
@@ -97,6 +100,15 @@ class RotaryDesc(ctypes.Structure):
                 ("frequencies", ctypes.POINTER(ctypes.c_double))]
 
 
+class NormHeads(ctypes.Structure):
+    _fields_ = [("x", ctypes.c_void_p), ("x_row_stride", ctypes.c_int64),
+                ("x_head_stride", ctypes.c_int64), ("num_heads", ctypes.c_int32),
+                ("weight", ctypes.c_void_p), ("out", ctypes.c_void_p),
+                ("out_row_stride", ctypes.c_int64), ("out_head_stride", ctypes.c_int64),
+                ("grad", ctypes.c_void_p), ("grad_row_stride", ctypes.c_int64),
+                ("grad_head_stride", ctypes.c_int64), ("weight_grad", ctypes.c_void_p)]
+
+
 class CePoly(ctypes.Structure):
     _fields_ = [("gamma", ctypes.c_double), ("eta", ctypes.c_double), ("theta", ctypes.c_double)]
 
@@ -131,6 +143,7 @@ def load() -> ctypes.CDLL:
     I32P = ctypes.POINTER(ctypes.c_int32)
     I64P = ctypes.POINTER(ctypes.c_int64)
     DP = ctypes.POINTER(ctypes.c_double)
+    NH = ctypes.POINTER(NormHeads)
     sig = {
         "libra_status_string": (ctypes.c_char_p, [ctypes.c_int]),
         "libra_last_error": (ctypes.c_char_p, []),
@@ -169,6 +182,19 @@ def load() -> ctypes.CDLL:
         "libra_append_attn_rotary": (ctypes.c_int, [P, P, P, P, I64, P, I64, P, I64, P, I64, I32, P,
                                                     I32, I32, I32, ctypes.c_float, I32, P, SZ, P,
                                                     P, P]),
+        "libra_kv_map": (ctypes.c_int, [I32, P, P, P, P, I32, P, I64, P, P, I64, P, P, P, P, P, P,
+                                        P]),
+        "libra_kv_accept": (ctypes.c_int, [P, I32, P, P, I32, P, P, I32, P]),
+        "libra_qk_norm_rotary": (ctypes.c_int, [P, I32, I32, ctypes.c_float, P, I64, I32, NH, NH,
+                                                P]),
+        "libra_qk_norm_rotary_workspace_bytes": (SZ, [I64, I32, I32, I32]),
+        "libra_qk_norm_rotary_backward": (ctypes.c_int, [P, I32, I32, ctypes.c_float, P, I64, I32,
+                                                         NH, NH, P, SZ, P]),
+        "libra_kv_append_norm": (ctypes.c_int, [P, P, I32, ctypes.c_float, P, P, I64, P, I64, I32,
+                                                P, P, I64, P, P, I64, I32, P, P]),
+        "libra_tree_attn_workspace_bytes": (SZ, [I64, I32, I32, I32]),
+        "libra_tree_attn": (ctypes.c_int, [P, P, I64, P, P, P, I32, P, I32, I32, I32,
+                                           ctypes.c_float, P, SZ, P, P, P]),
         "libra_profile_enable": (ctypes.c_int, [ctypes.c_int]),
         "libra_profile_collect": (ctypes.c_int, [ctypes.POINTER(KernelTimes)]),
         "libra_ce_fit": (ctypes.c_int, [DP, DP, I32, ctypes.POINTER(CePoly)]),
@@ -576,6 +602,182 @@ def libra_append_attn_rotary(layout: int, plan: int, rotary: int, positions, q, 
                                                    "out", device),
                                            _buffer(lse, _FLOAT32, rows * num_q_heads, "lse", device),
                                            _stream(stream, device)), "libra_append_attn_rotary")
+
+
+def libra_kv_map(prior_lens, new_lens, held_pages, block_table, bt_stride: int, free_pages,
+                 num_free, depths, slots, positions, row_starts, held_out, num_free_out, refused,
+                 stream=None):
+    """Block tables [batch, bt_stride], slots [rows] (int64) and positions [rows] from request
+    lengths [batch] on the GPU; everything else int32.  free_pages: the whole buffer of the stack,
+    num_free [1] its height; row_starts [batch + 1]; depths [rows] or None.  held_out may be
+    held_pages, num_free_out num_free."""
+    device = torch.cuda.current_device()
+    i32, batch, rows = torch.int32, prior_lens.numel(), slots.numel()
+    capacity = free_pages.numel()
+    _check(load().libra_kv_map(batch, _vector(prior_lens, i32, batch, "prior_lens", device),
+                               _vector(new_lens, i32, batch, "new_lens", device),
+                               _vector(held_pages, i32, batch, "held_pages", device),
+                               _buffer(block_table, _INT32, batch * bt_stride, "block_table", device),
+                               bt_stride, _vector(free_pages, i32, capacity, "free_pages", device),
+                               capacity, _vector(num_free, i32, 1, "num_free", device),
+                               _vector(depths, i32, rows, "depths", device), rows,
+                               _vector(slots, torch.int64, rows, "slots", device),
+                               _vector(positions, i32, rows, "positions", device),
+                               _vector(row_starts, i32, batch + 1, "row_starts", device),
+                               _vector(held_out, i32, batch, "held_out", device),
+                               _vector(num_free_out, i32, 1, "num_free_out", device),
+                               _vector(refused, i32, batch, "refused", device),
+                               _stream(stream, device)), "libra_kv_map")
+
+
+def libra_kv_accept(layout: int, prior_lens, accepted, counts, block_table, bt_stride: int,
+                    stream=None):
+    """Moves each request's accepted nodes [batch, max_accepted] (ascending; counts [batch] of
+    them) to the tokens behind its prior_lens [batch]; all int32."""
+    device = torch.cuda.current_device()
+    batch = prior_lens.numel()
+    if accepted.dim() != 2:
+        raise ValueError("accepted: [batch, max_accepted] expected")
+    most = accepted.shape[1]
+    _check(load().libra_kv_accept(layout, batch,
+                                  _vector(prior_lens, torch.int32, batch, "prior_lens", device),
+                                  _vector(accepted, torch.int32, batch * most, "accepted", device),
+                                  most, _vector(counts, torch.int32, batch, "counts", device),
+                                  _buffer(block_table, _INT32, batch * bt_stride, "block_table",
+                                          device), bt_stride, _stream(stream, device)),
+           "libra_kv_accept")
+
+
+def _heads(t, shape, dtype, what: str, device: int):
+    """(pointer, row stride, head stride) of [rows, heads, head_dim], any strides of the first two."""
+    if t.get_device() != device or t.dtype is not dtype or t.shape != shape:
+        raise ValueError(f"{what}: {dtype} tensor of {tuple(shape)} on the current device expected")
+    row, head, one = t.stride()
+    if one != 1 and shape[2] > 1:
+        raise ValueError(f"{what}: the channels of a head must be contiguous")
+    return t.data_ptr(), row, head
+
+
+def _norm_heads(x, weight, out, grad, weight_grad, dtype, weight_dtype, what: str, device: int):
+    if x is None:
+        return None
+    xs = _heads(x, x.shape, dtype, what, device)
+    os = _heads(out, x.shape, dtype, f"{what}'s output", device)
+    gs = (None, 0, 0) if grad is None else _heads(grad, x.shape, dtype, f"{what}'s gradient", device)
+    dim = x.shape[2]
+    return NormHeads(*xs, x.shape[1], _vector(weight, weight_dtype, dim, f"{what}'s weight", device),
+                     *os, *gs, _vector(weight_grad, torch.float32, dim, f"{what}'s weight gradient",
+                                       device))
+
+
+def _norm_call(q, k, q_weight, k_weight, device: int):
+    """(rows, head_dim, type, its code, the weights' type, its code) of a call's tensors."""
+    x, w = (q, q_weight) if q is not None else (k, k_weight)
+    if x is None or x.dim() != 3 or w is None:
+        raise ValueError("[rows, heads, head_dim] queries or keys with their weight expected")
+    if k is not None and (k.dim() != 3 or k.shape[0] != x.shape[0] or k.shape[2] != x.shape[2]):
+        raise ValueError("queries and keys of the same rows and head size expected")
+    code, w_code = _ROTARY_DTYPES.get(x.dtype), _ROTARY_DTYPES.get(w.dtype)
+    if code is None or w_code is None:
+        raise ValueError("bf16, fp16 or fp32 tensors expected")
+    return x.shape[0], x.shape[2], x.dtype, code, w.dtype, w_code
+
+
+def libra_qk_norm_rotary(rotary: int, q, k, q_weight, k_weight, eps: float, positions, q_out, k_out,
+                         stream=None):
+    """Normalises q and k [rows, heads, head_dim] (bf16, fp16 or fp32; any row and head strides; one
+    may be None) head by head, weights them [head_dim] and turns them by positions [rows] (int32)
+    into q_out and k_out, which may be q and k."""
+    device = torch.cuda.current_device()
+    rows, dim, dtype, code, wt, w_code = _norm_call(q, k, q_weight, k_weight, device)
+    hq = _norm_heads(q, q_weight, q_out, None, None, dtype, wt, "q", device)
+    hk = _norm_heads(k, k_weight, k_out, None, None, dtype, wt, "k", device)
+    _check(load().libra_qk_norm_rotary(rotary, code, w_code, eps,
+                                       _vector(positions, torch.int32, rows, "positions", device),
+                                       rows, dim, hq, hk, _stream(stream, device)),
+           "libra_qk_norm_rotary")
+
+
+def libra_qk_norm_rotary_workspace_bytes(rows: int, num_q_heads: int, num_k_heads: int,
+                                         head_dim: int) -> int:
+    return load().libra_qk_norm_rotary_workspace_bytes(rows, num_q_heads, num_k_heads, head_dim)
+
+
+def libra_qk_norm_rotary_backward(rotary: int, q_grad, k_grad, q, k, q_weight, k_weight, eps: float,
+                                  positions, dq, dk, dq_weight, dk_weight, workspace, stream=None):
+    """libra_qk_norm_rotary's gradients: from those of its outputs to dq and dk (of q's and k's shape
+    and type, which may be q and k, or q_grad and k_grad) and to the weights' (float32, or None)."""
+    device = torch.cuda.current_device()
+    rows, dim, dtype, code, wt, w_code = _norm_call(q, k, q_weight, k_weight, device)
+    if (q is None) != (q_grad is None) or (k is None) != (k_grad is None):
+        raise ValueError("a gradient for each of q and k expected")
+    hq = _norm_heads(q, q_weight, dq, q_grad, dq_weight, dtype, wt, "q", device)
+    hk = _norm_heads(k, k_weight, dk, k_grad, dk_weight, dtype, wt, "k", device)
+    ws_bytes = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    _check(load().libra_qk_norm_rotary_backward(rotary, code, w_code, eps,
+                                                _vector(positions, torch.int32, rows, "positions",
+                                                        device), rows, dim, hq, hk,
+                                                _buffer(workspace, None, 0, "workspace", device),
+                                                ws_bytes, _stream(stream, device)),
+           "libra_qk_norm_rotary_backward")
+
+
+def libra_kv_append_norm(layout: int, rotary: int, positions, slots, q, k_new, v_new, q_weight,
+                         k_weight, eps: float, q_out, stream=None):
+    """libra_kv_append with q and k_new normalised head by head and weighted (q_weight, k_weight:
+    [128], bf16, fp16 or fp32) before they are turned."""
+    device = torch.cuda.current_device()
+    rows = slots.numel()
+    w_code = None if k_weight is None else _ROTARY_DTYPES.get(k_weight.dtype)
+    if w_code is None:
+        raise ValueError("k_weight: bf16, fp16 or fp32 tensor expected")
+    qp, qs, hq = _rows(q, rows, None, "q", device)
+    kp, ks, hkv = _rows(k_new, rows, None, "k_new", device)
+    vp, vs, _ = _rows(v_new, rows, hkv, "v_new", device)
+    qo = None
+    if q_out is not None:
+        qo, stride, _ = _rows(q_out, rows, hq, "q_out", device)
+        if stride != hq * HEAD_DIM:
+            raise ValueError("q_out: dense rows expected")
+    _check(load().libra_kv_append_norm(layout, rotary, w_code, eps,
+                                       _vector(positions, torch.int32, rows, "positions", device),
+                                       _vector(slots, torch.int64, rows, "slots", device), rows, qp,
+                                       qs, hq, _vector(q_weight, k_weight.dtype, HEAD_DIM, "q_weight",
+                                                       device), kp, ks,
+                                       _vector(k_weight, k_weight.dtype, HEAD_DIM, "k_weight", device),
+                                       vp, vs, hkv, qo, _stream(stream, device)),
+           "libra_kv_append_norm")
+
+
+def libra_tree_attn_workspace_bytes(rows: int, batch: int, num_q_heads: int,
+                                    num_kv_heads: int) -> int:
+    return load().libra_tree_attn_workspace_bytes(rows, batch, num_q_heads, num_kv_heads)
+
+
+def libra_tree_attn(layout: int, q, prior_lens, row_starts, mask, block_table, bt_stride: int,
+                    num_q_heads: int, scale: float, workspace, out, lse=None, stream=None):
+    """Attention of drafted nodes: q and out [rows, num_q_heads, 128] bf16, prior_lens [batch] and
+    row_starts [batch + 1] int32, mask [rows, words] int32 (bit j: the row sees node j; None: a chain),
+    block_table int32 [batch, bt_stride], lse float32 [rows, num_q_heads] or None."""
+    device = torch.cuda.current_device()
+    rows, batch = q.shape[0], prior_lens.numel()
+    words = 0
+    if mask is not None:
+        if mask.dim() != 2:
+            raise ValueError("mask: [rows, words] expected")
+        words = mask.shape[1]
+    size = rows * num_q_heads * HEAD_DIM
+    _check(load().libra_tree_attn(layout, _buffer(q, _BF16_BITS, size, "q", device), rows,
+                                  _vector(prior_lens, torch.int32, batch, "prior_lens", device),
+                                  _vector(row_starts, torch.int32, batch + 1, "row_starts", device),
+                                  _vector(mask, torch.int32, rows * words, "mask", device), words,
+                                  _buffer(block_table, _INT32, batch * bt_stride, "block_table",
+                                          device), bt_stride, batch, num_q_heads, scale,
+                                  _buffer(workspace, None, 0, "workspace", device),
+                                  workspace.numel() * workspace.element_size(),
+                                  _buffer(out, _BF16_BITS, size, "out", device),
+                                  _buffer(lse, _FLOAT32, rows * num_q_heads, "lse", device),
+                                  _stream(stream, device)), "libra_tree_attn")
 
 
 def libra_profile_enable(enable: bool = True) -> None:
