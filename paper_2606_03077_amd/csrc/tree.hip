@@ -43,12 +43,8 @@ typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
-// Uniform reads of data that no launch here writes go through the scalar cache, whose counter is
-// another than the copies'.
-typedef const int32_t __attribute__((address_space(4))) * ScalarInts;
 
 constexpr int kStepKeys = 32;
-constexpr int kStages = 4;
 constexpr int kMinSteps = 4;
 constexpr int kTau = 8;
 constexpr float kSumTau = float(1 << kTau);
@@ -56,9 +52,9 @@ constexpr int kMaskWords = 8;
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
-// Workgroups of the launch: all that run at once.
+// Workgroups of the launch: all that run at once, by their LDS.
 constexpr int kCus = 256;
-constexpr int groups_of(int waves) { return waves == 8 ? kCus : 2 * kCus; }
+constexpr int groups_of(int waves) { return kCus * (waves == 8 ? 1 : waves == 4 ? 2 : 3); }
 
 __device__ __forceinline__ bf16x8 as_bf16x8(uint4 x) { return __builtin_bit_cast(bf16x8, x); }
 __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
@@ -86,9 +82,10 @@ struct TreeArgs {
   float* lse;
   float* part_o;
   float* part_lse;
+  int32_t* splits;
   int64_t stride;
-  int64_t rows;
   uint32_t last_page;
+  int rows, most;  // query rows, tokens that a row of the block table can hold
   int batch, hkv, hq, group, mask_words;
   float sl2;
 };
@@ -96,93 +93,291 @@ struct TreeArgs {
 // A sequence's sizes, kept inside the rows and the block table whatever the caller's memory holds.
 struct Seq {
   int prior, nodes, row0, len, steps, tiles;
-  // The steps of all its items: one a tile and KV head.
-  __device__ __forceinline__ int64_t cost(const TreeArgs& A) const { return int64_t(tiles) * A.hkv * steps; }
 };
-template <int kRows, class Ints>
-__device__ __forceinline__ Seq load_seq(const TreeArgs& A, Ints prior, Ints starts, int b) {
+template <int kRows>
+__device__ __forceinline__ Seq make_seq(const TreeArgs& A, int prior, int start, int end) {
   Seq s;
-  const int64_t r0 = min(max(int64_t(starts[b]), int64_t(0)), A.rows);
-  const int64_t r1 = min(max(int64_t(starts[b + 1]), r0), A.rows);
-  s.row0 = int(r0), s.nodes = int(r1 - r0);
-  const int64_t most = min(A.stride * kPage, int64_t(INT32_MAX) - 64);
-  s.prior = int(min(int64_t(max(prior[b], 0)), most));
-  s.len = int(min(int64_t(s.prior) + s.nodes, most));
+  s.row0 = min(max(start, 0), A.rows);
+  s.nodes = min(max(end, s.row0), A.rows) - s.row0;
+  s.prior = min(max(prior, 0), A.most);
+  s.len = int(min(uint32_t(s.prior) + uint32_t(s.nodes), uint32_t(A.most)));
   s.steps = (s.len + kStepKeys - 1) / kStepKeys;
   s.tiles = (s.nodes * A.group + kRows - 1) / kRows;  // rows * hq fits 32 bits
   return s;
 }
 
-// The launch's division: total steps, and steps per workgroup.
+// Lane l holds the lengths of sequence first + l, loaded at once: the sequences of a range are then
+// found without a chain of loads.
 template <int kRows>
-__device__ __forceinline__ int64_t total_steps(const TreeArgs& A, int lane) {
-  int64_t sum = 0;
-  for (int b = lane; b < A.batch; b += 64) sum += load_seq<kRows>(A, A.prior, A.starts, b).cost(A);
+struct Window {
+  int first, prior, start, end;
+  __device__ __forceinline__ void load(const TreeArgs& A, int from, int lane) {
+    first = from;
+    const int b = min(from + lane, A.batch - 1);
+    prior = A.prior[b], start = A.starts[b], end = A.starts[b + 1];
+  }
+  // The steps of this lane's sequence's items, one a tile and KV head.
+  __device__ __forceinline__ int64_t cost(const TreeArgs& A, int lane) const {
+    const Seq s = make_seq<kRows>(A, prior, start, end);
+    return first + lane < A.batch ? int64_t(s.tiles) * A.hkv * s.steps : 0;
+  }
+  __device__ __forceinline__ Seq get(const TreeArgs& A, int b, int lane) {
+    if (b >= first + 64) load(A, b, lane);
+    const int l = b - first;
+    return make_seq<kRows>(A, __builtin_amdgcn_readlane(prior, l), __builtin_amdgcn_readlane(start, l),
+                           __builtin_amdgcn_readlane(end, l));
+  }
+};
+
+__device__ __forceinline__ int64_t wave_sum(int64_t x) {
 #pragma unroll
-  for (int n = 32; n; n >>= 1) sum += __shfl_xor(sum, n);
-  return uniform64(sum);
-}
-__device__ __forceinline__ int64_t steps_each(int64_t total, int groups) {
-  return max((total + groups - 1) / groups, int64_t(kMinSteps));
+  for (int n = 32; n; n >>= 1) x += __shfl_xor(x, n);
+  return uniform64(x);
 }
 
 // A place in the launch's steps.
 template <int kRows>
 struct Cursor {
+  Window<kRows> window;
   Seq seq;
   int b, g, tile, step;
-  __device__ __forceinline__ void load(const TreeArgs& A) {
-    seq = load_seq<kRows>(A, (ScalarInts)A.prior, (ScalarInts)A.starts, b);
-  }
-  // The sequence that holds step `at`, which is below the total.
-  __device__ __forceinline__ void seek(const TreeArgs& A, int64_t at, int lane) {
+  // To the workgroup's first step; returns how many it has (0: none).
+  __device__ __forceinline__ int start(const TreeArgs& A, int w, int groups, int lane) {
+    int64_t total = 0;
+    for (int b0 = 0; b0 < A.batch; b0 += 64) {
+      window.load(A, b0, lane);
+      total += wave_sum(window.cost(A, lane));
+    }
+    const int64_t each = max((total + groups - 1) / groups, int64_t(kMinSteps));
+    const int64_t begin = w * each;
+    if (begin >= total) return 0;
     int64_t before = 0;
     for (int b0 = 0;; b0 += 64) {
-      const int i = b0 + lane;
-      const int64_t cost = i < A.batch ? load_seq<kRows>(A, A.prior, A.starts, i).cost(A) : 0;
+      if (window.first != b0) window.load(A, b0, lane);
+      const int64_t cost = window.cost(A, lane);
       int64_t upto = cost;
 #pragma unroll
       for (int n = 1; n < 64; n <<= 1) {
         const int64_t y = __shfl_up(upto, n);
         if (lane >= n) upto += y;
       }
-      const uint64_t beyond = __ballot(before + upto > at);
-      if (beyond || b0 + 64 >= A.batch) {
-        const int l = beyond ? __builtin_ctzll(beyond) : 0;
+      const uint64_t beyond = __ballot(before + upto > begin);
+      if (beyond) {
+        const int l = __builtin_ctzll(beyond);
         b = uniform(b0 + l);
-        load(A);
-        const int64_t in_seq = at - uniform64(before + __shfl(upto - cost, l));
+        seq = window.get(A, b, lane);
+        const int64_t in_seq = begin - before - uniform64(__shfl(upto - cost, l));
         const int item = uniform(int(in_seq / seq.steps));
         step = uniform(int(in_seq - int64_t(item) * seq.steps));
         g = uniform(item / seq.tiles);
         tile = item - g * seq.tiles;
-        return;
+        return int(min(each, total - begin));
       }
       before += uniform64(__shfl(upto, 63));
     }
   }
-  // To the next step; not past the launch's last one.
-  __device__ __forceinline__ void advance(const TreeArgs& A) {
-    if (++step < seq.steps) return;
+  // To the next sequence that has nodes.
+  __device__ __forceinline__ void next_seq(const TreeArgs& A, int lane) {
+    g = tile = step = 0;
+    do {
+      ++b;
+      seq = window.get(A, b, lane);
+    } while (seq.tiles == 0 && b + 1 < A.batch);
+  }
+  // To the first step of the next item; not past the launch's last one.
+  __device__ __forceinline__ void next_item(const TreeArgs& A, int lane) {
     step = 0;
     if (++tile < seq.tiles) return;
     tile = 0;
     if (++g < A.hkv) return;
-    g = 0;
-    do {
-      ++b;
-      load(A);
-    } while (seq.tiles == 0 && b + 1 < A.batch);
+    next_seq(A, lane);
   }
 };
 
+// What the merge gets to know of an item that workgroup w begins and does not end.
+struct Split {
+  int parts, row0, nodes, g, tile;
+};
+constexpr int kSplitInts = 8;
+
+// The rows of a wave: their running maximum and sum, and the unnormalised output, transposed: lane
+// (col, hh) holds channels 32 cb + 8 e + 4 hh .. + 3 of row col.
+struct Rows {
+  f32x16 acc[4];
+  float m, l;
+  __device__ __forceinline__ void clear() {
+    m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int cb = 0; cb < 4; ++cb)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) acc[cb][r] = 0.f;
+  }
+};
+
+// A step's probabilities from its scores, against the running maximum.  While a row has seen no
+// finite score the offset is the largest float: scores of -inf give 0, and the first finite one
+// infinity, which moves the maximum, as any sum above 2^kTau does.
+__device__ __forceinline__ void soften(Rows& R, const f32x16& sc, float sl2, bf16x8 (&pr)[2]) {
+  float p[16], ps;
+  auto take = [&]() {
+    const float neg_m = R.m == -INFINITY ? FLT_MAX : -R.m;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(sc[r], sl2, neg_m));
+    const float t0 = (p[0] + p[1]) + (p[2] + p[3]), t1 = (p[4] + p[5]) + (p[6] + p[7]);
+    const float t2 = (p[8] + p[9]) + (p[10] + p[11]), t3 = (p[12] + p[13]) + (p[14] + p[15]);
+    ps = (t0 + t1) + (t2 + t3);
+  };
+  take();
+  if (__ballot(!(ps <= kSumTau))) {
+    float mloc = sc[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) mloc = fmaxf(mloc, sc[r]);
+    float mc = fmaxf(mloc * sl2, R.m);
+    mc = fmaxf(mc, __shfl_xor(mc, 32));
+    const float alpha = R.m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(R.m - mc);
+    R.l *= alpha;
+#pragma unroll
+    for (int cb = 0; cb < 4; ++cb) R.acc[cb] *= alpha;
+    R.m = mc;
+    take();
+  }
+  R.l += ps;
+  pr[0] = as_bf16x8(make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]),
+                               pack_bf16x2(p[4], p[5]), pack_bf16x2(p[6], p[7])));
+  pr[1] = as_bf16x8(make_uint4(pack_bf16x2(p[8], p[9]), pack_bf16x2(p[10], p[11]),
+                               pack_bf16x2(p[12], p[13]), pack_bf16x2(p[14], p[15])));
+}
+
+// Which of a step's keys the row sees (bit i: key key0 + i), in a step that reaches past the cached
+// tokens.  bits: the row's mask words in LDS.
+__device__ __forceinline__ uint32_t seen_keys(const TreeArgs& A, const Seq& s, const uint32_t* bits, int node,
+                                              int key0) {
+  uint32_t sees;
+  const int d = key0 - s.prior;  // > -32: the first key's node
+  if (!A.mask) {
+    const int lim = node - d;
+    sees = lim >= 31 ? ~0u : lim < 0 ? 0u : (2u << lim) - 1;
+  } else if (d < 0) {
+    sees = bits[0] << -d | ((1u << -d) - 1);
+  } else {
+    const int i = d >> 5, sh = d & 31;
+    const uint32_t w0 = i < A.mask_words ? bits[i] : 0;
+    const uint32_t w1 = i + 1 < A.mask_words ? bits[i + 1] : 0;
+    sees = uint32_t((uint64_t(w1) << 32 | w0) >> sh);
+  }
+  const int left = s.len - key0;
+  if (left < 32) sees &= (1u << left) - 1;
+  return node < s.nodes ? sees : 0;
+}
+__device__ __forceinline__ void mask_scores(uint32_t sees, int hh, f32x16& sc) {
+  sees >>= 4 * hh;
+#pragma unroll
+  for (int r = 0; r < 16; ++r)
+    if (!(sees >> acc_row(r, 0) & 1)) sc[r] = -INFINITY;
+}
+
+// The products of a step's values, v[4 j + cb] being page j's of channel block cb.
+__device__ __forceinline__ void add_values(Rows& R, const uint4 (&v)[8], const bf16x8 (&pr)[2]) {
+#pragma unroll
+  for (int c = 0; c < 8; ++c)
+    R.acc[c & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(v[c]), pr[c >> 2], R.acc[c & 3], 0, 0, 0);
+}
+
+// Sets the top bit of each half whose bf16 is infinite or NaN (and other bits).
+__device__ __forceinline__ uint32_t special_bits(uint32_t x) { return (x & 0x7F807F80u) + 0x00800080u; }
+
+// Zeroes values in slots past the end, `valid` keys from the step's first; whether any that is left
+// is not finite.
+__device__ __forceinline__ bool trim_values(uint4 (&v)[8], int valid, int hh) {
+  uint32_t special = 0;
+#pragma unroll
+  for (int j = 0; j < 2; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int s0 = j * kPage + 8 * (e / 2) + 4 * hh + 2 * (e % 2);
+      const uint32_t keep = (s0 < valid ? 0x0000FFFFu : 0u) | (s0 + 1 < valid ? 0xFFFF0000u : 0u);
+#pragma unroll
+      for (int cb = 0; cb < 4; ++cb) {
+        uint32_t& x = reinterpret_cast<uint32_t*>(&v[4 * j + cb])[e];
+        x &= keep;
+        special |= special_bits(x);
+      }
+    }
+  return __ballot((special & 0x80008000u) != 0) != 0;
+}
+
+// Where some values of a masked step are not finite, a product with a probability of 0 would be NaN:
+// they are added one by one to the rows that see them (slow, and rare), and the products take
+// zeros in their place.  tiles: the two pages' V tiles, in LDS or memory.
+__device__ __forceinline__ void finite_values(uint4 (&v)[8]) {
+#pragma unroll
+  for (int c = 0; c < 8; ++c)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      uint32_t& x = reinterpret_cast<uint32_t*>(&v[c])[e];
+      x &= ~((special_bits(x) >> 15 & 0x00010001u) * 0xFFFFu);
+    }
+}
+template <class Tile>
+__device__ __forceinline__ void add_special_values(Rows& R, uint32_t sees, int hh, Tile tile0, Tile tile1) {
+#pragma unroll 1
+  for (int key = 0; key < kStepKeys; ++key) {
+    const bool seen = sees >> key & 1;
+    const int slot = key & (kPage - 1);
+    const Tile t = (key < kPage ? tile0 : tile1) + 1024 * (slot >> 2 & 1) + 32 * hh + 4 * (slot >> 3) + (slot & 3);
+#pragma unroll
+    for (int cb = 0; cb < 4; ++cb) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const uint32_t x = t[8 * (32 * cb + 8 * (r / 4) + r % 4)];
+        R.acc[cb][r] += seen && (x & 0x7F80u) == 0x7F80u ? __uint_as_float(x << 16) : 0.f;
+      }
+      __builtin_amdgcn_sched_barrier(0);  // few registers, rather than many loads at once
+    }
+  }
+}
+
+// The row's query as the score products' operands, and its mask words.
+__device__ __forceinline__ void load_query(const TreeArgs& A, const Seq& s, int g, int node, int head, int hh,
+                                           bf16x8 (&qop)[8], uint32_t* bits) {
+  const bool ok = node < s.nodes;
+  const uint4* qrow = reinterpret_cast<const uint4*>(
+      A.q + (size_t(s.row0 + (ok ? node : 0)) * A.hq + size_t(g) * A.group + head) * kDim);
+#pragma unroll
+  for (int c = 0; c < 8; ++c) qop[c] = as_bf16x8(ok ? qrow[2 * c + hh] : make_uint4(0, 0, 0, 0));
+  if (A.mask)
+    for (int i = hh; i < A.mask_words; i += 2)
+      bits[i] = ok ? A.mask[size_t(s.row0 + node) * A.mask_words + i] : 0;
+}
+
+// One int per lane straight into LDS, lane after lane.
+__device__ __forceinline__ void copy_lds_dword(const int32_t* src, int32_t* dst) {
+  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off"
+               :
+               : "s"(uint32_t(reinterpret_cast<uintptr_t>(dst))), "v"(src)
+               : "memory", "m0");
+}
+__device__ __forceinline__ void wave_sync() {  // LDS operations of one wave complete in order
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+}
+
+// A tile's waves share each step's K and V through LDS.
 template <int kWaves>
-__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(kWaves >= 4 ? 2 : 1, 2)))
-void tree_kernel(TreeArgs A) {
+struct Ring {
+  static constexpr int kStages = kWaves == 8 ? 8 : kWaves == 4 ? 4 : 3;
+  static constexpr int kCopies = 16 / kWaves;  // of 1 KiB, per wave and step
+};
+
+template <int kWaves>
+__global__ __launch_bounds__(64 * kWaves) __attribute__((amdgpu_waves_per_eu(kWaves > 1 ? 2 : 1, 2)))
+void tree_ring_kernel(TreeArgs A) {
   constexpr int kRows = 32 * kWaves;
-  constexpr int kCopies = 16 / kWaves;  // of 1 KiB, per wave and step
+  constexpr int kStages = Ring<kWaves>::kStages;
+  constexpr int kCopies = Ring<kWaves>::kCopies;
   __shared__ __align__(16) uint4 ring[kStages][4][256];  // K of the step's two pages, V of them
-  __shared__ uint32_t bits[kWaves][32][kMaskWords + 1];
+  __shared__ uint32_t bits[kRows][kMaskWords + 1];
+  __shared__ int32_t ids[kWaves][2][3][64];  // of two turns of 64 steps: a step's page ids and KV head
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = uniform(tid >> 6);
   const int col = lane & 31, hh = lane >> 5;
@@ -191,385 +386,309 @@ void tree_kernel(TreeArgs A) {
   // Neighbouring ranges on one XCD: workgroup w runs on XCD w % 8.
   const int per_xcd = int(gridDim.x) / kNumXcds;
   const int w = int(blockIdx.x) % kNumXcds * per_xcd + int(blockIdx.x) / kNumXcds;
-  const int64_t total = total_steps<kRows>(A, lane);
-  const int64_t each = steps_each(total, int(gridDim.x));
-  const int64_t begin = w * each;
-  if (begin >= total) return;
-  const int n_steps = int(min(each, total - begin));
+  int32_t* const split = A.splits + w * kSplitInts;
+  Cursor<kRows> at;
+  const int n_steps = at.start(A, w, int(gridDim.x), lane);
+  if (tid == 0) split[0] = 0;  // unless an item is begun and not ended, below
+  if (n_steps == 0) return;
 
-  Cursor<kRows> at, ahead;
-  at.seek(A, begin, lane);
-  ahead = at;
-  const uint32_t page_bytes = uint32_t(A.hkv) * kTileBytes;
-  // The page ids of the step that is copied next, loaded a step earlier.
-  int id[2];
-  auto load_ids = [&]() {
-    const ScalarInts row = (ScalarInts)A.table + int64_t(ahead.b) * A.stride;
-    const int p = 2 * ahead.step, last = (ahead.seq.len - 1) / kPage;
-    id[0] = row[p];
-    id[1] = row[min(p + 1, last)];
+  // What the copies need of each step, page ids and KV head, 64 steps at a time: lane l finds
+  // step l's place among the sequences and copies its two ids into LDS, asynchronously like the tiles,
+  // 64 steps ahead, so that no step waits for them.
+  Cursor<kRows> fill = at;
+  int filled = 0;
+  auto fill_ids = [&]() {
+    int32_t(&to)[3][64] = ids[wave][filled >> 6 & 1];
+    const int32_t *id0 = A.table, *id1 = A.table;
+    int head = 0, done = 0;
+    const int want = min(n_steps - filled, 64);
+    while (true) {  // the sequences of these steps
+      const Seq& s = fill.seq;
+      const int64_t left = (int64_t(A.hkv - fill.g) * s.tiles - fill.tile) * s.steps - fill.step;
+      const int take = int(min(left, int64_t(want - done)));
+      const int x = lane - done;
+      if (x >= 0 && x < take) {
+        const uint32_t item = uint32_t(fill.step + x) / uint32_t(s.steps);
+        const int step = fill.step + x - int(item) * s.steps;
+        head = fill.g + int((uint32_t(fill.tile) + item) / uint32_t(s.tiles));
+        const int32_t* row = A.table + fill.b * A.stride;
+        id0 = row + 2 * step;
+        id1 = row + min(2 * step + 1, (s.len - 1) / kPage);
+      }
+      done += take;
+      if (done < want) {
+        fill.next_seq(A, lane);
+        continue;
+      }
+      const uint32_t items = uint32_t(fill.step + take) / uint32_t(s.steps);
+      fill.step += take - int(items) * s.steps;
+      const uint32_t tile = uint32_t(fill.tile) + items;
+      fill.g += int(tile / uint32_t(s.tiles));
+      fill.tile = int(tile % uint32_t(s.tiles));
+      if (fill.g == A.hkv && filled + want < n_steps) fill.next_seq(A, lane);
+      break;
+    }
+    copy_lds_dword(id0, &to[0][0]);
+    copy_lds_dword(id1, &to[1][0]);
+    to[2][lane] = head;
+    filled += 64;
   };
-  // This wave's part of a step: 1 KiB pieces of the tiles K 0, K 1, V 0, V 1.
+  // A wave copies 1 KiB pieces of the step's tiles K 0, K 1, V 0, V 1.
+  const uint32_t page_bytes = uint32_t(A.hkv) * kTileBytes, lane_bytes = uint32_t(lane) * 16;
+  const int piece0 = wave * kCopies;
   int copied = 0;
+  int id0, id1, head;  // of the step that is copied next
+  auto read_ids = [&]() {
+    const int32_t(&from)[3][64] = ids[wave][copied >> 6 & 1];
+    const int i = copied & 63;
+    if constexpr (kCopies > 4) id0 = from[0][i], id1 = from[1][i];
+    else id0 = id1 = from[piece0 / 4 & 1][i];
+    head = from[2][i];
+  };
   auto copy_step = [&]() {
-    uint64_t off[2];
-#pragma unroll
-    for (int p = 0; p < 2; ++p)
-      off[p] = uint64_t(min(uint32_t(id[p]), A.last_page)) * page_bytes + uint32_t(ahead.g) * kTileBytes;
-    uint4(&stage)[4][256] = ring[copied & (kStages - 1)];
+    const uint32_t in_page = uint32_t(uniform(head)) * kTileBytes;
+    const uint64_t off[2] = {uint64_t(min(uint32_t(uniform(id0)), A.last_page)) * page_bytes + in_page,
+                             uint64_t(min(uint32_t(uniform(id1)), A.last_page)) * page_bytes + in_page};
+    const uint32_t stage = uint32_t(reinterpret_cast<uintptr_t>(&ring[copied % kStages][0][0]));
 #pragma unroll
     for (int c = 0; c < kCopies; ++c) {
-      const int piece = wave * kCopies + c, tile = piece >> 2, part = piece & 3;
-      const char* src = reinterpret_cast<const char*>(tile < 2 ? A.k_cache : A.v_cache) +
-                        off[tile & 1] + part * 1024 + lane * 16;
-      const uint32_t dst = uint32_t(reinterpret_cast<uintptr_t>(&stage[tile][part * 64]));
-      asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off"
+      const int piece = piece0 + c, tile = piece / 4;
+      const uint64_t src = reinterpret_cast<uint64_t>(tile < 2 ? A.k_cache : A.v_cache) +
+                           off[kCopies > 4 ? tile & 1 : 0] + piece % 4 * 1024;
+      asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2 nt"
                    :
-                   : "s"(dst), "v"(src)
+                   : "s"(stage + piece * 1024), "v"(lane_bytes), "s"(src)
                    : "memory", "m0");
     }
     if (++copied < n_steps) {
-      ahead.advance(A);
-      load_ids();
+      // At a turn's begin its ids landed long ago; the next turn's take the place of the last's.
+      if ((copied & 63) == 0 && filled < n_steps) fill_ids();
+      read_ids();
     }
   };
-  load_ids();
+  // Waits until all but the last `steps` steps' copies have landed, for every wave.
+  auto wait_steps = [&](int steps) {
+    switch (min(steps, kStages - 2)) {
+      case 0: wait_loads<0>(); break;
+      case 1: wait_loads<kCopies>(); break;
+      case 2: wait_loads<2 * kCopies>(); break;
+      case 3: wait_loads<3 * kCopies>(); break;
+      case 4: wait_loads<4 * kCopies>(); break;
+      case 5: wait_loads<5 * kCopies>(); break;
+      default: wait_loads<6 * kCopies>(); break;
+    }
+    __syncthreads();
+  };
+  fill_ids();
+  wait_loads<0>();
+  wave_sync();
+  if (filled < n_steps) fill_ids();
+  read_ids();
 #pragma unroll 1
   for (int i = 0; i < kStages - 1 && copied < n_steps; ++i) copy_step();
-  if (n_steps >= kStages - 1) wait_loads<(kStages - 2) * kCopies>();
-  else wait_loads<0>();
-  __syncthreads();
 
   bf16x8 qop[8];
-  f32x16 acc[4];
-  float m = -INFINITY, l = 0.f;
-  int node = 0, head = 0, first_step = 0;
-  bool ok = false;
-#pragma unroll 1
-  for (int n = 0; n < n_steps; ++n) {
-    if (copied < n_steps) copy_step();
-    const Seq& s = at.seq;
-    const int g = at.g;
-    const bool starts = n == 0 || at.step == 0;
-    if (starts) {
-      const int r = at.tile * kRows + 32 * wave + col;
-      node = r / G, head = r - node * G;
-      ok = node < s.nodes;
-      first_step = at.step;
-      const uint4* qrow = reinterpret_cast<const uint4*>(
-          A.q + (size_t(s.row0 + (ok ? node : 0)) * A.hq + size_t(g) * G + head) * kDim);
+  Rows R;
+  int n = 0;
+  while (true) {  // the range's parts of items
+    const Seq s = at.seq;
+    const int step0 = at.step, step1 = min(s.steps, step0 + n_steps - n);
+    const int r_tile = at.tile * kRows + 32 * wave + col;
+    const int node = r_tile / G, head = r_tile - node * G;
+    uint32_t* const my_bits = bits[32 * wave + col];
+    load_query(A, s, at.g, node, head, hh, qop, my_bits);
+    R.clear();
+    wave_sync();
+    if (n == 0) wait_steps(copied - 1);
+    auto scores = [&](const uint4(&stage)[4][256]) {
+      uint4 k[8];
 #pragma unroll
-      for (int c = 0; c < 8; ++c) qop[c] = as_bf16x8(ok ? qrow[2 * c + hh] : make_uint4(0, 0, 0, 0));
-      if (A.mask)
-        for (int i = hh; i < A.mask_words; i += 2)
-          bits[wave][col][i] = ok ? A.mask[size_t(s.row0 + node) * A.mask_words + i] : 0;
-      m = -INFINITY, l = 0.f;
+      for (int c = 0; c < 8; ++c) k[c] = stage[col >> 4][(2 * c + hh) * 16 + (col & 15)];
+      f32x16 sc;
 #pragma unroll
-      for (int cb = 0; cb < 4; ++cb)
+      for (int r = 0; r < 16; ++r) sc[r] = 0.f;
 #pragma unroll
-        for (int r2 = 0; r2 < 16; ++r2) acc[cb][r2] = 0.f;
-      __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-      __builtin_amdgcn_wave_barrier();
-    }
-    const uint4(&stage)[4][256] = ring[n & (kStages - 1)];
-    const int key0 = at.step * kStepKeys;
-    const bool masked = key0 + kStepKeys > s.prior;  // uniform
-
-    f32x16 sc;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) sc[r] = 0.f;
-#pragma unroll
-    for (int c = 0; c < 8; ++c)
-      sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-          as_bf16x8(stage[col >> 4][(2 * c + hh) * 16 + (col & 15)]), qop[c], sc, 0, 0, 0);
-    if (masked) {
-      // Bit i: the row sees key key0 + i.
-      uint32_t sees;
-      const int d = key0 - s.prior;  // > -32: the first key's node
-      if (!A.mask) {
-        const int lim = node - d;
-        sees = lim >= 31 ? ~0u : lim < 0 ? 0u : (2u << lim) - 1;
-      } else if (d < 0) {
-        sees = bits[wave][col][0] << -d | ((1u << -d) - 1);
-      } else {
-        const int i = d >> 5, sh = d & 31;
-        const uint32_t w0 = i < A.mask_words ? bits[wave][col][i] : 0;
-        const uint32_t w1 = i + 1 < A.mask_words ? bits[wave][col][i + 1] : 0;
-        sees = uint32_t((uint64_t(w1) << 32 | w0) >> sh);
-      }
-      const int left = s.len - key0;
-      if (left < 32) sees &= (1u << left) - 1;
-      if (!ok) sees = 0;
-      sees >>= 4 * hh;
-#pragma unroll
-      for (int r = 0; r < 16; ++r)
-        if (!(sees >> acc_row(r, 0) & 1)) sc[r] = -INFINITY;
-    }
-    auto rescale = [&]() {
-      float mloc = sc[0];
-#pragma unroll
-      for (int r = 1; r < 16; ++r) mloc = fmaxf(mloc, sc[r]);
-      float mc = fmaxf(mloc * A.sl2, m);
-      mc = fmaxf(mc, __shfl_xor(mc, 32));
-      const float alpha = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - mc);
-      l *= alpha;
-#pragma unroll
-      for (int cb = 0; cb < 4; ++cb) acc[cb] *= alpha;
-      m = mc;
+      for (int c = 0; c < 8; ++c) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k[c]), qop[c], sc, 0, 0, 0);
+      return sc;
     };
-    if (starts) rescale();
-    // While a row has seen no finite score, the offset is the largest float: scores of -inf give 0,
-    // and the first finite one infinity, which moves the maximum.
-    float p[16], ps;
-    auto take = [&]() {
-      const float neg_m = m == -INFINITY ? FLT_MAX : -m;
+    auto values = [&](const uint4(&stage)[4][256], uint4(&v)[8]) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) p[r] = __builtin_amdgcn_exp2f(fmaf(sc[r], A.sl2, neg_m));
-      const float t0 = (p[0] + p[1]) + (p[2] + p[3]), t1 = (p[4] + p[5]) + (p[6] + p[7]);
-      const float t2 = (p[8] + p[9]) + (p[10] + p[11]), t3 = (p[12] + p[13]) + (p[14] + p[15]);
-      ps = (t0 + t1) + (t2 + t3);
+      for (int c = 0; c < 8; ++c) v[c] = stage[2 + (c >> 2)][128 * hh + 32 * (c & 3) + col];
     };
-    take();
-    if (__ballot(!(ps <= kSumTau))) {
-      rescale();
-      take();
+    // After a step: the next one's copies have landed, and all waves are done with this one's stage.
+    auto next = [&]() {
+      ++n;
+      if (n < n_steps) wait_steps(copied - n - 1);
+    };
+    int step = step0;
+    // Steps over cached tokens alone, which every row sees.
+    for (const int plain = min(step1, s.prior / kStepKeys); step < plain; ++step) {
+      if (copied < n_steps) copy_step();
+      const uint4(&stage)[4][256] = ring[n % kStages];
+      const f32x16 sc = scores(stage);
+      uint4 v[8];
+      values(stage, v);
+      bf16x8 pr[2];
+      soften(R, sc, A.sl2, pr);
+      add_values(R, v, pr);
+      next();
     }
-    l += ps;
-    const bf16x8 pr[2] = {
-        as_bf16x8(make_uint4(pack_bf16x2(p[0], p[1]), pack_bf16x2(p[2], p[3]), pack_bf16x2(p[4], p[5]),
-                             pack_bf16x2(p[6], p[7]))),
-        as_bf16x8(make_uint4(pack_bf16x2(p[8], p[9]), pack_bf16x2(p[10], p[11]),
-                             pack_bf16x2(p[12], p[13]), pack_bf16x2(p[14], p[15])))};
-    if (!masked) {
-#pragma unroll
-      for (int c = 0; c < 8; ++c)
-        acc[c & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-            as_bf16x8(stage[2 + (c >> 2)][128 * hh + 32 * (c & 3) + col]), pr[c >> 2], acc[c & 3], 0, 0, 0);
-    } else {
-      // Slots past the end hold anything: zero.
-      uint32_t keep[2][4];
-#pragma unroll
-      for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const int valid = s.len - key0 - j * kPage;
-          const int s0 = 8 * (e / 2) + 4 * hh + 2 * (e % 2);
-          keep[j][e] = (s0 < valid ? 0x0000FFFFu : 0u) | (s0 + 1 < valid ? 0xFFFF0000u : 0u);
-        }
-      auto value = [&](int cb, int j) {
-        uint4 v = stage[2 + j][128 * hh + 32 * cb + col];
-        v.x &= keep[j][0], v.y &= keep[j][1], v.z &= keep[j][2], v.w &= keep[j][3];
-        return v;
-      };
-      auto has_special = [](uint32_t x) { return (x & 0x7F80u) == 0x7F80u || (x & 0x7F800000u) == 0x7F800000u; };
-#pragma unroll 1
-      for (int cb2 = 0; cb2 < 4; ++cb2) {
-        uint4 v[2];
-        bool special = false;
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          v[j] = value(cb2, j);
-          special |= has_special(v[j].x) || has_special(v[j].y) || has_special(v[j].z) || has_special(v[j].w);
-        }
-        const bool any = __ballot(special) != 0;
-        const uint4 raw[2] = {v[0], v[1]};
-        if (any) {
-          auto finite = [](uint32_t x) {
-            return ((x & 0x7F80u) == 0x7F80u ? 0u : x & 0xFFFFu) |
-                   ((x & 0x7F800000u) == 0x7F800000u ? 0u : x & 0xFFFF0000u);
-          };
-#pragma unroll
-          for (int j = 0; j < 2; ++j)
-            v[j] = make_uint4(finite(v[j].x), finite(v[j].y), finite(v[j].z), finite(v[j].w));
-        }
-#pragma unroll
-        for (int cb = 0; cb < 4; ++cb) {
-          if (cb != cb2) continue;
-#pragma unroll
-          for (int j = 0; j < 2; ++j)
-            acc[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(v[j]), pr[j], acc[cb], 0, 0, 0);
-          if (!any) continue;
-          // The same products with 1 in the places of +inf, of -inf and of NaN: above 0 where the row
-          // sees one.
-#pragma unroll 1
-          for (int kind = 0; kind < 3; ++kind) {
-            const uint32_t lo = kind == 1 ? 0xFF80u : 0x7F80u;
-            auto ones = [&](uint32_t x) {
-              uint32_t o = 0;
-#pragma unroll
-              for (int half = 0; half < 32; half += 16) {
-                const uint32_t e = x >> half & 0xFFFF;
-                if (kind == 2 ? (e & 0x7FFF) > 0x7F80u : e == lo) o |= 0x3F80u << half;
-              }
-              return o;
-            };
-            f32x16 seen;
-#pragma unroll
-            for (int r = 0; r < 16; ++r) seen[r] = 0.f;
-#pragma unroll
-            for (int j = 0; j < 2; ++j)
-              seen = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                  as_bf16x8(make_uint4(ones(raw[j].x), ones(raw[j].y), ones(raw[j].z), ones(raw[j].w))),
-                  pr[j], seen, 0, 0, 0);
-            const float put = kind == 0 ? INFINITY : kind == 1 ? -INFINITY : NAN;
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-              if (seen[r] > 0.f) acc[cb][r] += put;
-          }
-        }
+    for (; step < step1; ++step) {
+      if (copied < n_steps) copy_step();
+      const uint4(&stage)[4][256] = ring[n % kStages];
+      f32x16 sc = scores(stage);
+      const uint32_t sees = seen_keys(A, s, my_bits, node, step * kStepKeys);
+      mask_scores(sees, hh, sc);
+      bf16x8 pr[2];
+      soften(R, sc, A.sl2, pr);
+      uint4 v[8];
+      values(stage, v);
+      if (trim_values(v, s.len - step * kStepKeys, hh)) {
+        finite_values(v);
+        add_special_values(R, sees, hh, reinterpret_cast<const uint16_t*>(stage[2]),
+                           reinterpret_cast<const uint16_t*>(stage[3]));
       }
+      add_values(R, v, pr);
+      next();
     }
-
-    const bool ends = at.step + 1 == s.steps;
-    if (ends || n + 1 == n_steps) {
-      // Row col's sum over both lane halves; a lane holds channels 32 cb + 8 e + 4 hh .. + 3.
-      const float ls = l + __shfl_xor(l, 32);
-      const float inv = ls > 0.f ? 1.f / ls : ls == 0.f ? 0.f : ls;  // a NaN stays
-      if (first_step == 0 && ends) {
-        if (ok) {
-          const size_t orow = size_t(s.row0 + node) * A.hq + size_t(g) * G + head;
-          uint16_t* o = A.out + orow * kDim + 4 * hh;
+    // Row col's sum over both lane halves.
+    const float ls = R.l + __shfl_xor(R.l, 32);
+    const float inv = ls > 0.f ? 1.f / ls : ls == 0.f ? 0.f : ls;  // a NaN stays
+    if (node < s.nodes) {
+      if (step0 == 0 && step1 == s.steps) {
+        const size_t orow = size_t(s.row0 + node) * A.hq + size_t(at.g) * G + head;
+        uint16_t* o = A.out + orow * kDim + 4 * hh;
 #pragma unroll
-          for (int cb = 0; cb < 4; ++cb)
+        for (int cb = 0; cb < 4; ++cb)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              *reinterpret_cast<uint2*>(o + 32 * cb + 8 * e) =
-                  make_uint2(pack_bf16x2(acc[cb][4 * e] * inv, acc[cb][4 * e + 1] * inv),
-                             pack_bf16x2(acc[cb][4 * e + 2] * inv, acc[cb][4 * e + 3] * inv));
-          if (A.lse && hh == 0) A.lse[orow] = ls == 0.f ? -INFINITY : (m + log2f(ls)) * kLn2;
-        }
+          for (int e = 0; e < 4; ++e)
+            *reinterpret_cast<uint2*>(o + 32 * cb + 8 * e) =
+                make_uint2(pack_bf16x2(R.acc[cb][4 * e] * inv, R.acc[cb][4 * e + 1] * inv),
+                           pack_bf16x2(R.acc[cb][4 * e + 2] * inv, R.acc[cb][4 * e + 3] * inv));
+        if (A.lse && hh == 0) A.lse[orow] = ls == 0.f ? -INFINITY : (R.m + log2f(ls)) * kLn2;
       } else {
-        const size_t slot = size_t(2) * w + (first_step == 0 ? 1 : 0);
-        const size_t prow = slot * kRows + 32 * wave + col;
-        if (ok) {
-          float* o = A.part_o + prow * kDim + 4 * hh;
+        const size_t prow = (size_t(2) * w + (step0 == 0 ? 1 : 0)) * kRows + 32 * wave + col;
+        float* o = A.part_o + prow * kDim + 4 * hh;
 #pragma unroll
-          for (int cb = 0; cb < 4; ++cb)
+        for (int cb = 0; cb < 4; ++cb)
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              *reinterpret_cast<f32x4*>(o + 32 * cb + 8 * e) =
-                  f32x4{acc[cb][4 * e] * inv, acc[cb][4 * e + 1] * inv, acc[cb][4 * e + 2] * inv,
-                        acc[cb][4 * e + 3] * inv};
-          if (hh == 0) A.part_lse[prow] = ls == 0.f ? -INFINITY : m + log2f(ls);
-        }
+          for (int e = 0; e < 4; ++e)
+            *reinterpret_cast<f32x4*>(o + 32 * cb + 8 * e) =
+                f32x4{R.acc[cb][4 * e] * inv, R.acc[cb][4 * e + 1] * inv, R.acc[cb][4 * e + 2] * inv,
+                      R.acc[cb][4 * e + 3] * inv};
+        if (hh == 0) A.part_lse[prow] = ls == 0.f ? -INFINITY : R.m + log2f(ls);
       }
     }
-    if (n + 1 < n_steps) {
-      at.advance(A);
-      // Step n + 1's copies have landed; those of the two after it may be in flight.
-      if (n + kStages - 1 < n_steps) wait_loads<(kStages - 2) * kCopies>();
-      else wait_loads<0>();
-      __syncthreads();
+    if (step1 < s.steps && step0 == 0 && tid == 0) {
+      // The item's other parts are those of the workgroups after this one, n_steps each.
+      split[0] = (s.steps - step1 + n_steps - 1) / n_steps + 1;
+      split[1] = s.row0, split[2] = s.nodes, split[3] = at.g, split[4] = at.tile;
     }
+    if (n == n_steps) return;
+    at.next_item(A, lane);
   }
 }
 
-// Joins the parts of split items.  A workgroup takes a node's heads, `heads` of them at a time from
-// blockIdx.y; 16 threads, eight channels each, fold an eighth part or all of a head's, as many
-// groups to a head as its parts need.
+// Joins the parts of the items that workgroups of the attention began and did not end: workgroup
+// (x, y) those of the x-th such item, which it finds among all workgroups' records, and block_rows
+// of the tile's rows; 16 threads, eight channels each, fold a row's parts,
+// four at a time, or as many groups of 16 as the parts need share a row.
 constexpr int kMergeThreads = 256;
+static_assert(groups_of(1) <= 3 * kMergeThreads, "the merge looks at three records a thread");
 constexpr int kMergeGroups = kMergeThreads / 16;
 constexpr int kMergeBatch = 4;
 
-template <int kRows>
-__global__ __launch_bounds__(kMergeThreads) void tree_merge_kernel(TreeArgs A, int groups) {
-  __shared__ int64_t found[kMergeThreads / 64][3];
+__global__ __launch_bounds__(kMergeThreads) void tree_merge_kernel(TreeArgs A, int groups, int tile_rows, int block_rows) {
   __shared__ __align__(16) float shared[kMergeGroups][16][12];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int64_t row = blockIdx.x;
-  // The row's sequence, the steps before it, and all steps.
-  int64_t seqs = 0, before = 0, total = 0;
-  for (int b = tid; b < A.batch; b += kMergeThreads) {
-    const int64_t cost = load_seq<kRows>(A, A.prior, A.starts, b).cost(A);
-    total += cost;
-    if (A.starts[b + 1] <= row) ++seqs, before += cost;
-  }
+  __shared__ int counts[3][kMergeThreads / 64], found;
+  const int tid = threadIdx.x;
+  if (tid == 0) found = -1;
+  uint64_t has[3];  // of records 256 i + 64 wave ..
 #pragma unroll
-  for (int n = 32; n; n >>= 1) {
-    seqs += __shfl_xor(seqs, n);
-    before += __shfl_xor(before, n);
-    total += __shfl_xor(total, n);
+  for (int i = 0; i < 3; ++i) {
+    const int at = kMergeThreads * i + tid;
+    has[i] = __ballot(at < groups && A.splits[at * kSplitInts] != 0);
+    if ((tid & 63) == 0) counts[i][tid >> 6] = __popcll(has[i]);
   }
-  if (lane == 0) found[wave][0] = seqs, found[wave][1] = before, found[wave][2] = total;
   __syncthreads();
-  seqs = before = total = 0;
+  int before = 0;
 #pragma unroll
-  for (int w = 0; w < kMergeThreads / 64; ++w) seqs += found[w][0], before += found[w][1], total += found[w][2];
-  if (seqs >= A.batch) return;  // padding
-  const int b = int(seqs);
-  const Seq s = load_seq<kRows>(A, A.prior, A.starts, b);
-  // (Starts that do not ascend could put the sequence anywhere.)
-  if (row < s.row0 || row >= s.row0 + s.nodes || before + s.cost(A) > total) return;
-  const int64_t each = steps_each(total, groups);
-  const int node = int(row - s.row0);
-  // An item has at most this many parts; every group of a head folds kMergeBatch of them at a time.
-  const int64_t most = (s.steps + each - 2) / each + 1;
-  const int per_head = most <= kMergeBatch ? 1 : most <= 4 * kMergeBatch ? 4 : kMergeGroups;
-  const int at_once = kMergeGroups / per_head;
-  const int grp = tid >> 4, t = tid & 15, k = grp % per_head;
-  for (int h0 = int(blockIdx.y) * at_once; h0 < A.hq; h0 += int(gridDim.y) * at_once) {
-    const int h = h0 + grp / per_head;
-    int64_t w0 = 0, w1 = 0;
-    int in_tile = 0;
-    if (h < A.hq) {
-      const int g = h / A.group;
-      const int r = node * A.group + (h - g * A.group);
-      const int64_t first = before + (int64_t(g) * s.tiles + r / kRows) * s.steps;
-      in_tile = r % kRows;
-      w0 = first / each, w1 = (first + s.steps - 1) / each;
+  for (int i = 0; i < 3; ++i)
+#pragma unroll
+    for (int v = 0; v < kMergeThreads / 64; ++v) {
+      if (v == tid >> 6 && has[i] >> (tid & 63) & 1 &&
+          before + __popcll(has[i] & ((uint64_t(1) << (tid & 63)) - 1)) == int(blockIdx.x))
+        found = kMergeThreads * i + tid;
+      before += counts[i][v];
     }
-    const int n = w0 == w1 ? 0 : int(w1 - w0) + 1;
+  __syncthreads();
+  const int w = found;
+  if (w < 0) return;
+  const int32_t* split = A.splits + w * kSplitInts;
+  const Split s{split[0], split[1], split[2], split[3], split[4]};
+  const int n = s.parts;
+  const int per_row = n <= kMergeBatch ? 1 : n <= 4 * kMergeBatch ? 4 : kMergeGroups;
+  const int at_once = kMergeGroups / per_row;
+  const int grp = tid >> 4, t = tid & 15, k = grp % per_row;
+  const int first = blockIdx.y * block_rows;
+  for (int i0 = 0; i0 < block_rows; i0 += at_once) {
+    const int i = i0 + grp / per_row, in_tile = first + i;
+    const int r = s.tile * tile_rows + in_tile;
+    const int node = r / A.group, head = r - node * A.group;
+    const bool live = i < block_rows && node < s.nodes;
     float M = -INFINITY, sum = 0.f, acc[8] = {};
     auto fold = [&](float Mk, float wk, const float (&xk)[8]) {
-      // A NaN moves no maximum, but makes both factors' sums NaN.
+      // A part without a key of the row adds nothing, whatever else it holds; a NaN makes a NaN.
       const float Mn = fmaxf(M, Mk);
       const float a = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - Mn);
       const float c = Mk == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(Mk - Mn);
       sum = sum * a + wk * c;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) acc[i] = (a == 0.f ? 0.f : acc[i] * a) + (c == 0.f ? 0.f : xk[i] * c);
+      for (int e = 0; e < 8; ++e) acc[e] = (a == 0.f ? 0.f : acc[e] * a) + (c == 0.f ? 0.f : xk[e] * c);
       M = Mn;
     };
-    for (int j0 = k * kMergeBatch; j0 < n; j0 += per_head * kMergeBatch) {
-      float lj[kMergeBatch], x[kMergeBatch][8];
+    for (int j0 = k * kMergeBatch; j0 < n; j0 += per_row * kMergeBatch) {
+      float lj[kMergeBatch];
+      f32x4 lo[kMergeBatch], hi[kMergeBatch];
 #pragma unroll
       for (int j = 0; j < kMergeBatch; ++j) {
         lj[j] = -INFINITY;
-        if (j0 + j < n) {
-          const size_t slot = j0 + j == 0 ? size_t(2) * w0 + 1 : size_t(2) * (w0 + j0 + j);
-          lj[j] = A.part_lse[slot * kRows + in_tile];
-          const f32x4* o = reinterpret_cast<const f32x4*>(A.part_o + (slot * kRows + in_tile) * kDim + 8 * t);
-          const f32x4 lo = o[0], hi = o[1];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) x[j][i] = lo[i], x[j][4 + i] = hi[i];
+        lo[j] = hi[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (live && j0 + j < n) {
+          const size_t slot = j0 + j == 0 ? size_t(2) * w + 1 : size_t(2) * (w + j0 + j);
+          lj[j] = A.part_lse[slot * tile_rows + in_tile];
+          const f32x4* o = reinterpret_cast<const f32x4*>(A.part_o + (slot * tile_rows + in_tile) * kDim + 8 * t);
+          lo[j] = o[0], hi[j] = o[1];
         }
       }
 #pragma unroll
-      for (int j = 0; j < kMergeBatch; ++j)
-        if (j0 + j < n) fold(lj[j], 1.f, x[j]);
+      for (int j = 0; j < kMergeBatch; ++j) {
+        const float x[8] = {lo[j][0], lo[j][1], lo[j][2], lo[j][3], hi[j][0], hi[j][1], hi[j][2], hi[j][3]};
+        fold(lj[j], 1.f, x);
+      }
     }
-    if (per_head > 1) {
+    if (per_row > 1) {
       float* mine = shared[grp][t];
       mine[0] = M, mine[1] = sum;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) mine[2 + i] = acc[i];
+      for (int e = 0; e < 8; ++e) mine[2 + e] = acc[e];
       __syncthreads();
       if (k == 0)
-        for (int o = 1; o < per_head; ++o) {
+        for (int o = 1; o < per_row; ++o) {
           const float* other = shared[grp + o][t];
           float x[8];
 #pragma unroll
-          for (int i = 0; i < 8; ++i) x[i] = other[2 + i];
+          for (int e = 0; e < 8; ++e) x[e] = other[2 + e];
           fold(other[0], other[1], x);
         }
       __syncthreads();
     }
-    if (k == 0 && n > 0) {
+    if (k == 0 && live) {
       const float inv = sum == 0.f ? 0.f : 1.f / sum;
-      const size_t orow = size_t(row) * A.hq + h;
+      const size_t orow = size_t(s.row0 + node) * A.hq + size_t(s.g) * A.group + head;
       uint32_t o[4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) o[i] = pack_bf16x2(acc[2 * i] * inv, acc[2 * i + 1] * inv);
+      for (int e = 0; e < 4; ++e) o[e] = pack_bf16x2(acc[2 * e] * inv, acc[2 * e + 1] * inv);
       *reinterpret_cast<uint4*>(A.out + orow * kDim + 8 * t) = make_uint4(o[0], o[1], o[2], o[3]);
       if (A.lse && t == 0) A.lse[orow] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
     }
@@ -594,7 +713,9 @@ TreeArgs tree_args(const KvLayout& L, const TreeCall& c, int waves) {
   const size_t part_rows = size_t(2) * groups_of(waves) * 32 * waves;
   A.part_o = static_cast<float*>(c.ws);
   A.part_lse = A.part_o + part_rows * kDim;
-  A.rows = c.rows;
+  A.splits = reinterpret_cast<int32_t*>(A.part_lse + part_rows);
+  A.rows = int(c.rows);
+  A.most = int(std::min<int64_t>(c.stride * kPage, INT32_MAX - 64));
   A.last_page = uint32_t(std::min<int64_t>(L.desc.num_pages - 1, INT32_MAX));
   A.batch = c.batch, A.hkv = L.desc.num_kv_heads, A.hq = c.hq, A.group = c.hq / A.hkv;
   A.sl2 = c.scale * kLog2e;
@@ -605,7 +726,7 @@ TreeArgs tree_args(const KvLayout& L, const TreeCall& c, int waves) {
 
 size_t tree_workspace(int64_t rows, int32_t batch, int32_t hq, int32_t hkv) {
   const int waves = waves_of(rows, batch, hq / hkv);
-  return size_t(2) * groups_of(waves) * 32 * waves * (kDim + 1) * sizeof(float);
+  return size_t(groups_of(waves)) * (size_t(2) * 32 * waves * (kDim + 1) * sizeof(float) + kSplitInts * sizeof(int32_t));
 }
 
 hipError_t launch_tree(const KvLayout& L, const TreeCall& c, hipStream_t s) {
@@ -613,10 +734,10 @@ hipError_t launch_tree(const KvLayout& L, const TreeCall& c, hipStream_t s) {
   const TreeArgs A = tree_args(L, c, waves);
   const dim3 grid{unsigned(groups_of(waves))}, block{unsigned(64 * waves)};
   switch (waves) {
-    case 1: hipLaunchKernelGGL(tree_kernel<1>, grid, block, 0, s, A); break;
-    case 2: hipLaunchKernelGGL(tree_kernel<2>, grid, block, 0, s, A); break;
-    case 4: hipLaunchKernelGGL(tree_kernel<4>, grid, block, 0, s, A); break;
-    default: hipLaunchKernelGGL(tree_kernel<8>, grid, block, 0, s, A); break;
+    case 1: hipLaunchKernelGGL(tree_ring_kernel<1>, grid, block, 0, s, A); break;
+    case 2: hipLaunchKernelGGL(tree_ring_kernel<2>, grid, block, 0, s, A); break;
+    case 4: hipLaunchKernelGGL(tree_ring_kernel<4>, grid, block, 0, s, A); break;
+    default: hipLaunchKernelGGL(tree_ring_kernel<8>, grid, block, 0, s, A); break;
   }
   return hipGetLastError();
 }
@@ -624,16 +745,14 @@ hipError_t launch_tree(const KvLayout& L, const TreeCall& c, hipStream_t s) {
 hipError_t launch_tree_merge(const KvLayout& L, const TreeCall& c, hipStream_t s) {
   const int waves = waves_of(c.rows, c.batch, c.hq / L.desc.num_kv_heads);
   const TreeArgs A = tree_args(L, c, waves);
-  const int groups = groups_of(waves);
-  // Few rows: their heads over more workgroups.
-  const unsigned y = unsigned(std::clamp<int64_t>(2048 / c.rows, 1, c.hq));
-  const dim3 grid{unsigned(c.rows), y}, block{unsigned(kMergeThreads)};
-  switch (waves) {
-    case 1: hipLaunchKernelGGL(tree_merge_kernel<32>, grid, block, 0, s, A, groups); break;
-    case 2: hipLaunchKernelGGL(tree_merge_kernel<64>, grid, block, 0, s, A, groups); break;
-    case 4: hipLaunchKernelGGL(tree_merge_kernel<128>, grid, block, 0, s, A, groups); break;
-    default: hipLaunchKernelGGL(tree_merge_kernel<256>, grid, block, 0, s, A, groups); break;
-  }
+  // At most as many items are split as there are, or workgroups.
+  const int rows = 32 * waves, groups = groups_of(waves);
+  const int64_t items = A.hkv * (int64_t(c.batch) + c.rows * A.group / rows);
+  const unsigned x = unsigned(std::min<int64_t>(items, groups));
+  int block_rows = 16;
+  while (block_rows > 1 && x * (rows / block_rows) < 2048) block_rows /= 2;
+  hipLaunchKernelGGL(tree_merge_kernel, dim3(x, unsigned(rows / block_rows)), dim3(kMergeThreads), 0, s, A, groups,
+                     rows, block_rows);
   return hipGetLastError();
 }
 
