@@ -70,6 +70,12 @@ __device__ __forceinline__ void wait_loads() {  // all but the last kCount vecto
   __builtin_amdgcn_s_waitcnt((kCount & 15) | (kCount >> 4) << 14 | 0x0F70);
 }
 
+// What the merge gets to know of an item that workgroup w begins and does not end.
+struct alignas(32) Split {
+  int32_t parts;  // 0: there is none
+  int32_t row0, nodes, g, tile;
+};
+
 struct TreeArgs {
   const uint16_t* k_cache;
   const uint16_t* v_cache;
@@ -82,7 +88,7 @@ struct TreeArgs {
   float* lse;
   float* part_o;
   float* part_lse;
-  int32_t* splits;
+  Split* splits;  // of each workgroup
   int64_t stride;
   uint32_t last_page;
   int rows, most;  // query rows, tokens that a row of the block table can hold
@@ -193,12 +199,6 @@ struct Cursor {
     next_seq(A, lane);
   }
 };
-
-// What the merge gets to know of an item that workgroup w begins and does not end.
-struct Split {
-  int parts, row0, nodes, g, tile;
-};
-constexpr int kSplitInts = 8;
 
 // The rows of a wave: their running maximum and sum, and the unnormalised output, transposed: lane
 // (col, hh) holds channels 32 cb + 8 e + 4 hh .. + 3 of row col.
@@ -367,6 +367,7 @@ template <int kWaves>
 struct Ring {
   static constexpr int kStages = kWaves == 8 ? 8 : kWaves == 4 ? 4 : 3;
   static constexpr int kCopies = 16 / kWaves;  // of 1 KiB, per wave and step
+  static constexpr bool kAhead = kWaves == 8;  // scores are taken a step ahead
 };
 
 template <int kWaves>
@@ -375,6 +376,7 @@ void tree_ring_kernel(TreeArgs A) {
   constexpr int kRows = 32 * kWaves;
   constexpr int kStages = Ring<kWaves>::kStages;
   constexpr int kCopies = Ring<kWaves>::kCopies;
+  constexpr bool kAhead = Ring<kWaves>::kAhead;
   __shared__ __align__(16) uint4 ring[kStages][4][256];  // K of the step's two pages, V of them
   __shared__ uint32_t bits[kRows][kMaskWords + 1];
   __shared__ int32_t ids[kWaves][2][3][64];  // of two turns of 64 steps: a step's page ids and KV head
@@ -386,10 +388,9 @@ void tree_ring_kernel(TreeArgs A) {
   // Neighbouring ranges on one XCD: workgroup w runs on XCD w % 8.
   const int per_xcd = int(gridDim.x) / kNumXcds;
   const int w = int(blockIdx.x) % kNumXcds * per_xcd + int(blockIdx.x) / kNumXcds;
-  int32_t* const split = A.splits + w * kSplitInts;
   Cursor<kRows> at;
   const int n_steps = at.start(A, w, int(gridDim.x), lane);
-  if (tid == 0) split[0] = 0;  // unless an item is begun and not ended, below
+  if (tid == 0) A.splits[w].parts = 0;  // unless an item is begun and not ended, below
   if (n_steps == 0) return;
 
   // What the copies need of each step, page ids and KV head, 64 steps at a time: lane l finds
@@ -437,16 +438,16 @@ void tree_ring_kernel(TreeArgs A) {
   const uint32_t page_bytes = uint32_t(A.hkv) * kTileBytes, lane_bytes = uint32_t(lane) * 16;
   const int piece0 = wave * kCopies;
   int copied = 0;
-  int id0, id1, head;  // of the step that is copied next
+  int id0, id1, kv_head;  // of the step that is copied next
   auto read_ids = [&]() {
     const int32_t(&from)[3][64] = ids[wave][copied >> 6 & 1];
     const int i = copied & 63;
     if constexpr (kCopies > 4) id0 = from[0][i], id1 = from[1][i];
     else id0 = id1 = from[piece0 / 4 & 1][i];
-    head = from[2][i];
+    kv_head = from[2][i];
   };
   auto copy_step = [&]() {
-    const uint32_t in_page = uint32_t(uniform(head)) * kTileBytes;
+    const uint32_t in_page = uint32_t(uniform(kv_head)) * kTileBytes;
     const uint64_t off[2] = {uint64_t(min(uint32_t(uniform(id0)), A.last_page)) * page_bytes + in_page,
                              uint64_t(min(uint32_t(uniform(id1)), A.last_page)) * page_bytes + in_page};
     const uint32_t stage = uint32_t(reinterpret_cast<uintptr_t>(&ring[copied % kStages][0][0]));
@@ -468,16 +469,26 @@ void tree_ring_kernel(TreeArgs A) {
   };
   // Waits until all but the last `steps` steps' copies have landed, for every wave.
   auto wait_steps = [&](int steps) {
-    switch (min(steps, kStages - 2)) {
+    switch (min(steps, kStages - 1)) {
       case 0: wait_loads<0>(); break;
       case 1: wait_loads<kCopies>(); break;
       case 2: wait_loads<2 * kCopies>(); break;
       case 3: wait_loads<3 * kCopies>(); break;
       case 4: wait_loads<4 * kCopies>(); break;
       case 5: wait_loads<5 * kCopies>(); break;
-      default: wait_loads<6 * kCopies>(); break;
+      case 6: wait_loads<6 * kCopies>(); break;
+      default: wait_loads<7 * kCopies>(); break;
     }
     __syncthreads();
+  };
+  // Before step n: its copies have landed (and the next two steps' where scores are taken ahead, for
+  // two steps at once), all waves are done with the steps before, and their stages are filled again.
+  int n = 0;
+  auto open_step = [&]() {
+    if (kAhead && n % 2) return;
+    wait_steps(max(copied - n - (kAhead ? 3 : 1), 0));
+#pragma unroll 1
+    while (copied < min(n + kStages, n_steps)) copy_step();
   };
   fill_ids();
   wait_loads<0>();
@@ -485,78 +496,116 @@ void tree_ring_kernel(TreeArgs A) {
   if (filled < n_steps) fill_ids();
   read_ids();
 #pragma unroll 1
-  for (int i = 0; i < kStages - 1 && copied < n_steps; ++i) copy_step();
+  while (copied < min(kStages - (kAhead ? 2 : 1), n_steps)) copy_step();
 
   bf16x8 qop[8];
   Rows R;
-  int n = 0;
+  auto load_keys = [&](uint4(&k)[8], int n) {
+    const uint4(&stage)[4][256] = ring[n % kStages];
+#pragma unroll
+    for (int c = 0; c < 8; ++c) k[c] = stage[col >> 4][(2 * c + hh) * 16 + (col & 15)];
+  };
+  auto score = [&](const uint4(&k)[8]) {
+    f32x16 sc;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sc[r] = 0.f;
+#pragma unroll
+    for (int c = 0; c < 8; ++c) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k[c]), qop[c], sc, 0, 0, 0);
+    return sc;
+  };
+  auto load_value = [&](int n, int c) { return ring[n % kStages][2 + (c >> 2)][128 * hh + 32 * (c & 3) + col]; };
+  // The wave's row of this lane in the cursor's item.
+  auto row_of = [&](int& node, int& head) {
+    const int r = at.tile * kRows + 32 * wave + col;
+    node = r / G, head = r - node * G;
+  };
+  int node, head;
+  uint32_t* const my_bits = bits[32 * wave + col];
+  row_of(node, head);
+  load_query(A, at.seq, at.g, node, head, hh, qop, my_bits);
   while (true) {  // the range's parts of items
     const Seq s = at.seq;
-    const int step0 = at.step, step1 = min(s.steps, step0 + n_steps - n);
-    const int r_tile = at.tile * kRows + 32 * wave + col;
-    const int node = r_tile / G, head = r_tile - node * G;
-    uint32_t* const my_bits = bits[32 * wave + col];
-    load_query(A, s, at.g, node, head, hh, qop, my_bits);
+    const int g = at.g, tile = at.tile, step0 = at.step, step1 = min(s.steps, step0 + n_steps - n);
     R.clear();
     wave_sync();
-    if (n == 0) wait_steps(copied - 1);
-    auto scores = [&](const uint4(&stage)[4][256]) {
-      uint4 k[8];
-#pragma unroll
-      for (int c = 0; c < 8; ++c) k[c] = stage[col >> 4][(2 * c + hh) * 16 + (col & 15)];
-      f32x16 sc;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) sc[r] = 0.f;
-#pragma unroll
-      for (int c = 0; c < 8; ++c) sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k[c]), qop[c], sc, 0, 0, 0);
-      return sc;
-    };
-    auto values = [&](const uint4(&stage)[4][256], uint4(&v)[8]) {
-#pragma unroll
-      for (int c = 0; c < 8; ++c) v[c] = stage[2 + (c >> 2)][128 * hh + 32 * (c & 3) + col];
-    };
-    // After a step: the next one's copies have landed, and all waves are done with this one's stage.
-    auto next = [&]() {
-      ++n;
-      if (n < n_steps) wait_steps(copied - n - 1);
-    };
+    f32x16 sc;
     int step = step0;
-    // Steps over cached tokens alone, which every row sees.
-    for (const int plain = min(step1, s.prior / kStepKeys); step < plain; ++step) {
-      if (copied < n_steps) copy_step();
-      const uint4(&stage)[4][256] = ring[n % kStages];
-      const f32x16 sc = scores(stage);
-      uint4 v[8];
-      values(stage, v);
-      bf16x8 pr[2];
-      soften(R, sc, A.sl2, pr);
-      add_values(R, v, pr);
-      next();
+    if constexpr (kAhead) {
+      open_step();
+      uint4 k[8];
+      load_keys(k, n);
+      sc = score(k);
     }
-    for (; step < step1; ++step) {
-      if (copied < n_steps) copy_step();
-      const uint4(&stage)[4][256] = ring[n % kStages];
-      f32x16 sc = scores(stage);
-      const uint32_t sees = seen_keys(A, s, my_bits, node, step * kStepKeys);
-      mask_scores(sees, hh, sc);
+    // Steps over cached tokens alone, which every row sees.
+    for (const int plain = min(step1 - (kAhead ? 1 : 0), s.prior / kStepKeys); step < plain; ++step, ++n) {
+      if (!kAhead || step > step0) open_step();
+      bf16x8 pr[2];
+      uint4 k[8];
+      if constexpr (kAhead) {
+        load_keys(k, n + 1);
+        soften(R, sc, A.sl2, pr);
+        // The next step's scores, a chain of products, among this step's values' independent ones.
+#pragma unroll
+        for (int r = 0; r < 16; ++r) sc[r] = 0.f;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k[c]), qop[c], sc, 0, 0, 0);
+          R.acc[c & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(load_value(n, c)), pr[c >> 2], R.acc[c & 3], 0, 0, 0);
+        }
+      } else {
+        load_keys(k, n);
+        sc = score(k);
+        uint4 v[8];
+#pragma unroll
+        for (int c = 0; c < 8; ++c) v[c] = load_value(n, c);
+        soften(R, sc, A.sl2, pr);
+        add_values(R, v, pr);
+      }
+    }
+    for (; step < step1; ++step, ++n) {
+      if (!kAhead || step > step0) open_step();
+      uint4 k[8], v[8];
+      if constexpr (!kAhead) {
+        load_keys(k, n);
+        sc = score(k);
+      }
+      const int key0 = step * kStepKeys;
+      uint32_t sees = ~0u;
+      if (key0 + kStepKeys > s.prior) {
+        sees = seen_keys(A, s, my_bits, node, key0);
+        mask_scores(sees, hh, sc);
+      }
       bf16x8 pr[2];
       soften(R, sc, A.sl2, pr);
-      uint4 v[8];
-      values(stage, v);
-      if (trim_values(v, s.len - step * kStepKeys, hh)) {
+#pragma unroll
+      for (int c = 0; c < 8; ++c) v[c] = load_value(n, c);
+      if (trim_values(v, s.len - key0, hh) && key0 + kStepKeys > s.prior) {
         finite_values(v);
+        const uint4(&stage)[4][256] = ring[n % kStages];
         add_special_values(R, sees, hh, reinterpret_cast<const uint16_t*>(stage[2]),
                            reinterpret_cast<const uint16_t*>(stage[3]));
       }
       add_values(R, v, pr);
-      next();
+      if constexpr (kAhead) {
+        if (step + 1 < step1) {
+          load_keys(k, n + 1);
+          sc = score(k);
+        }
+      }
+    }
+    // The next part's queries are on their way before this part's results.
+    const int row_node = node, row_head = head;
+    if (n < n_steps) {
+      at.next_item(A, lane);
+      row_of(node, head);
+      load_query(A, at.seq, at.g, node, head, hh, qop, my_bits);
     }
     // Row col's sum over both lane halves.
     const float ls = R.l + __shfl_xor(R.l, 32);
     const float inv = ls > 0.f ? 1.f / ls : ls == 0.f ? 0.f : ls;  // a NaN stays
-    if (node < s.nodes) {
+    if (row_node < s.nodes) {
       if (step0 == 0 && step1 == s.steps) {
-        const size_t orow = size_t(s.row0 + node) * A.hq + size_t(at.g) * G + head;
+        const size_t orow = size_t(s.row0 + row_node) * A.hq + size_t(g) * G + row_head;
         uint16_t* o = A.out + orow * kDim + 4 * hh;
 #pragma unroll
         for (int cb = 0; cb < 4; ++cb)
@@ -581,25 +630,22 @@ void tree_ring_kernel(TreeArgs A) {
     }
     if (step1 < s.steps && step0 == 0 && tid == 0) {
       // The item's other parts are those of the workgroups after this one, n_steps each.
-      split[0] = (s.steps - step1 + n_steps - 1) / n_steps + 1;
-      split[1] = s.row0, split[2] = s.nodes, split[3] = at.g, split[4] = at.tile;
+      A.splits[w] = {(s.steps - step1 + n_steps - 1) / n_steps + 1, s.row0, s.nodes, g, tile};
     }
     if (n == n_steps) return;
-    at.next_item(A, lane);
   }
 }
 
-// Joins the parts of the items that workgroups of the attention began and did not end: workgroup
-// (x, y) those of the x-th such item, which it finds among all workgroups' records, and block_rows
-// of the tile's rows; 16 threads, eight channels each, fold a row's parts,
-// four at a time, or as many groups of 16 as the parts need share a row.
+// Joins the parts of the items that workgroups of the attention began and did not end.  Workgroup
+// (x, y) takes kMergeGroups / kPerRow rows of the tile of workgroup x's item; kPerRow groups of 16
+// threads, eight channels each, fold a row's parts.  Where items have many parts, most records are
+// empty, and x counts the others: the workgroup finds its own among all of them.
 constexpr int kMergeThreads = 256;
-static_assert(groups_of(1) <= 3 * kMergeThreads, "the merge looks at three records a thread");
 constexpr int kMergeGroups = kMergeThreads / 16;
-constexpr int kMergeBatch = 4;
+static_assert(groups_of(1) <= 3 * kMergeThreads, "the merge looks at three records a thread");
 
-__global__ __launch_bounds__(kMergeThreads) void tree_merge_kernel(TreeArgs A, int groups, int tile_rows, int block_rows) {
-  __shared__ __align__(16) float shared[kMergeGroups][16][12];
+// The x-th workgroup with a split item, or -1.
+__device__ __forceinline__ int find_split(const TreeArgs& A, int groups, int x) {
   __shared__ int counts[3][kMergeThreads / 64], found;
   const int tid = threadIdx.x;
   if (tid == 0) found = -1;
@@ -607,7 +653,7 @@ __global__ __launch_bounds__(kMergeThreads) void tree_merge_kernel(TreeArgs A, i
 #pragma unroll
   for (int i = 0; i < 3; ++i) {
     const int at = kMergeThreads * i + tid;
-    has[i] = __ballot(at < groups && A.splits[at * kSplitInts] != 0);
+    has[i] = __ballot(at < groups && A.splits[at].parts != 0);
     if ((tid & 63) == 0) counts[i][tid >> 6] = __popcll(has[i]);
   }
   __syncthreads();
@@ -617,81 +663,83 @@ __global__ __launch_bounds__(kMergeThreads) void tree_merge_kernel(TreeArgs A, i
 #pragma unroll
     for (int v = 0; v < kMergeThreads / 64; ++v) {
       if (v == tid >> 6 && has[i] >> (tid & 63) & 1 &&
-          before + __popcll(has[i] & ((uint64_t(1) << (tid & 63)) - 1)) == int(blockIdx.x))
+          before + __popcll(has[i] & ((uint64_t(1) << (tid & 63)) - 1)) == x)
         found = kMergeThreads * i + tid;
       before += counts[i][v];
     }
   __syncthreads();
-  const int w = found;
+  return found;
+}
+
+template <int kPerRow>
+__global__ __launch_bounds__(kMergeThreads) void tree_merge_kernel(TreeArgs A, int groups, int tile_rows) {
+  constexpr int kBatch = kPerRow == 1 ? 2 : 4;  // parts that a group loads at a time
+  const int w = kPerRow == 1 ? int(blockIdx.x) : find_split(A, groups, blockIdx.x);
   if (w < 0) return;
-  const int32_t* split = A.splits + w * kSplitInts;
-  const Split s{split[0], split[1], split[2], split[3], split[4]};
+  const Split s = A.splits[w];
   const int n = s.parts;
-  const int per_row = n <= kMergeBatch ? 1 : n <= 4 * kMergeBatch ? 4 : kMergeGroups;
-  const int at_once = kMergeGroups / per_row;
-  const int grp = tid >> 4, t = tid & 15, k = grp % per_row;
-  const int first = blockIdx.y * block_rows;
-  for (int i0 = 0; i0 < block_rows; i0 += at_once) {
-    const int i = i0 + grp / per_row, in_tile = first + i;
-    const int r = s.tile * tile_rows + in_tile;
-    const int node = r / A.group, head = r - node * A.group;
-    const bool live = i < block_rows && node < s.nodes;
-    float M = -INFINITY, sum = 0.f, acc[8] = {};
-    auto fold = [&](float Mk, float wk, const float (&xk)[8]) {
-      // A part without a key of the row adds nothing, whatever else it holds; a NaN makes a NaN.
-      const float Mn = fmaxf(M, Mk);
-      const float a = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - Mn);
-      const float c = Mk == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(Mk - Mn);
-      sum = sum * a + wk * c;
+  if (n == 0) return;
+  const int tid = threadIdx.x, grp = tid >> 4, t = tid & 15, k = grp % kPerRow;
+  const int in_tile = int(blockIdx.y) * (kMergeGroups / kPerRow) + grp / kPerRow;
+  const int r = s.tile * tile_rows + in_tile;
+  const int node = r / A.group, head = r - node * A.group;
+  const bool live = node < s.nodes;
+  if (kPerRow == 1 && !live) return;
+  float M = -INFINITY, sum = 0.f, acc[8] = {};
+  auto fold = [&](float Mk, float wk, const float (&xk)[8]) {
+    // A part without a key of the row adds nothing, whatever else it holds; a NaN makes a NaN.
+    const float Mn = fmaxf(M, Mk);
+    const float a = M == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(M - Mn);
+    const float c = Mk == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(Mk - Mn);
+    sum = sum * a + wk * c;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) acc[e] = (a == 0.f ? 0.f : acc[e] * a) + (c == 0.f ? 0.f : xk[e] * c);
-      M = Mn;
-    };
-    for (int j0 = k * kMergeBatch; j0 < n; j0 += per_row * kMergeBatch) {
-      float lj[kMergeBatch];
-      f32x4 lo[kMergeBatch], hi[kMergeBatch];
+    for (int e = 0; e < 8; ++e) acc[e] = (a == 0.f ? 0.f : acc[e] * a) + (c == 0.f ? 0.f : xk[e] * c);
+    M = Mn;
+  };
+  for (int j0 = k * kBatch; j0 < n; j0 += kPerRow * kBatch) {
+    float lj[kBatch];
+    f32x4 lo[kBatch], hi[kBatch];
 #pragma unroll
-      for (int j = 0; j < kMergeBatch; ++j) {
-        lj[j] = -INFINITY;
-        lo[j] = hi[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (live && j0 + j < n) {
-          const size_t slot = j0 + j == 0 ? size_t(2) * w + 1 : size_t(2) * (w + j0 + j);
-          lj[j] = A.part_lse[slot * tile_rows + in_tile];
-          const f32x4* o = reinterpret_cast<const f32x4*>(A.part_o + (slot * tile_rows + in_tile) * kDim + 8 * t);
-          lo[j] = o[0], hi[j] = o[1];
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < kMergeBatch; ++j) {
-        const float x[8] = {lo[j][0], lo[j][1], lo[j][2], lo[j][3], hi[j][0], hi[j][1], hi[j][2], hi[j][3]};
-        fold(lj[j], 1.f, x);
+    for (int j = 0; j < kBatch; ++j) {
+      lj[j] = -INFINITY;
+      lo[j] = hi[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+      if (live && j0 + j < n) {
+        const size_t slot = j0 + j == 0 ? size_t(2) * w + 1 : size_t(2) * (w + j0 + j);
+        lj[j] = A.part_lse[slot * tile_rows + in_tile];
+        const f32x4* o = reinterpret_cast<const f32x4*>(A.part_o + (slot * tile_rows + in_tile) * kDim + 8 * t);
+        lo[j] = o[0], hi[j] = o[1];
       }
     }
-    if (per_row > 1) {
-      float* mine = shared[grp][t];
-      mine[0] = M, mine[1] = sum;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) mine[2 + e] = acc[e];
-      __syncthreads();
-      if (k == 0)
-        for (int o = 1; o < per_row; ++o) {
-          const float* other = shared[grp + o][t];
-          float x[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = other[2 + e];
-          fold(other[0], other[1], x);
-        }
-      __syncthreads();
+    for (int j = 0; j < kBatch; ++j) {
+      const float x[8] = {lo[j][0], lo[j][1], lo[j][2], lo[j][3], hi[j][0], hi[j][1], hi[j][2], hi[j][3]};
+      fold(lj[j], 1.f, x);
     }
-    if (k == 0 && live) {
-      const float inv = sum == 0.f ? 0.f : 1.f / sum;
-      const size_t orow = size_t(s.row0 + node) * A.hq + size_t(s.g) * A.group + head;
-      uint32_t o[4];
+  }
+  if constexpr (kPerRow > 1) {
+    __shared__ __align__(16) float shared[kMergeGroups][16][12];
+    float* mine = shared[grp][t];
+    mine[0] = M, mine[1] = sum;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) o[e] = pack_bf16x2(acc[2 * e] * inv, acc[2 * e + 1] * inv);
-      *reinterpret_cast<uint4*>(A.out + orow * kDim + 8 * t) = make_uint4(o[0], o[1], o[2], o[3]);
-      if (A.lse && t == 0) A.lse[orow] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
+    for (int e = 0; e < 8; ++e) mine[2 + e] = acc[e];
+    __syncthreads();
+    if (k > 0) return;
+    for (int o = 1; o < kPerRow; ++o) {
+      const float* other = shared[grp + o][t];
+      float x[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) x[e] = other[2 + e];
+      fold(other[0], other[1], x);
     }
+  }
+  if (live) {
+    const float inv = sum == 0.f ? 0.f : 1.f / sum;
+    const size_t orow = size_t(s.row0 + node) * A.hq + size_t(s.g) * A.group + head;
+    uint32_t o[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] = pack_bf16x2(acc[2 * e] * inv, acc[2 * e + 1] * inv);
+    *reinterpret_cast<uint4*>(A.out + orow * kDim + 8 * t) = make_uint4(o[0], o[1], o[2], o[3]);
+    if (A.lse && t == 0) A.lse[orow] = sum == 0.f ? -INFINITY : (M + log2f(sum)) * kLn2;
   }
 }
 
@@ -713,7 +761,7 @@ TreeArgs tree_args(const KvLayout& L, const TreeCall& c, int waves) {
   const size_t part_rows = size_t(2) * groups_of(waves) * 32 * waves;
   A.part_o = static_cast<float*>(c.ws);
   A.part_lse = A.part_o + part_rows * kDim;
-  A.splits = reinterpret_cast<int32_t*>(A.part_lse + part_rows);
+  A.splits = reinterpret_cast<Split*>(A.part_lse + part_rows);
   A.rows = int(c.rows);
   A.most = int(std::min<int64_t>(c.stride * kPage, INT32_MAX - 64));
   A.last_page = uint32_t(std::min<int64_t>(L.desc.num_pages - 1, INT32_MAX));
@@ -726,7 +774,7 @@ TreeArgs tree_args(const KvLayout& L, const TreeCall& c, int waves) {
 
 size_t tree_workspace(int64_t rows, int32_t batch, int32_t hq, int32_t hkv) {
   const int waves = waves_of(rows, batch, hq / hkv);
-  return size_t(groups_of(waves)) * (size_t(2) * 32 * waves * (kDim + 1) * sizeof(float) + kSplitInts * sizeof(int32_t));
+  return size_t(groups_of(waves)) * (size_t(2) * 32 * waves * (kDim + 1) * sizeof(float) + sizeof(Split));
 }
 
 hipError_t launch_tree(const KvLayout& L, const TreeCall& c, hipStream_t s) {
@@ -745,15 +793,17 @@ hipError_t launch_tree(const KvLayout& L, const TreeCall& c, hipStream_t s) {
 hipError_t launch_tree_merge(const KvLayout& L, const TreeCall& c, hipStream_t s) {
   const int waves = waves_of(c.rows, c.batch, c.hq / L.desc.num_kv_heads);
   const TreeArgs A = tree_args(L, c, waves);
-  // At most as many items are split as there are, or workgroups.
   const int rows = 32 * waves, groups = groups_of(waves);
+  // Items, at most, and with them the parts of one, about.
   const int64_t items = A.hkv * (int64_t(c.batch) + c.rows * A.group / rows);
-  const unsigned x = unsigned(std::min<int64_t>(items, groups));
-  int block_rows = 16;
-  while (block_rows > 1 && x * (rows / block_rows) < 2048) block_rows /= 2;
-  hipLaunchKernelGGL(tree_merge_kernel, dim3(x, unsigned(rows / block_rows)), dim3(kMergeThreads), 0, s, A, groups,
-                     rows, block_rows);
-  return hipGetLastError();
+  auto launch = [&](auto kernel, int64_t x, int per_row) {
+    hipLaunchKernelGGL(kernel, dim3(unsigned(x), unsigned(rows * per_row / kMergeGroups)), dim3(kMergeThreads), 0, s, A,
+                       groups, rows);
+    return hipGetLastError();
+  };
+  if (groups <= 4 * items) return launch(tree_merge_kernel<1>, groups, 1);
+  if (groups <= 32 * items) return launch(tree_merge_kernel<4>, std::min<int64_t>(items, groups), 4);
+  return launch(tree_merge_kernel<16>, std::min<int64_t>(items, groups), 16);
 }
 
 }  // namespace libra
