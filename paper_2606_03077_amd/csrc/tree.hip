@@ -48,7 +48,8 @@ constexpr int kStepKeys = 32;
 constexpr int kMinSteps = 4;
 constexpr int kTau = 8;
 constexpr float kSumTau = float(1 << kTau);
-constexpr int kMaskWords = 8;
+constexpr int kMaskWords = LIBRA_MAX_MASK_WORDS;
+constexpr int kPartBlock = 32 * kDim / 4;  // 32 rows of a part, in fours of floats
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
@@ -603,30 +604,36 @@ void tree_ring_kernel(TreeArgs A) {
     // Row col's sum over both lane halves.
     const float ls = R.l + __shfl_xor(R.l, 32);
     const float inv = ls > 0.f ? 1.f / ls : ls == 0.f ? 0.f : ls;  // a NaN stays
-    if (row_node < s.nodes) {
-      if (step0 == 0 && step1 == s.steps) {
-        const size_t orow = size_t(s.row0 + row_node) * A.hq + size_t(g) * G + row_head;
-        uint16_t* o = A.out + orow * kDim + 4 * hh;
+    if (step0 == 0 && step1 == s.steps) {
+      const size_t orow = size_t(s.row0 + row_node) * A.hq + size_t(g) * G + row_head;
+      uint4* const o = reinterpret_cast<uint4*>(A.out + orow * kDim);
 #pragma unroll
-        for (int cb = 0; cb < 4; ++cb)
+      for (int cb = 0; cb < 4; ++cb)
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            *reinterpret_cast<uint2*>(o + 32 * cb + 8 * e) =
-                make_uint2(pack_bf16x2(R.acc[cb][4 * e] * inv, R.acc[cb][4 * e + 1] * inv),
-                           pack_bf16x2(R.acc[cb][4 * e + 2] * inv, R.acc[cb][4 * e + 3] * inv));
-        if (A.lse && hh == 0) A.lse[orow] = ls == 0.f ? -INFINITY : (R.m + log2f(ls)) * kLn2;
-      } else {
-        const size_t prow = (size_t(2) * w + (step0 == 0 ? 1 : 0)) * kRows + 32 * wave + col;
-        float* o = A.part_o + prow * kDim + 4 * hh;
+        for (int e = 0; e < 4; e += 2) {
+          // The row's lanes exchange halves, so that each has eight channels: granule e or e + 1.
+          uint32_t x[4];
 #pragma unroll
-        for (int cb = 0; cb < 4; ++cb)
+          for (int i = 0; i < 2; ++i) {
+            const auto r = __builtin_amdgcn_permlane32_swap(
+                pack_bf16x2(R.acc[cb][4 * e + 2 * i] * inv, R.acc[cb][4 * e + 2 * i + 1] * inv),
+                pack_bf16x2(R.acc[cb][4 * e + 4 + 2 * i] * inv, R.acc[cb][4 * e + 5 + 2 * i] * inv), false, false);
+            x[i] = r[0], x[2 + i] = r[1];
+          }
+          if (row_node < s.nodes) o[4 * cb + e + hh] = make_uint4(x[0], x[1], x[2], x[3]);
+        }
+      if (row_node < s.nodes && A.lse && hh == 0) A.lse[orow] = ls == 0.f ? -INFINITY : (R.m + log2f(ls)) * kLn2;
+    } else if (row_node < s.nodes) {
+      // A part, as the lanes hold it: four channels of a lane after those of the lane before.
+      const size_t block = (size_t(2) * w + (step0 == 0 ? 1 : 0)) * kWaves + wave;
+      f32x4* const o = reinterpret_cast<f32x4*>(A.part_o) + block * kPartBlock + lane;
 #pragma unroll
-          for (int e = 0; e < 4; ++e)
-            *reinterpret_cast<f32x4*>(o + 32 * cb + 8 * e) =
-                f32x4{R.acc[cb][4 * e] * inv, R.acc[cb][4 * e + 1] * inv, R.acc[cb][4 * e + 2] * inv,
-                      R.acc[cb][4 * e + 3] * inv};
-        if (hh == 0) A.part_lse[prow] = ls == 0.f ? -INFINITY : R.m + log2f(ls);
-      }
+      for (int cb = 0; cb < 4; ++cb)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          o[(4 * cb + e) * 64] = f32x4{R.acc[cb][4 * e] * inv, R.acc[cb][4 * e + 1] * inv, R.acc[cb][4 * e + 2] * inv,
+                                       R.acc[cb][4 * e + 3] * inv};
+      if (hh == 0) A.part_lse[block * 32 + col] = ls == 0.f ? -INFINITY : R.m + log2f(ls);
     }
     if (step1 < s.steps && step0 == 0 && tid == 0) {
       // The item's other parts are those of the workgroups after this one, n_steps each.
@@ -679,8 +686,10 @@ __global__ __launch_bounds__(kMergeThreads) void tree_merge_kernel(TreeArgs A, i
   const Split s = A.splits[w];
   const int n = s.parts;
   if (n == 0) return;
-  const int tid = threadIdx.x, grp = tid >> 4, t = tid & 15, k = grp % kPerRow;
-  const int in_tile = int(blockIdx.y) * (kMergeGroups / kPerRow) + grp / kPerRow;
+  // Neighbouring lanes take neighbouring rows, whose parts lie together; t: eight channels.
+  constexpr int kBlockRows = kMergeGroups / kPerRow;
+  const int tid = threadIdx.x, t = tid / kBlockRows % 16, k = tid / (16 * kBlockRows);
+  const int in_tile = int(blockIdx.y) * kBlockRows + tid % kBlockRows;
   const int r = s.tile * tile_rows + in_tile;
   const int node = r / A.group, head = r - node * A.group;
   const bool live = node < s.nodes;
@@ -706,8 +715,9 @@ __global__ __launch_bounds__(kMergeThreads) void tree_merge_kernel(TreeArgs A, i
       if (live && j0 + j < n) {
         const size_t slot = j0 + j == 0 ? size_t(2) * w + 1 : size_t(2) * (w + j0 + j);
         lj[j] = A.part_lse[slot * tile_rows + in_tile];
-        const f32x4* o = reinterpret_cast<const f32x4*>(A.part_o + (slot * tile_rows + in_tile) * kDim + 8 * t);
-        lo[j] = o[0], hi[j] = o[1];
+        const f32x4* o = reinterpret_cast<const f32x4*>(A.part_o) + (slot * tile_rows + in_tile) / 32 * kPartBlock +
+                         t * 64 + in_tile % 32;
+        lo[j] = o[0], hi[j] = o[32];
       }
     }
 #pragma unroll
@@ -717,15 +727,15 @@ __global__ __launch_bounds__(kMergeThreads) void tree_merge_kernel(TreeArgs A, i
     }
   }
   if constexpr (kPerRow > 1) {
-    __shared__ __align__(16) float shared[kMergeGroups][16][12];
-    float* mine = shared[grp][t];
+    __shared__ float shared[kMergeThreads][11];
+    float* mine = shared[tid];
     mine[0] = M, mine[1] = sum;
 #pragma unroll
     for (int e = 0; e < 8; ++e) mine[2 + e] = acc[e];
     __syncthreads();
     if (k > 0) return;
     for (int o = 1; o < kPerRow; ++o) {
-      const float* other = shared[grp + o][t];
+      const float* other = shared[tid + o * 16 * kBlockRows];
       float x[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) x[e] = other[2 + e];
