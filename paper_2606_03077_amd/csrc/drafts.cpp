@@ -159,7 +159,7 @@ libra_status libra_qk_norm_rotary(libra_rotary rotary, int32_t dtype, int32_t we
     return RotaryRows{t.x, t.out, t.x_row_stride, t.x_head_stride, t.out_row_stride, t.out_head_stride,
                       positions, rows, t.num_heads, dtype, false};
   };
-  const RowNorms norms{{tq.weight, weight_dtype, eps}, {tk.weight, weight_dtype, eps}};
+  const RowNorms norms{head_norm(tq.weight, weight_dtype, eps), head_norm(tk.weight, weight_dtype, eps)};
   hipError_t e;
   {
     ProfScope ps(LIBRA_KERNEL_ROTARY, static_cast<hipStream_t>(stream), true);
@@ -197,7 +197,7 @@ libra_status libra_qk_norm_rotary_backward(libra_rotary rotary, int32_t dtype, i
     return NormBackRows{t.x, t.grad, t.out, t.x_row_stride, t.x_head_stride, t.grad_row_stride,
                         t.grad_head_stride, t.out_row_stride, t.out_head_stride, t.num_heads, dw};
   };
-  const RowNorms norms{{tq.weight, weight_dtype, eps}, {tk.weight, weight_dtype, eps}};
+  const RowNorms norms{head_norm(tq.weight, weight_dtype, eps), head_norm(tk.weight, weight_dtype, eps)};
   hipError_t e;
   {
     ProfScope ps(LIBRA_KERNEL_ROTARY, static_cast<hipStream_t>(stream), true);
@@ -241,7 +241,7 @@ libra_status libra_kv_append_norm(libra_kv_layout layout, libra_rotary rotary, i
       return set_error(LIBRA_E_INVAL, "in place, q's rows must be dense");
   }
   const NewRows n{rotary, positions, q, k_new, v_new, q_row_stride, k_row_stride, v_row_stride};
-  const RowNorms norms{{q_weight, weight_dtype, eps}, {k_weight, weight_dtype, eps}};
+  const RowNorms norms{head_norm(q_weight, weight_dtype, eps), head_norm(k_weight, weight_dtype, eps)};
   hipError_t e;
   {
     ProfScope ps(LIBRA_KERNEL_CACHE_WRITE, static_cast<hipStream_t>(stream), true);

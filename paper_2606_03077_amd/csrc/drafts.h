@@ -11,7 +11,12 @@ struct HeadNorm {
   const void* weight;  // [head size], of weight_dtype
   int32_t weight_dtype;
   float eps;
+  int32_t quads;  // whether the weight is aligned to four of its elements
 };
+inline HeadNorm head_norm(const void* weight, int32_t dtype, float eps) {
+  const size_t quad = dtype == LIBRA_DTYPE_FP32 ? 16 : 8;
+  return {weight, dtype, eps, reinterpret_cast<uintptr_t>(weight) % quad == 0};
+}
 // The norms of a call's queries and keys.
 struct RowNorms {
   HeadNorm q, k;

@@ -7,6 +7,7 @@
 // that an ended request of thousands of pages is everybody's work.  Pages given back are pushed
 // before any is taken.
 #include <algorithm>
+#include <climits>
 
 #include "drafts.h"
 #include "row_types.h"
@@ -14,26 +15,37 @@
 namespace libra {
 namespace {
 
-constexpr int kMapThreads = 1024;
-constexpr int kMapWaves = kMapThreads / 64;
+constexpr int kMapThreads = 1024;  // of the form that takes requests in turns
+
+// Int: 32 bits where the call's sizes cannot exceed them, which takes half the scans' time.
+template <class Int>
+struct Sums {
+  Int back, need, rows;
+};
+template <class Int>
+__device__ __forceinline__ Sums<Int> operator+(const Sums<Int>& a, const Sums<Int>& b) {
+  return {a.back + b.back, a.need + b.need, a.rows + b.rows};
+}
 
 // Inclusive sums over the workgroup's threads, and their total.
-__device__ __forceinline__ int64_t block_scan(int64_t x, int64_t* wave_sums, int64_t& total) {
+template <int kThreads, class Int>
+__device__ __forceinline__ Sums<Int> block_scan(Sums<Int> x, Sums<Int>* wave_sums, Sums<Int>& total) {
+  constexpr int kWaves = kThreads / 64;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
   for (int n = 1; n < 64; n <<= 1) {
-    const int64_t y = __shfl_up(x, n);
-    if (lane >= n) x += y;
+    const Sums<Int> y{__shfl_up(x.back, n), __shfl_up(x.need, n), __shfl_up(x.rows, n)};
+    if (lane >= n) x = x + y;
   }
   __syncthreads();  // the sums of an earlier scan have been read
   if (lane == 63) wave_sums[wave] = x;
   __syncthreads();
-  int64_t before = 0;
-  total = 0;
+  Sums<Int> before{};
+  total = {};
 #pragma unroll
-  for (int w = 0; w < kMapWaves; ++w) {
-    if (w < wave) before += wave_sums[w];
-    total += wave_sums[w];
+  for (int w = 0; w < kWaves; ++w) {
+    if (w < wave) before = before + wave_sums[w];
+    total = total + wave_sums[w];
   }
   return x + before;
 }
@@ -53,6 +65,12 @@ __device__ __forceinline__ int find(const Int* sums, int n, Int x) {
 struct Request {
   int64_t prior, added, held, want;
   bool valid;
+  // Rows past the call's do not count, so that their sum stays in bounds.
+  template <class Int>
+  __device__ __forceinline__ Sums<Int> sums(int64_t rows) const {
+    return {valid ? Int(max(held - want, int64_t(0))) : 0, valid ? Int(max(want - held, int64_t(0))) : 0,
+            Int(min(max(added, int64_t(0)), rows + 1))};
+  }
 };
 __device__ __forceinline__ Request load_request(const MapArgs& A, int b) {
   Request r{};
@@ -63,91 +81,125 @@ __device__ __forceinline__ Request load_request(const MapArgs& A, int b) {
   return r;
 }
 
-// Slot and position of row r, request b's.
-__device__ __forceinline__ void map_row(const MapArgs& A, int64_t r, int b, int64_t total) {
-  int64_t slot = -1;
-  int32_t position = 0;
-  if (r < total) {
-    const int64_t prior = A.prior[b], at = prior + r - A.starts[b];
-    if (!A.refused[b]) slot = int64_t(A.table[b * A.stride + at / kPage]) * kPage + at % kPage;
-    position = int32_t(A.depths ? prior + A.depths[r] : at);
-  }
-  A.slots[r] = slot;
-  A.positions[r] = position;
+// Row r of request b, whose first row is `start`.
+__device__ __forceinline__ void map_row(const MapArgs& A, int64_t r, int b, int64_t start, int64_t prior,
+                                        bool refused) {
+  const int64_t at = prior + r - start;
+  A.slots[r] = refused ? -1 : int64_t(A.table[b * A.stride + at / kPage]) * kPage + at % kPage;
+  A.positions[r] = int32_t(A.depths ? prior + A.depths[r] : at);
 }
+__device__ __forceinline__ void pad_row(const MapArgs& A, int64_t r) { A.slots[r] = -1, A.positions[r] = 0; }
 
+// kTurns: more requests than threads, which are taken in turns and read again in the second pass.
+// Otherwise a request stays in its thread's registers, and what the rows need of it in LDS.
 // rows: how many of the rows this launch maps too (all or none).
-__global__ __launch_bounds__(kMapThreads) void kv_map_kernel(MapArgs A, int64_t rows) {
-  __shared__ int64_t wave_sums[kMapWaves];
-  __shared__ int64_t sums[kMapThreads];
+template <int kThreads, bool kTurns, class Int>
+__global__ __launch_bounds__(kThreads) void kv_map_kernel(MapArgs A, int64_t rows) {
+  __shared__ Sums<Int> wave_sums[kThreads / 64];
+  __shared__ Int upto[kThreads];  // of pages
+  __shared__ int32_t start[kThreads], prior[kThreads], held[kThreads], want[kThreads];
+  __shared__ uint8_t refusal[kThreads];
+  __shared__ unsigned long long given_upto;
   const int t = threadIdx.x;
   const int64_t have = min(max(int64_t(*A.num_free), int64_t(0)), A.capacity);
-  int64_t top = have, total;
+  int64_t top = have;
+  Request q;
+  Sums<Int> sums, total;
+  if (t == 0) given_upto = 0;
   // Pages given back.
-  for (int b0 = 0; b0 < A.batch; b0 += kMapThreads) {
-    const Request q = load_request(A, b0 + t);
-    const int64_t upto = block_scan(q.valid ? max(q.held - q.want, int64_t(0)) : 0, wave_sums, total);
-    if (total == 0) continue;  // uniform
-    sums[t] = upto;
-    __syncthreads();
-    for (int64_t i = t; i < total; i += kMapThreads) {
-      const int n = find(sums, kMapThreads, i);
-      // The request's last surplus page is its last held one.
-      const int64_t column = A.held[b0 + n] - (sums[n] - i);
-      if (top + i < A.capacity) A.free_pages[top + i] = A.table[(b0 + n) * A.stride + column];
+  for (int b0 = 0; b0 < A.batch; b0 += kThreads) {
+    q = load_request(A, b0 + t);
+    sums = block_scan<kThreads>(q.sums<Int>(A.rows), wave_sums, total);
+    if (total.back > 0) {  // uniform
+      upto[t] = sums.back, held[t] = int32_t(q.held);
+      __syncthreads();
+#pragma unroll 4
+      for (Int i = t; i < total.back; i += kThreads) {
+        const int n = find(upto, min(kThreads, A.batch - b0), i);
+        // The request's last surplus page is its last held one.
+        if (top + i < A.capacity)
+          A.free_pages[top + i] = A.table[(b0 + n) * A.stride + held[n] - (upto[n] - i)];
+      }
+      top = min(top + total.back, A.capacity);
     }
-    top = min(top + total, A.capacity);
   }
   __syncthreads();  // the pages given back can be read
-  int64_t asked = 0, given = 0, row0 = 0;
-  for (int b0 = 0; b0 < A.batch; b0 += kMapThreads) {
+  Int asked = 0;
+  int64_t row0 = 0;
+  for (int b0 = 0; b0 < A.batch; b0 += kThreads) {
     const int b = b0 + t;
-    const Request q = load_request(A, b);
-    const int64_t need = q.valid ? max(q.want - q.held, int64_t(0)) : 0;
-    const int64_t upto = asked + block_scan(need, wave_sums, total);
-    const int64_t wanted = total;
-    int64_t n_rows;
-    const int64_t row1 = row0 + block_scan(max(q.added, int64_t(0)), wave_sums, n_rows);
+    if (kTurns) {
+      q = load_request(A, b);
+      sums = block_scan<kThreads>(q.sums<Int>(A.rows), wave_sums, total);
+    }
+    const Sums<Int> own = q.sums<Int>(A.rows);
+    const Int need = own.need, asked_upto = asked + sums.need;
+    const int64_t row1 = row0 + sums.rows;
     // Once a request is refused for want of pages, so is every later one that needs any: those that
     // get theirs take the first of the pages asked for.
-    const bool refused = !q.valid || (need > 0 && upto > top);
-    sums[t] = upto;
-    int64_t granted;
-    block_scan(refused ? 0 : need, wave_sums, granted);
+    const bool refused = !q.valid || (need > 0 && asked_upto > top);
+    upto[t] = asked_upto, refusal[t] = refused, want[t] = int32_t(q.valid ? q.want : 0);
+    start[t] = int32_t(min(row1 - own.rows, A.rows)), prior[t] = int32_t(q.prior);
+    if (!refused && need > 0) atomicMax(&given_upto, (unsigned long long)asked_upto);
     if (b < A.batch) {
       A.starts[b + 1] = int32_t(min(row1, A.rows));
       A.held_out[b] = int32_t(refused ? q.held : q.want);
       A.refused[b] = refused;
     }
-    __syncthreads();  // sums, refused and starts of this turn
-    for (int64_t i = t; i < wanted; i += kMapThreads) {
-      const int n = find(sums, kMapThreads, asked + i);
-      if (A.refused[b0 + n]) continue;
-      const int64_t want = (int64_t(A.prior[b0 + n]) + A.added[b0 + n] + kPage - 1) / kPage;
-      A.table[(b0 + n) * A.stride + want - (sums[n] - asked - i)] = A.free_pages[top - 1 - asked - i];
+    __syncthreads();
+#pragma unroll 4
+    for (Int i = t; i < total.need; i += kThreads) {
+      const int n = find(upto, min(kThreads, A.batch - b0), Int(asked + i));
+      if (refusal[n]) continue;
+      A.table[(b0 + n) * A.stride + want[n] - (upto[n] - asked - i)] = A.free_pages[top - 1 - asked - i];
     }
-    asked += wanted, given += granted, row0 += n_rows;
+    asked += total.need, row0 += total.rows;
     __syncthreads();
   }
-  if (t == 0) *A.num_free_out = int32_t(top - given);
+  if (t == 0) *A.num_free_out = int32_t(top - int64_t(given_upto));
   if (t == 0) A.starts[0] = 0;
   __syncthreads();
   row0 = min(row0, A.rows);
-  for (int64_t r = t; r < rows; r += kMapThreads)
-    map_row(A, r, r < row0 ? find(A.starts + 1, A.batch, int32_t(r)) : 0, row0);
+#pragma unroll 4
+  for (int64_t r = t; r < rows; r += kThreads) {
+    if (r >= row0) {
+      pad_row(A, r);
+    } else if (kTurns) {
+      const int b = find(A.starts + 1, A.batch, int32_t(r));
+      map_row(A, r, b, A.starts[b], A.prior[b], A.refused[b]);
+    } else {
+      // The last request that starts at or before the row (threads past the batch start after it).
+      int lo = 0, hi = A.batch - 1;
+      while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (start[mid] <= r) lo = mid;
+        else hi = mid - 1;
+      }
+      map_row(A, r, lo, start[lo], prior[lo], refusal[lo]);
+    }
+  }
 }
 
 constexpr int kRowThreads = 256;
+constexpr int kRowStarts = 2048;  // requests whose starts a workgroup searches in LDS
 __global__ __launch_bounds__(kRowThreads) void kv_map_rows_kernel(MapArgs A) {
+  __shared__ int32_t ends[kRowStarts];
+  const bool staged = A.batch <= kRowStarts;
+  if (staged) {
+    for (int b = threadIdx.x; b < A.batch; b += kRowThreads) ends[b] = A.starts[b + 1];
+    __syncthreads();
+  }
   const int64_t r = int64_t(blockIdx.x) * kRowThreads + threadIdx.x;
   if (r >= A.rows) return;
-  const int64_t total = A.starts[A.batch];
-  map_row(A, r, r < total ? find(A.starts + 1, A.batch, int32_t(r)) : 0, total);
+  if (A.batch == 0 || r >= (staged ? ends[A.batch - 1] : A.starts[A.batch])) return pad_row(A, r);
+  const int b = staged ? find(ends, A.batch, int32_t(r)) : find(A.starts + 1, A.batch, int32_t(r));
+  map_row(A, r, b, A.starts[b], A.prior[b], A.refused[b]);
 }
 
 // One workgroup per (sequence, KV head): accepted tokens 16 at a time, 16 threads to a token.  Nodes
 // come in ascending order, so a token's new place is behind none that is still to be read; within
-// the 16 all are read before one is written.
+// the 16 all are read before one is written.  A thread moves a key's granule, and eight values 16
+// channels apart, so that neighbouring threads touch neighbouring granules of the V tile.
 __global__ __launch_bounds__(256) void kv_accept_kernel(AcceptArgs A) {
   const int b = int(blockIdx.x) / A.hkv, g = int(blockIdx.x) - b * A.hkv;
   const int s = threadIdx.x >> 4, j = threadIdx.x & 15;
@@ -174,28 +226,38 @@ __global__ __launch_bounds__(256) void kv_accept_kernel(AcceptArgs A) {
       const int sl = int((prior + node) % kPage);
       k = *reinterpret_cast<const uint4*>(A.k_cache + from + k_off(sl, 8 * j));
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] = A.v_cache[from + v_off(sl, 8 * j + e)];
+      for (int e = 0; e < 8; ++e) v[e] = A.v_cache[from + v_off(sl, j + 16 * e)];
     }
     __syncthreads();
     if (moves) {
       const int sl = int((prior + i) % kPage);
       *reinterpret_cast<uint4*>(A.k_cache + to + k_off(sl, 8 * j)) = k;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) A.v_cache[to + v_off(sl, 8 * j + e)] = v[e];
+      for (int e = 0; e < 8; ++e) A.v_cache[to + v_off(sl, j + 16 * e)] = v[e];
     }
     __syncthreads();
   }
 }
 
 // Rows that the one workgroup maps itself, instead of a second launch.
-constexpr int64_t kOneLaunchRows = 4096;
+constexpr int64_t kOneLaunchRows = 1024;
 
 }  // namespace
 
 hipError_t launch_kv_map(const MapArgs& a, hipStream_t s) {
   const bool one = a.rows <= kOneLaunchRows;
-  hipLaunchKernelGGL(kv_map_kernel, dim3(1), dim3(kMapThreads), 0, s, a, one ? a.rows : 0);
-  const hipError_t e = hipGetLastError();
+  auto launch = [&](auto kernel, int threads) {
+    hipLaunchKernelGGL(kernel, dim3(1), dim3(unsigned(threads)), 0, s, a, one ? a.rows : 0);
+    return hipGetLastError();
+  };
+  // 64 requests of one token each take 5 us with 256 threads, 10 with 1,024; but pages that move
+  // are worth more threads.
+  const bool small = std::max(a.stride, a.rows + 1) * int64_t(std::max(a.batch, 1)) <= INT32_MAX;
+  const hipError_t e =
+      a.batch > kMapThreads ? launch(kv_map_kernel<kMapThreads, true, int64_t>, kMapThreads)
+      : !small              ? launch(kv_map_kernel<kMapThreads, false, int64_t>, kMapThreads)
+      : a.batch > 64        ? launch(kv_map_kernel<kMapThreads, false, int32_t>, kMapThreads)
+                            : launch(kv_map_kernel<256, false, int32_t>, 256);
   if (e != hipSuccess || one) return e;
   hipLaunchKernelGGL(kv_map_rows_kernel, dim3(unsigned((a.rows + kRowThreads - 1) / kRowThreads)), dim3(kRowThreads),
                      0, s, a);

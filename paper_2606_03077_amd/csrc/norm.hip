@@ -17,6 +17,7 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kMaxPairs = kMaxRotaryDim / 2;
 constexpr int kMaxParts = 1024;  // workgroups of one tensor
+constexpr int64_t kPastBytes = int64_t(128) << 20;  // of dx, from which nothing goes through the caches
 
 template <class T>
 struct BackArgs {
@@ -37,7 +38,7 @@ struct BackCall {
 
 // Wide form: a power of two of channels, R a multiple of 8, everything aligned for four channels.
 // A thread owns two quads of a head: four pairs, or eight channels that are not turned.
-template <class T, bool kInter>
+template <class T, bool kInter, int kHeads, bool kPastCaches>
 __device__ __forceinline__ void back_wide(const RotaryArgs<kMaxPairs>& rot, const BackArgs<T>& A,
                                           const BackCall& C, int block, float (*sums)[8]) {
   using Quad = typename T::Quad;
@@ -49,9 +50,8 @@ __device__ __forceinline__ void back_wide(const RotaryArgs<kMaxPairs>& rot, cons
   const bool turned = j < R8;
   const int2 qd = quads_of<T, kInter>(j, R8, per_head);
   float wa[4], wb[4], da[4] = {}, db[4] = {};
-#pragma unroll
-  for (int e = 0; e < 4; ++e)
-    wa[e] = norm_weight(A.norm, 4 * qd.x + e), wb[e] = norm_weight(A.norm, 4 * qd.y + e);
+  norm_weights(A.norm, 4 * qd.x, wa);
+  norm_weights(A.norm, 4 * qd.y, wb);
   if (r < A.block_rows) {
     for (int64_t row = int64_t(block) * A.block_rows + r; row < C.rows; row += int64_t(A.blocks) * A.block_rows) {
       float2 cs[4];
@@ -63,42 +63,57 @@ __device__ __forceinline__ void back_wide(const RotaryArgs<kMaxPairs>& rot, cons
           cs[i].y = -cs[i].y;
         }
       }
-      for (int h = h0; h < A.heads; h += A.head_slots) {
-        const typename T::Elem* x = A.x + row * A.x_row + h * A.x_head;
-        const typename T::Elem* dy = A.dy + row * A.dy_row + h * A.dy_head;
-        typename T::Elem* dx = A.dx + row * A.dx_row + h * A.dx_head;
-        float f[4], g[4], u[4], v[4];
-        T::unpack(*reinterpret_cast<const Quad*>(x + 4 * qd.x), f);
-        T::unpack(*reinterpret_cast<const Quad*>(x + 4 * qd.y), g);
-        T::unpack(*reinterpret_cast<const Quad*>(dy + 4 * qd.x), u);
-        T::unpack(*reinterpret_cast<const Quad*>(dy + 4 * qd.y), v);
-        if (turned) {
-          float y[4], z[4];
-          turn_values<kInter>(u, v, cs, y, z);
+      for (int hb = h0; hb < A.heads; hb += kHeads * A.head_slots) {
+        Quad xa[kHeads], xb[kHeads], ya[kHeads], yb[kHeads];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) u[e] = y[e], v[e] = z[e];
+        for (int i = 0; i < kHeads; ++i) {
+          const int h = hb + i * A.head_slots;
+          if (h >= A.heads) continue;
+          const typename T::Elem* x = A.x + row * A.x_row + h * A.x_head;
+          const typename T::Elem* dy = A.dy + row * A.dy_row + h * A.dy_head;
+          xa[i] = load_quad<kPastCaches>(reinterpret_cast<const Quad*>(x + 4 * qd.x));
+          xb[i] = load_quad<kPastCaches>(reinterpret_cast<const Quad*>(x + 4 * qd.y));
+          ya[i] = load_quad<kPastCaches>(reinterpret_cast<const Quad*>(dy + 4 * qd.x));
+          yb[i] = load_quad<kPastCaches>(reinterpret_cast<const Quad*>(dy + 4 * qd.y));
         }
-        float squares = 0.f, along = 0.f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) squares = __builtin_fmaf(f[e], f[e], squares);
+        for (int i = 0; i < kHeads; ++i) {
+          const int h = hb + i * A.head_slots;
+          if (h >= A.heads) continue;  // a head's threads all take part, or none
+          float f[4], g[4], u[4], v[4];
+          T::unpack(xa[i], f);
+          T::unpack(xb[i], g);
+          T::unpack(ya[i], u);
+          T::unpack(yb[i], v);
+          if (turned) {
+            float y[4], z[4];
+            turn_values<kInter>(u, v, cs, y, z);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) squares = __builtin_fmaf(g[e], g[e], squares);
+            for (int e = 0; e < 4; ++e) u[e] = y[e], v[e] = z[e];
+          }
+          float squares = 0.f, along = 0.f;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) along = __builtin_fmaf(u[e] * wa[e], f[e], along);
+          for (int e = 0; e < 4; ++e) squares = __builtin_fmaf(f[e], f[e], squares);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) along = __builtin_fmaf(v[e] * wb[e], g[e], along);
-        const float s = norm_scale(group_sum(squares, per_head), C.dim, A.norm.eps);
-        const float m = group_sum(along, per_head) * s / float(C.dim);  // mean(w du n)
+          for (int e = 0; e < 4; ++e) squares = __builtin_fmaf(g[e], g[e], squares);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float n = f[e] * s, o = g[e] * s;
-          da[e] = __builtin_fmaf(u[e], n, da[e]);
-          db[e] = __builtin_fmaf(v[e], o, db[e]);
-          f[e] = s * __builtin_fmaf(-n, m, u[e] * wa[e]);
-          g[e] = s * __builtin_fmaf(-o, m, v[e] * wb[e]);
+          for (int e = 0; e < 4; ++e) along = __builtin_fmaf(u[e] * wa[e], f[e], along);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) along = __builtin_fmaf(v[e] * wb[e], g[e], along);
+          const float s = norm_scale(group_sum(squares, per_head), C.dim, A.norm.eps);
+          const float m = group_sum(along, per_head) * s / float(C.dim);  // mean(w du n)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float n = f[e] * s, o = g[e] * s;
+            da[e] = __builtin_fmaf(u[e], n, da[e]);
+            db[e] = __builtin_fmaf(v[e], o, db[e]);
+            f[e] = s * __builtin_fmaf(-n, m, u[e] * wa[e]);
+            g[e] = s * __builtin_fmaf(-o, m, v[e] * wb[e]);
+          }
+          typename T::Elem* dx = A.dx + row * A.dx_row + h * A.dx_head;
+          store_quad<kPastCaches>(reinterpret_cast<Quad*>(dx + 4 * qd.x), T::pack(f));
+          store_quad<kPastCaches>(reinterpret_cast<Quad*>(dx + 4 * qd.y), T::pack(g));
         }
-        *reinterpret_cast<Quad*>(dx + 4 * qd.x) = T::pack(f);
-        *reinterpret_cast<Quad*>(dx + 4 * qd.y) = T::pack(g);
       }
     }
   }
@@ -115,13 +130,13 @@ __device__ __forceinline__ void back_wide(const RotaryArgs<kMaxPairs>& rot, cons
   }
 }
 
-template <class T, bool kInter>
+template <class T, bool kInter, int kHeads, bool kPastCaches>
 __global__ __launch_bounds__(kThreads) void norm_back_wide_kernel(RotaryArgs<kMaxPairs> rot, BackArgs<T> Q,
                                                                   BackArgs<T> K, BackCall C) {
   __shared__ float sums[kThreads][8];
   const int i = int(blockIdx.x);
-  if (i < Q.blocks) back_wide<T, kInter>(rot, Q, C, i, sums);
-  else back_wide<T, kInter>(rot, K, C, i - Q.blocks, sums);
+  if (i < Q.blocks) back_wide<T, kInter, kHeads, kPastCaches>(rot, Q, C, i, sums);
+  else back_wide<T, kInter, kHeads, kPastCaches>(rot, K, C, i - Q.blocks, sums);
 }
 
 // Any head size, R, alignment: a wave per head, whose values go through LDS, where a channel finds
@@ -200,7 +215,7 @@ __global__ __launch_bounds__(kThreads) void norm_back_any_kernel(RotaryArgs<kMax
   else back_any<T>(rot, K, C, i - Q.blocks, shared);
 }
 
-// Adds the workgroups' parts of 16 channels of a weight's gradient: 16 threads to a channel, in
+// Adds the workgroups' parts of 16 channels of a weight's gradient: 64 threads to a channel, in
 // float64, which costs nothing here and leaves float32's last rounding alone.
 struct SumArgs {
   const float* parts[2];
@@ -208,19 +223,28 @@ struct SumArgs {
   int blocks[2];
   int dim;
 };
-__global__ __launch_bounds__(kThreads) void norm_weight_sum_kernel(SumArgs A) {
-  __shared__ double sums[16][17];
+constexpr int kSumThreads = 1024, kSumRows = kSumThreads / 16;
+__global__ __launch_bounds__(kSumThreads) void norm_weight_sum_kernel(SumArgs A) {
+  __shared__ double sums[kSumRows][17];
   const int which = blockIdx.y, c = threadIdx.x & 15, k = threadIdx.x >> 4;
   const int d = blockIdx.x * 16 + c, n = A.blocks[which];
+  if (!A.out[which]) return;
   double sum = 0;
-  if (d < A.dim && A.out[which])
-    for (int i = k; i < n; i += 16) sum += double(A.parts[which][size_t(i) * A.dim + d]);
+  if (d < A.dim) {
+#pragma unroll
+    for (int i = 0; i < kMaxParts / kSumRows; ++i)
+      if (k + i * kSumRows < n) sum += double(A.parts[which][size_t(k + i * kSumRows) * A.dim + d]);
+  }
   sums[k][c] = sum;
   __syncthreads();
-  if (k == 0 && d < A.dim && A.out[which]) {
-    for (int i = 1; i < 16; ++i) sum += sums[i][c];
-    A.out[which][d] = float(sum);
-  }
+  if (k < 8)
+    for (int i = k + 8; i < kSumRows; i += 8) sum += sums[i][c];
+  __syncthreads();
+  if (k < 8) sums[k][c] = sum;
+  __syncthreads();
+  if (k > 0 || d >= A.dim) return;
+  for (int i = 1; i < 8; ++i) sum += sums[i][c];
+  A.out[which][d] = float(sum);
 }
 
 bool aligned_quads(const void* p, int64_t row, int64_t head, size_t quad) {
@@ -264,8 +288,14 @@ hipError_t back(const Rotary& r, const NormBackRows& q, const NormBackRows& k, c
   };
   const BackArgs<T> Q = args(q, norms.q, 0), K = args(k, norms.k, 1);
   const BackCall C{positions, rows, dim};
+  const int64_t bytes = rows * (q.heads + k.heads) * dim * int64_t(sizeof(typename T::Elem));
+  const bool past = bytes >= kPastBytes;
+  auto wide_form = [&](auto pairing) {
+    constexpr bool kInter = decltype(pairing)::value;
+    return past ? norm_back_wide_kernel<T, kInter, 4, true> : norm_back_wide_kernel<T, kInter, 4, false>;
+  };
   auto form = !wide ? norm_back_any_kernel<T>
-              : r.pairing == LIBRA_ROTARY_INTERLEAVED ? norm_back_wide_kernel<T, true> : norm_back_wide_kernel<T, false>;
+              : r.pairing == LIBRA_ROTARY_INTERLEAVED ? wide_form(std::true_type{}) : wide_form(std::false_type{});
   if (Q.blocks + K.blocks > 0) {  // none without rows, whose weight gradients are 0
     hipLaunchKernelGGL(form, dim3(unsigned(Q.blocks + K.blocks)), dim3(kThreads), 0, s, rotary_args<kMaxPairs>(r), Q, K, C);
     const hipError_t e = hipGetLastError();
@@ -273,7 +303,7 @@ hipError_t back(const Rotary& r, const NormBackRows& q, const NormBackRows& k, c
   }
   if (!q.dweight && !k.dweight) return hipSuccess;
   const SumArgs S{{Q.parts, K.parts}, {q.dweight, k.dweight}, {Q.blocks, K.blocks}, dim};
-  hipLaunchKernelGGL(norm_weight_sum_kernel, dim3(unsigned((dim + 15) / 16), 2), dim3(kThreads), 0, s, S);
+  hipLaunchKernelGGL(norm_weight_sum_kernel, dim3(unsigned((dim + 15) / 16), 2), dim3(kSumThreads), 0, s, S);
   return hipGetLastError();
 }
 

@@ -105,9 +105,8 @@ __device__ __forceinline__ void turn_rows_wide(const Rot& rot, const RowsArgs<T>
   }
   [[maybe_unused]] float wa[4], wb[4];
   if constexpr (kNorm) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      wa[e] = norm_weight(norm, 4 * qd.x + e), wb[e] = norm_weight(norm, 4 * qd.y + e);
+    norm_weights(norm, 4 * qd.x, wa);
+    norm_weights(norm, 4 * qd.y, wb);
   }
   float2 cs[4];
   if (turned) {
@@ -526,9 +525,8 @@ __device__ __forceinline__ void store_key(const WriteArgs& A, const Rot& rot, co
     }
     if constexpr (kNorm) {
       float wa[4], wb[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        wa[e] = norm_weight(norm, 4 * qd.x + e), wb[e] = norm_weight(norm, 4 * qd.y + e);
+      norm_weights(norm, 4 * qd.x, wa);
+      norm_weights(norm, 4 * qd.y, wb);
       norm_quads<Bf16, kInter>(a, b, wa, wb, kDim / 8, kDim, norm.eps, turned, t);
     } else if (turned) {
       turn_quads<Bf16, kInter>(a, b, t);

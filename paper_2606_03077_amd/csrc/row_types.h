@@ -140,6 +140,20 @@ __device__ __forceinline__ float norm_weight(const HeadNorm& n, int d) {
   return n.weight_dtype == LIBRA_DTYPE_BF16 ? Bf16::get(e) : Fp16::get(e);
 }
 
+// Weights of channels d .. d + 3; in one load where that is aligned (norm.quads).
+__device__ __forceinline__ void norm_weights(const HeadNorm& n, int d, float (&w)[4]) {
+  if (!n.quads) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = norm_weight(n, d + e);
+  } else if (n.weight_dtype == LIBRA_DTYPE_FP32) {
+    Fp32::unpack(*reinterpret_cast<const float4*>(static_cast<const float*>(n.weight) + d), w);
+  } else {
+    const uint2 q = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(n.weight) + d);
+    if (n.weight_dtype == LIBRA_DTYPE_BF16) Bf16::unpack(q, w);
+    else Fp16::unpack(q, w);
+  }
+}
+
 __device__ __forceinline__ float norm_scale(float squares, int dim, float eps) {
   const float v = squares / float(dim) + eps;
   const float r = __builtin_amdgcn_rsqf(v);
