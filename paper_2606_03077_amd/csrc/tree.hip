@@ -368,7 +368,8 @@ template <int kWaves>
 struct Ring {
   static constexpr int kStages = kWaves == 8 ? 8 : kWaves == 4 ? 4 : 3;
   static constexpr int kCopies = 16 / kWaves;  // of 1 KiB, per wave and step
-  static constexpr bool kAhead = kWaves == 8;  // scores are taken a step ahead
+  static constexpr bool kAhead = kWaves >= 4;      // scores are taken a step ahead
+  static constexpr int kUnit = kWaves == 8 ? 2 : 1;  // steps between barriers
 };
 
 template <int kWaves>
@@ -378,6 +379,7 @@ void tree_ring_kernel(TreeArgs A) {
   constexpr int kStages = Ring<kWaves>::kStages;
   constexpr int kCopies = Ring<kWaves>::kCopies;
   constexpr bool kAhead = Ring<kWaves>::kAhead;
+  constexpr int kUnit = Ring<kWaves>::kUnit;
   __shared__ __align__(16) uint4 ring[kStages][4][256];  // K of the step's two pages, V of them
   __shared__ uint32_t bits[kRows][kMaskWords + 1];
   __shared__ int32_t ids[kWaves][2][3][64];  // of two turns of 64 steps: a step's page ids and KV head
@@ -435,38 +437,40 @@ void tree_ring_kernel(TreeArgs A) {
     to[2][lane] = head;
     filled += 64;
   };
-  // A wave copies 1 KiB pieces of the step's tiles K 0, K 1, V 0, V 1.
+  // A wave copies 1 KiB pieces of the step's tiles K 0, K 1, V 0, V 1.  Lane l holds the offsets of step
+  // l of the current turn: of both pages, or of the one that the wave's pieces lie in.
+  constexpr int kPages = kCopies > 4 ? 2 : 1;
   const uint32_t page_bytes = uint32_t(A.hkv) * kTileBytes, lane_bytes = uint32_t(lane) * 16;
   const int piece0 = wave * kCopies;
+  uint64_t off[kPages];
   int copied = 0;
-  int id0, id1, kv_head;  // of the step that is copied next
-  auto read_ids = [&]() {
-    const int32_t(&from)[3][64] = ids[wave][copied >> 6 & 1];
-    const int i = copied & 63;
-    if constexpr (kCopies > 4) id0 = from[0][i], id1 = from[1][i];
-    else id0 = id1 = from[piece0 / 4 & 1][i];
-    kv_head = from[2][i];
-  };
   auto copy_step = [&]() {
-    const uint32_t in_page = uint32_t(uniform(kv_head)) * kTileBytes;
-    const uint64_t off[2] = {uint64_t(min(uint32_t(uniform(id0)), A.last_page)) * page_bytes + in_page,
-                             uint64_t(min(uint32_t(uniform(id1)), A.last_page)) * page_bytes + in_page};
+    if ((copied & 63) == 0) {
+      // A turn's ids landed long ago; the next turn's then take the place of the last's.
+      const int32_t(&from)[3][64] = ids[wave][copied >> 6 & 1];
+#pragma unroll
+      for (int j = 0; j < kPages; ++j)
+        off[j] = uint64_t(min(uint32_t(from[kPages > 1 ? j : piece0 / 4 & 1][lane]), A.last_page)) * page_bytes +
+                 uint32_t(from[2][lane]) * kTileBytes;
+      if (copied > 0 && filled < n_steps) fill_ids();
+    }
+    uint64_t at_page[kPages];
+#pragma unroll
+    for (int j = 0; j < kPages; ++j)
+      at_page[j] = uint64_t(uint32_t(__builtin_amdgcn_readlane(int(off[j]), copied & 63))) |
+                   uint64_t(uint32_t(__builtin_amdgcn_readlane(int(off[j] >> 32), copied & 63))) << 32;
     const uint32_t stage = uint32_t(reinterpret_cast<uintptr_t>(&ring[copied % kStages][0][0]));
 #pragma unroll
     for (int c = 0; c < kCopies; ++c) {
       const int piece = piece0 + c, tile = piece / 4;
       const uint64_t src = reinterpret_cast<uint64_t>(tile < 2 ? A.k_cache : A.v_cache) +
-                           off[kCopies > 4 ? tile & 1 : 0] + piece % 4 * 1024;
+                           at_page[kPages > 1 ? tile & 1 : 0] + piece % 4 * 1024;
       asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2 nt"
                    :
                    : "s"(stage + piece * 1024), "v"(lane_bytes), "s"(src)
                    : "memory", "m0");
     }
-    if (++copied < n_steps) {
-      // At a turn's begin its ids landed long ago; the next turn's take the place of the last's.
-      if ((copied & 63) == 0 && filled < n_steps) fill_ids();
-      read_ids();
-    }
+    ++copied;
   };
   // Waits until all but the last `steps` steps' copies have landed, for every wave.
   auto wait_steps = [&](int steps) {
@@ -482,22 +486,22 @@ void tree_ring_kernel(TreeArgs A) {
     }
     __syncthreads();
   };
-  // Before step n: its copies have landed (and the next two steps' where scores are taken ahead, for
-  // two steps at once), all waves are done with the steps before, and their stages are filled again.
+  // Before step n (every kUnit steps): the copies of the steps until the next time have landed, and
+  // where scores are taken ahead those of one more; all waves are done with the steps before, and
+  // their stages are filled again.
   int n = 0;
   auto open_step = [&]() {
-    if (kAhead && n % 2) return;
-    wait_steps(max(copied - n - (kAhead ? 3 : 1), 0));
-#pragma unroll 1
-    while (copied < min(n + kStages, n_steps)) copy_step();
+    if (n % kUnit) return;
+    wait_steps(max(copied - n - kUnit - (kAhead ? 1 : 0), 0));
+    const int until = min(n + kStages, n_steps);
+    while (copied < until) copy_step();
   };
   fill_ids();
   wait_loads<0>();
   wave_sync();
   if (filled < n_steps) fill_ids();
-  read_ids();
 #pragma unroll 1
-  while (copied < min(kStages - (kAhead ? 2 : 1), n_steps)) copy_step();
+  while (copied < min(kStages - kUnit, n_steps)) copy_step();
 
   bf16x8 qop[8];
   Rows R;
@@ -545,7 +549,10 @@ void tree_ring_kernel(TreeArgs A) {
       if constexpr (kAhead) {
         load_keys(k, n + 1);
         soften(R, sc, A.sl2, pr);
-        // The next step's scores, a chain of products, among this step's values' independent ones.
+        // The next step's scores, a chain of products, among this step's values' independent ones.  A
+        // wave at its products goes before the other one of its SIMD, which may take its
+        // probabilities meanwhile.
+        __builtin_amdgcn_s_setprio(1);
 #pragma unroll
         for (int r = 0; r < 16; ++r) sc[r] = 0.f;
 #pragma unroll
@@ -553,6 +560,7 @@ void tree_ring_kernel(TreeArgs A) {
           sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k[c]), qop[c], sc, 0, 0, 0);
           R.acc[c & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(load_value(n, c)), pr[c >> 2], R.acc[c & 3], 0, 0, 0);
         }
+        __builtin_amdgcn_s_setprio(0);
       } else {
         load_keys(k, n);
         sc = score(k);
