@@ -3,9 +3,9 @@
 //
 // Lengths are read on the GPU, so the launch divides the work itself.  A KV head's N G (node, head)
 // rows are cut into tiles of M = 32 kWaves rows, an item is a tile over all P + N keys, and a step
-// is 32 keys of an item.  With S steps in all, workgroup w takes steps [w q, (w + 1) q) of the
-// items in order, q = max(ceil(S / workgroups), kMinSteps): some whole items, and at most a part
-// of one before and of one behind them.  Parts are float32 results, normalised, with their
+// is 32 keys of an item.  With U units in all, one a step and kItemCost before each item's first,
+// workgroup w takes those of the units [w q, (w + 1) q) in the items' order that are steps, q =
+// ceil(U / workgroups): some whole items, and at most a part of one before and of one behind them.  Parts are float32 results, normalised, with their
 // log-sum-exps in slots 2 w (an item begun by another workgroup) and 2 w + 1 (one that it begins and
 // does not end); the merge finds an item's slots by the same arithmetic.  Neighbouring ranges run on
 // one XCD, so that tiles of the same keys share its L2.
@@ -45,7 +45,7 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kStepKeys = 32;
-constexpr int kMinSteps = 4;
+constexpr int kItemCost = 6;  // what an item costs besides its steps, in steps
 constexpr int kTau = 8;
 constexpr float kSumTau = float(1 << kTau);
 constexpr int kMaskWords = LIBRA_MAX_MASK_WORDS;
@@ -123,10 +123,11 @@ struct Window {
     const int b = min(from + lane, A.batch - 1);
     prior = A.prior[b], start = A.starts[b], end = A.starts[b + 1];
   }
-  // The steps of this lane's sequence's items, one a tile and KV head.
-  __device__ __forceinline__ int64_t cost(const TreeArgs& A, int lane) const {
+  // This lane's sequence's items, one a tile and KV head, and their steps.
+  __device__ __forceinline__ void count(const TreeArgs& A, int lane, int64_t& items, int64_t& steps) const {
     const Seq s = make_seq<kRows>(A, prior, start, end);
-    return first + lane < A.batch ? int64_t(s.tiles) * A.hkv * s.steps : 0;
+    items = first + lane < A.batch && s.steps > 0 ? int64_t(s.tiles) * A.hkv : 0;
+    steps = items * s.steps;
   }
   __device__ __forceinline__ Seq get(const TreeArgs& A, int b, int lane) {
     if (b >= first + 64) load(A, b, lane);
@@ -148,40 +149,61 @@ struct Cursor {
   Window<kRows> window;
   Seq seq;
   int b, g, tile, step;
-  // To the workgroup's first step; returns how many it has (0: none).
-  __device__ __forceinline__ int start(const TreeArgs& A, int w, int groups, int lane) {
-    int64_t total = 0;
+  // To the workgroup's first step; returns how many it has (0: none).  each: the ranges' size.
+  __device__ __forceinline__ int start(const TreeArgs& A, int w, int groups, int lane, int64_t& each) {
+    int64_t items, steps, total = 0, total_steps = 0;
     for (int b0 = 0; b0 < A.batch; b0 += 64) {
       window.load(A, b0, lane);
-      total += wave_sum(window.cost(A, lane));
+      window.count(A, lane, items, steps);
+      total += wave_sum(steps + kItemCost * items);
     }
-    const int64_t each = max((total + groups - 1) / groups, int64_t(kMinSteps));
-    const int64_t begin = w * each;
+    each = (total + groups - 1) / groups;
+    const int64_t begin = w * each, end = min(begin + each, total);
     if (begin >= total) return 0;
-    int64_t before = 0;
-    for (int b0 = 0;; b0 += 64) {
+    // Steps before a place in the ranges' units: of an item, kItemCost units and then its steps.
+    int64_t before = 0, steps_before = 0, first_step = -1;
+    for (int b0 = 0; b0 < A.batch; b0 += 64) {
       if (window.first != b0) window.load(A, b0, lane);
-      const int64_t cost = window.cost(A, lane);
-      int64_t upto = cost;
+      window.count(A, lane, items, steps);
+      int64_t upto = steps + kItemCost * items, upto_steps = steps;
+      const int64_t cost = upto;
 #pragma unroll
       for (int n = 1; n < 64; n <<= 1) {
-        const int64_t y = __shfl_up(upto, n);
-        if (lane >= n) upto += y;
+        const int64_t y = __shfl_up(upto, n), z = __shfl_up(upto_steps, n);
+        if (lane >= n) upto += y, upto_steps += z;
       }
-      const uint64_t beyond = __ballot(before + upto > begin);
-      if (beyond) {
-        const int l = __builtin_ctzll(beyond);
-        b = uniform(b0 + l);
-        seq = window.get(A, b, lane);
-        const int64_t in_seq = begin - before - uniform64(__shfl(upto - cost, l));
-        const int item = uniform(int(in_seq / seq.steps));
-        step = uniform(int(in_seq - int64_t(item) * seq.steps));
+      // Where `unit` lies in this turn's sequences: the sequence, the item in it, the step in that.
+      auto locate = [&](int64_t unit, int& at_b, int& at_item, int& at_step) -> int64_t {
+        const int l = __builtin_ctzll(__ballot(before + upto > unit));
+        at_b = uniform(b0 + l);
+        seq = window.get(A, at_b, lane);
+        const int64_t in_seq = unit - before - uniform64(__shfl(upto - cost, l));
+        const int item_units = seq.steps + kItemCost;
+        at_item = uniform(int(in_seq / item_units));
+        at_step = max(uniform(int(in_seq - int64_t(at_item) * item_units)) - kItemCost, 0);
+        return steps_before + uniform64(__shfl(upto_steps - steps, l)) + int64_t(at_item) * seq.steps + at_step;
+      };
+      const int64_t here = before + uniform64(__shfl(upto, 63));
+      if (end < here && end >= before) {  // begin lies in this turn too, or in one before
+        int b1, item1, step1;
+        total_steps = locate(end, b1, item1, step1);
+      } else if (end == here) {
+        total_steps = steps_before + uniform64(__shfl(upto_steps, 63));
+      }
+      if (first_step < 0 && begin < here) {
+        int item;
+        first_step = locate(begin, b, item, step);
         g = uniform(item / seq.tiles);
         tile = item - g * seq.tiles;
-        return int(min(each, total - begin));
       }
-      before += uniform64(__shfl(upto, 63));
+      if (end <= here) break;
+      before = here;
+      steps_before += uniform64(__shfl(upto_steps, 63));
     }
+    // The window may have gone on to the range's end.
+    if (b < window.first) window.load(A, b / 64 * 64, lane);
+    seq = window.get(A, b, lane);
+    return int(total_steps - first_step);
   }
   // To the next sequence that has nodes.
   __device__ __forceinline__ void next_seq(const TreeArgs& A, int lane) {
@@ -355,7 +377,7 @@ __device__ __forceinline__ void load_query(const TreeArgs& A, const Seq& s, int 
 __device__ __forceinline__ void copy_lds_dword(const int32_t* src, int32_t* dst) {
   asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off"
                :
-               : "s"(uint32_t(reinterpret_cast<uintptr_t>(dst))), "v"(src)
+               : "s"(uniform(int(reinterpret_cast<uintptr_t>(dst)))), "v"(src)
                : "memory", "m0");
 }
 __device__ __forceinline__ void wave_sync() {  // LDS operations of one wave complete in order
@@ -392,7 +414,8 @@ void tree_ring_kernel(TreeArgs A) {
   const int per_xcd = int(gridDim.x) / kNumXcds;
   const int w = int(blockIdx.x) % kNumXcds * per_xcd + int(blockIdx.x) / kNumXcds;
   Cursor<kRows> at;
-  const int n_steps = at.start(A, w, int(gridDim.x), lane);
+  int64_t each;
+  const int n_steps = uniform(at.start(A, w, int(gridDim.x), lane, each));
   if (tid == 0) A.splits[w].parts = 0;  // unless an item is begun and not ended, below
   if (n_steps == 0) return;
 
@@ -459,7 +482,7 @@ void tree_ring_kernel(TreeArgs A) {
     for (int j = 0; j < kPages; ++j)
       at_page[j] = uint64_t(uint32_t(__builtin_amdgcn_readlane(int(off[j]), copied & 63))) |
                    uint64_t(uint32_t(__builtin_amdgcn_readlane(int(off[j] >> 32), copied & 63))) << 32;
-    const uint32_t stage = uint32_t(reinterpret_cast<uintptr_t>(&ring[copied % kStages][0][0]));
+    const int stage = uniform(int(reinterpret_cast<uintptr_t>(&ring[copied % kStages][0][0])));
 #pragma unroll
     for (int c = 0; c < kCopies; ++c) {
       const int piece = piece0 + c, tile = piece / 4;
@@ -644,8 +667,8 @@ void tree_ring_kernel(TreeArgs A) {
       if (hh == 0) A.part_lse[block * 32 + col] = ls == 0.f ? -INFINITY : R.m + log2f(ls);
     }
     if (step1 < s.steps && step0 == 0 && tid == 0) {
-      // The item's other parts are those of the workgroups after this one, n_steps each.
-      A.splits[w] = {(s.steps - step1 + n_steps - 1) / n_steps + 1, s.row0, s.nodes, g, tile};
+      // The item's other parts are those of the workgroups after this one.
+      A.splits[w] = {int((s.steps - step1 + each - 1) / each) + 1, s.row0, s.nodes, g, tile};
     }
     if (n == n_steps) return;
   }
