@@ -554,6 +554,8 @@ void tree_ring_kernel(TreeArgs A) {
   while (true) {  // the range's parts of items
     const Seq s = at.seq;
     const int g = at.g, tile = at.tile, step0 = at.step, step1 = min(s.steps, step0 + n_steps - n);
+    // A wave without rows in the tile only copies and keeps step.
+    const bool idle = tile * kRows + 32 * wave >= s.nodes * G;
     R.clear();
     wave_sync();
     f32x16 sc;
@@ -567,6 +569,7 @@ void tree_ring_kernel(TreeArgs A) {
     // Steps over cached tokens alone, which every row sees.
     for (const int plain = min(step1 - (kAhead ? 1 : 0), s.prior / kStepKeys); step < plain; ++step, ++n) {
       if (!kAhead || step > step0) open_step();
+      if (idle) continue;
       bf16x8 pr[2];
       uint4 k[8];
       if constexpr (kAhead) {
@@ -596,6 +599,7 @@ void tree_ring_kernel(TreeArgs A) {
     }
     for (; step < step1; ++step, ++n) {
       if (!kAhead || step > step0) open_step();
+      if (idle) continue;
       uint4 k[8], v[8];
       if constexpr (!kAhead) {
         load_keys(k, n);
@@ -784,10 +788,12 @@ __global__ __launch_bounds__(kMergeThreads) void tree_merge_kernel(TreeArgs A, i
   }
 }
 
-// Waves of a workgroup, 32 rows each: enough for the rows of an average sequence's KV head.
+// Waves of a workgroup, 32 rows each: enough for the rows of an average sequence's KV head.  64 rows
+// take four waves, of which two only copy, as 64 sequences of 4,000 tokens and 8 KV heads ran in 115
+// us so, in 136 with two waves to a workgroup and in 185 as two tiles of one.
 int waves_of(int64_t rows, int32_t batch, int32_t group) {
   const int64_t mean = (rows + std::max(batch, 1) - 1) / std::max(batch, 1) * group;
-  return mean <= 32 ? 1 : mean <= 64 ? 2 : mean <= 128 ? 4 : 8;
+  return mean <= 32 ? 1 : mean <= 128 ? 4 : 8;
 }
 
 TreeArgs tree_args(const KvLayout& L, const TreeCall& c, int waves) {
@@ -824,7 +830,6 @@ hipError_t launch_tree(const KvLayout& L, const TreeCall& c, hipStream_t s) {
   const dim3 grid{unsigned(groups_of(waves))}, block{unsigned(64 * waves)};
   switch (waves) {
     case 1: hipLaunchKernelGGL(tree_ring_kernel<1>, grid, block, 0, s, A); break;
-    case 2: hipLaunchKernelGGL(tree_ring_kernel<2>, grid, block, 0, s, A); break;
     case 4: hipLaunchKernelGGL(tree_ring_kernel<4>, grid, block, 0, s, A); break;
     default: hipLaunchKernelGGL(tree_ring_kernel<8>, grid, block, 0, s, A); break;
   }

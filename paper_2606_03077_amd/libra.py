@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import struct
 from typing import Optional, Sequence
 
 import numpy as np
@@ -143,7 +144,6 @@ def load() -> ctypes.CDLL:
     I32P = ctypes.POINTER(ctypes.c_int32)
     I64P = ctypes.POINTER(ctypes.c_int64)
     DP = ctypes.POINTER(ctypes.c_double)
-    NH = ctypes.POINTER(NormHeads)
     sig = {
         "libra_status_string": (ctypes.c_char_p, [ctypes.c_int]),
         "libra_last_error": (ctypes.c_char_p, []),
@@ -185,11 +185,10 @@ def load() -> ctypes.CDLL:
         "libra_kv_map": (ctypes.c_int, [I32, P, P, P, P, I32, P, I64, P, P, I64, P, P, P, P, P, P,
                                         P]),
         "libra_kv_accept": (ctypes.c_int, [P, I32, P, P, I32, P, P, I32, P]),
-        "libra_qk_norm_rotary": (ctypes.c_int, [P, I32, I32, ctypes.c_float, P, I64, I32, NH, NH,
-                                                P]),
+        "libra_qk_norm_rotary": (ctypes.c_int, [P, I32, I32, ctypes.c_float, P, I64, I32, P, P, P]),
         "libra_qk_norm_rotary_workspace_bytes": (SZ, [I64, I32, I32, I32]),
         "libra_qk_norm_rotary_backward": (ctypes.c_int, [P, I32, I32, ctypes.c_float, P, I64, I32,
-                                                         NH, NH, P, SZ, P]),
+                                                         P, P, P, SZ, P]),
         "libra_kv_append_norm": (ctypes.c_int, [P, P, I32, ctypes.c_float, P, P, I64, P, I64, I32,
                                                 P, P, I64, P, P, I64, I32, P, P]),
         "libra_tree_attn_workspace_bytes": (SZ, [I64, I32, I32, I32]),
@@ -648,6 +647,9 @@ def libra_kv_accept(layout: int, prior_lens, accepted, counts, block_table, bt_s
            "libra_kv_accept")
 
 
+_NORM_HEADS = struct.Struct("@PqqiPPqqPqqP").pack  # NormHeads' fields
+
+
 def _heads(t, shape, dtype, what: str, device: int):
     """(pointer, row stride, head stride) of [rows, heads, head_dim], any strides of the first two."""
     if t.get_device() != device or t.dtype is not dtype or t.shape != shape:
@@ -659,15 +661,17 @@ def _heads(t, shape, dtype, what: str, device: int):
 
 
 def _norm_heads(x, weight, out, grad, weight_grad, dtype, weight_dtype, what: str, device: int):
+    """A libra_norm_heads as bytes (a third of a ctypes structure's time)."""
     if x is None:
         return None
-    xs = _heads(x, x.shape, dtype, what, device)
-    os = _heads(out, x.shape, dtype, f"{what}'s output", device)
-    gs = (None, 0, 0) if grad is None else _heads(grad, x.shape, dtype, f"{what}'s gradient", device)
-    dim = x.shape[2]
-    return NormHeads(*xs, x.shape[1], _vector(weight, weight_dtype, dim, f"{what}'s weight", device),
-                     *os, *gs, _vector(weight_grad, torch.float32, dim, f"{what}'s weight gradient",
-                                       device))
+    shape = x.shape
+    dim = shape[2]
+    xp, xr, xh = _heads(x, shape, dtype, what, device)
+    op, orow, oh = _heads(out, shape, dtype, what, device)
+    gp, gr, gh = (0, 0, 0) if grad is None else _heads(grad, shape, dtype, what, device)
+    return _NORM_HEADS(xp, xr, xh, shape[1], _vector(weight, weight_dtype, dim, what, device) or 0, op,
+                       orow, oh, gp, gr, gh,
+                       _vector(weight_grad, torch.float32, dim, what, device) or 0)
 
 
 def _norm_call(q, k, q_weight, k_weight, device: int):

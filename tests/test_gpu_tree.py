@@ -166,7 +166,7 @@ def test_long_contexts_are_split(prior, nodes, hq, hkv):
     run([prior, 40], [nodes, nodes], hq, hkv)
 
 
-@pytest.mark.parametrize("form", [1, 2, 4, 8])
+@pytest.mark.parametrize("form", [1, 2, 4, 8])  # 32, 64, 128, 256 rows
 def test_one_long_among_many(form):
     """Each form of the kernel; workgroups that end one request's item and begin the next's."""
     rng = np.random.default_rng(form)
@@ -409,3 +409,50 @@ def test_a_drafted_step():
     assert int(held.sum()) + int(num_free) == pool
     libra.libra_rotary_destroy(rot)
     cache.close()
+
+
+@pytest.mark.parametrize("nodes", [1, 6, 20, 50])
+def test_large_batches_against_append_attention(nodes):
+    """Chains over so many tokens that a workgroup's range goes on for several turns of page ids, in every
+    form, against libra_append_attn (which writes the tokens that are there): both within 2^-8 of sum p |v|
+    (at most the largest |v|) and of themselves, twice."""
+    rng = np.random.default_rng(nodes)
+    B, hq, hkv = 70, 8, 4
+    lens = rng.integers(1000, 30000, size=B)
+    pages = -(-lens // 16)
+    pool = int(pages.sum())
+    g = torch.Generator(device="cuda").manual_seed(nodes)
+    k, v = (torch.randn((pool * hkv * 2048,), device="cuda", generator=g, dtype=torch.bfloat16) for _ in "kv")
+    layout = libra.libra_kv_layout_create(k, v, pool, hkv)
+    perm, at = rng.permutation(pool), 0
+    table = np.zeros((B, int(pages.max())), np.int32)
+    for b, n in enumerate(pages):
+        table[b, :n] = perm[at:at + n]
+        at += n
+    starts = torch.arange(B + 1, dtype=I32, device="cuda") * nodes
+    rows = B * nodes
+    q = torch.randn((rows, hq, 128), device="cuda", generator=g).bfloat16()
+    bt = torch.from_numpy(table).cuda()
+    ws = torch.empty(libra.libra_tree_attn_workspace_bytes(rows, B, hq, hkv), dtype=torch.uint8, device="cuda")
+    out, lse = torch.empty_like(q), torch.empty((rows, hq), device="cuda")
+    prior = torch.tensor((lens - nodes).tolist(), dtype=I32, device="cuda")
+    libra.libra_tree_attn(layout, q, prior, starts, None, bt, table.shape[1], hq, SCALE, ws, out, lse)
+    # The new tokens as they are, gathered.
+    cu = torch.tensor(np.concatenate([[0], np.cumsum(lens)]), dtype=I32, device="cuda")
+    ks, vs = (torch.empty((int(lens.sum()), hkv, 128), dtype=torch.bfloat16, device="cuda") for _ in "kv")
+    libra.libra_kv_gather(layout, bt, table.shape[1], cu, B, table.shape[1], ks, vs)
+    new = torch.cat([torch.arange(int(e) - nodes, int(e)) for e in np.cumsum(lens)]).cuda()
+    plan = libra.libra_splitkv_plan(libra.LIBRA_MODE_APPEND, B, hq, hkv, lens.tolist(), [nodes] * B)
+    want, want_lse = torch.empty_like(q), torch.empty_like(lse)
+    libra.libra_append_attn(layout, plan, q, ks[new].contiguous(), vs[new].contiguous(), bt, table.shape[1], B, hq,
+                            SCALE, libra.alloc_workspace(plan), want, want_lse)
+    torch.cuda.synchronize()
+    libra.libra_plan_destroy(plan)
+    tol = 2 * 2.0 ** -8 * (1 + want.float().abs())  # sum p |v| over a thousand keys or more is about 0.8
+    assert ((out.float() - want.float()).abs() <= tol).all()
+    assert ((lse - want_lse).abs() <= 1e-3).all()
+    again = torch.empty_like(out)
+    libra.libra_tree_attn(layout, q, prior, starts, None, bt, table.shape[1], hq, SCALE, ws, again, None)
+    torch.cuda.synchronize()
+    libra.libra_kv_layout_destroy(layout)
+    assert torch.equal(again.view(torch.int16), out.view(torch.int16))
