@@ -677,8 +677,8 @@ libra_status libra_kv_append_norm(libra_kv_layout layout, libra_rotary rotary, i
  * sees nothing gives out = 0, lse = -inf.  Keys and values that a row does not see may be
  * anything, infinities and NaN too, and so may slots past the last node.
  *
- * q, out: device bf16 [rows][num_q_heads][128], lse: device float32 [rows][num_q_heads] or NULL.  Rows
- * outside every request's are neither read nor written.  Lengths are read on the device, by the
+ * q, out: device bf16 [rows][num_q_heads][128], apart; lse: device float32 [rows][num_q_heads] or
+ * NULL.  Rows outside every request's are neither read nor written.  Lengths are read on the device, by the
  * kernels: tokens past bt_stride * 16 are not seen, and block-table ids of the tokens in [0,
  * prior + nodes) that lie outside the cache read another page of it, so that a request that
  * libra_kv_map refused gives meaningless rows but no fault.

@@ -31,14 +31,14 @@ libra_status check_weight(const void* w, int32_t dtype, const char* what) {
 
 // One of a call's tensors, rows x num_heads vectors; written: whether its vectors must be apart.
 libra_status check_heads(const void* p, int64_t rows, int32_t heads, int32_t dim, int64_t row, int64_t head,
-                         size_t size, bool written, const std::string& what) {
-  if (!p) return set_error(LIBRA_E_INVAL, what + " is NULL");
-  if (!aligned_to(p, size)) return set_error(LIBRA_E_INVAL, what + " must be aligned to its type");
-  if (row < 0 || head < 0 || !addressable(rows, heads, row, head))
-    return set_error(LIBRA_E_INVAL, what + ": strides must be >= 0, and offsets below 2^56 elements");
-  if (written && !disjoint(rows, heads, dim, row, head))
-    return set_error(LIBRA_E_INVAL, what + "'s heads overlap each other");
-  return LIBRA_OK;
+                         size_t size, bool written, const char* tensor, const char* part) {
+  const char* wrong = nullptr;
+  if (!p) wrong = " is NULL";
+  else if (!aligned_to(p, size)) wrong = " must be aligned to its type";
+  else if (row < 0 || head < 0 || !addressable(rows, heads, row, head))
+    wrong = ": strides must be >= 0, and offsets below 2^56 elements";
+  else if (written && !disjoint(rows, heads, dim, row, head)) wrong = "'s heads overlap each other";
+  return wrong ? set_error(LIBRA_E_INVAL, std::string(tensor) + part + wrong) : LIBRA_OK;
 }
 
 // Whether the written tensor, where it is an input, has its strides.
@@ -64,21 +64,21 @@ libra_status check_norm(libra_rotary rotary, int32_t dtype, int32_t weight_dtype
   const size_t size = dtype_size(dtype);
   for (const libra_norm_heads* t : {&q, &k}) {
     if (!t->num_heads) continue;
-    const std::string name = t == &q ? "q" : "k";
-    st = check_weight(t->weight, weight_dtype, (name + "'s weight").c_str());
+    const char* const name = t == &q ? "q" : "k";
+    st = check_weight(t->weight, weight_dtype, t == &q ? "q's weight" : "k's weight");
     if (st != LIBRA_OK) return st;
     if (backward && t->weight_grad && !aligned_to(t->weight_grad, 4))
-      return set_error(LIBRA_E_INVAL, name + "'s weight_grad must be aligned to float32");
+      return set_error(LIBRA_E_INVAL, std::string(name) + "'s weight_grad must be aligned to float32");
     if (rows == 0) continue;
-    st = check_heads(t->x, rows, t->num_heads, head_dim, t->x_row_stride, t->x_head_stride, size, false, name + "'s x");
+    st = check_heads(t->x, rows, t->num_heads, head_dim, t->x_row_stride, t->x_head_stride, size, false, name, "'s x");
     if (st == LIBRA_OK)
-      st = check_heads(t->out, rows, t->num_heads, head_dim, t->out_row_stride, t->out_head_stride, size, true, name + "'s out");
+      st = check_heads(t->out, rows, t->num_heads, head_dim, t->out_row_stride, t->out_head_stride, size, true, name, "'s out");
     if (st == LIBRA_OK && backward)
-      st = check_heads(t->grad, rows, t->num_heads, head_dim, t->grad_row_stride, t->grad_head_stride, size, false, name + "'s grad");
+      st = check_heads(t->grad, rows, t->num_heads, head_dim, t->grad_row_stride, t->grad_head_stride, size, false, name, "'s grad");
     if (st != LIBRA_OK) return st;
     if (!in_place(t->x, t->x_row_stride, t->x_head_stride, *t, rows) ||
         (backward && !in_place(t->grad, t->grad_row_stride, t->grad_head_stride, *t, rows)))
-      return set_error(LIBRA_E_INVAL, "in place, " + name + "'s tensors need the same strides");
+      return set_error(LIBRA_E_INVAL, std::string("in place, ") + name + "'s tensors need the same strides");
   }
   if (rows > 0 && q.num_heads + k.num_heads > 0 && !positions)
     return set_error(LIBRA_E_INVAL, "positions is NULL");

@@ -719,8 +719,8 @@ __global__ __launch_bounds__(kMergeThreads) void tree_merge_kernel(TreeArgs A, i
   const int w = kPerRow == 1 ? int(blockIdx.x) : find_split(A, groups, blockIdx.x);
   if (w < 0) return;
   const Split s = A.splits[w];
-  const int n = s.parts;
-  if (n == 0) return;
+  const int n = min(s.parts, groups - w);  // of lengths that changed meanwhile, too, within the workspace
+  if (n <= 0) return;
   // Neighbouring lanes take neighbouring rows, whose parts lie together; t: eight channels.
   constexpr int kBlockRows = kMergeGroups / kPerRow;
   const int tid = threadIdx.x, t = tid / kBlockRows % 16, k = tid / (16 * kBlockRows);
