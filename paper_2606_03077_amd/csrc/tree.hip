@@ -390,8 +390,9 @@ template <int kWaves>
 struct Ring {
   static constexpr int kStages = kWaves == 8 ? 8 : kWaves == 4 ? 4 : 3;
   static constexpr int kCopies = 16 / kWaves;  // of 1 KiB, per wave and step
-  static constexpr bool kAhead = kWaves >= 4;      // scores are taken a step ahead
+  static constexpr int kDepth = kWaves > 1 ? 1 : 0;           // steps that scores are taken ahead
   static constexpr int kUnit = kWaves == 8 ? 2 : 1;  // steps between barriers
+  static_assert(kStages >= 2 * kUnit + kDepth, "what a unit reads is copied before it begins");
 };
 
 template <int kWaves>
@@ -400,7 +401,7 @@ void tree_ring_kernel(TreeArgs A) {
   constexpr int kRows = 32 * kWaves;
   constexpr int kStages = Ring<kWaves>::kStages;
   constexpr int kCopies = Ring<kWaves>::kCopies;
-  constexpr bool kAhead = Ring<kWaves>::kAhead;
+  constexpr int kDepth = Ring<kWaves>::kDepth;
   constexpr int kUnit = Ring<kWaves>::kUnit;
   __shared__ __align__(16) uint4 ring[kStages][4][256];  // K of the step's two pages, V of them
   __shared__ uint32_t bits[kRows][kMaskWords + 1];
@@ -510,12 +511,12 @@ void tree_ring_kernel(TreeArgs A) {
     __syncthreads();
   };
   // Before step n (every kUnit steps): the copies of the steps until the next time have landed, and
-  // where scores are taken ahead those of one more; all waves are done with the steps before, and
+  // of as many more as scores are taken ahead; all waves are done with the steps before, and
   // their stages are filled again.
   int n = 0;
   auto open_step = [&]() {
     if (n % kUnit) return;
-    wait_steps(max(copied - n - kUnit - (kAhead ? 1 : 0), 0));
+    wait_steps(max(copied - n - kUnit - kDepth, 0));
     const int until = min(n + kStages, n_steps);
     while (copied < until) copy_step();
   };
@@ -558,53 +559,62 @@ void tree_ring_kernel(TreeArgs A) {
     const bool idle = tile * kRows + 32 * wave >= s.nodes * G;
     R.clear();
     wave_sync();
-    f32x16 sc;
     int step = step0;
-    if constexpr (kAhead) {
-      open_step();
-      uint4 k[8];
-      load_keys(k, n);
-      sc = score(k);
-    }
     // Steps over cached tokens alone, which every row sees.
-    for (const int plain = min(step1 - (kAhead ? 1 : 0), s.prior / kStepKeys); step < plain; ++step, ++n) {
-      if (!kAhead || step > step0) open_step();
-      if (idle) continue;
-      bf16x8 pr[2];
-      uint4 k[8];
-      if constexpr (kAhead) {
-        load_keys(k, n + 1);
-        soften(R, sc, A.sl2, pr);
-        // The next step's scores, a chain of products, among this step's values' independent ones.  A
-        // wave at its products goes before the other one of its SIMD, which may take its
-        // probabilities meanwhile.
-        __builtin_amdgcn_s_setprio(1);
+    const int plain = min(s.prior / kStepKeys, step1 - kDepth);
+    if constexpr (kDepth > 0) {
+      if (!idle && step < plain) {
+        f32x16 sc[kDepth];
+        uint4 k[8];
+        const int first = n;
+        open_step();
 #pragma unroll
-        for (int r = 0; r < 16; ++r) sc[r] = 0.f;
-#pragma unroll
-        for (int c = 0; c < 8; ++c) {
-          sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k[c]), qop[c], sc, 0, 0, 0);
-          R.acc[c & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(load_value(n, c)), pr[c >> 2], R.acc[c & 3], 0, 0, 0);
+        for (int d = 0; d < kDepth; ++d) {
+          load_keys(k, n + d);
+          sc[d] = score(k);
         }
-        __builtin_amdgcn_s_setprio(0);
-      } else {
+        while (step < plain) {
+#pragma unroll
+          for (int d = 0; d < kDepth; ++d, ++step, ++n) {
+            if (d > 0 && step >= plain) break;
+            if (n > first) open_step();
+            bf16x8 pr[2];
+            load_keys(k, n + kDepth);
+            soften(R, sc[d], A.sl2, pr);
+            // A later step's scores, a chain of products, among this step's values' independent ones.  A
+            // wave at its products goes before the other one of its SIMD, which may take its
+            // probabilities meanwhile.
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int r = 0; r < 16; ++r) sc[d][r] = 0.f;
+#pragma unroll
+            for (int c = 0; c < 8; ++c) {
+              sc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(k[c]), qop[c], sc[d], 0, 0, 0);
+              R.acc[c & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(load_value(n, c)), pr[c >> 2], R.acc[c & 3], 0, 0, 0);
+            }
+            __builtin_amdgcn_s_setprio(0);
+          }
+        }
+      }
+    } else {
+      for (; step < plain; ++step, ++n) {
+        open_step();
+        uint4 k[8], v[8];
         load_keys(k, n);
-        sc = score(k);
-        uint4 v[8];
+        const f32x16 sc = score(k);
 #pragma unroll
         for (int c = 0; c < 8; ++c) v[c] = load_value(n, c);
+        bf16x8 pr[2];
         soften(R, sc, A.sl2, pr);
         add_values(R, v, pr);
       }
     }
     for (; step < step1; ++step, ++n) {
-      if (!kAhead || step > step0) open_step();
+      open_step();
       if (idle) continue;
       uint4 k[8], v[8];
-      if constexpr (!kAhead) {
-        load_keys(k, n);
-        sc = score(k);
-      }
+      load_keys(k, n);
+      f32x16 sc = score(k);
       const int key0 = step * kStepKeys;
       uint32_t sees = ~0u;
       if (key0 + kStepKeys > s.prior) {
@@ -622,12 +632,6 @@ void tree_ring_kernel(TreeArgs A) {
                            reinterpret_cast<const uint16_t*>(stage[3]));
       }
       add_values(R, v, pr);
-      if constexpr (kAhead) {
-        if (step + 1 < step1) {
-          load_keys(k, n + 1);
-          sc = score(k);
-        }
-      }
     }
     // The next part's queries are on their way before this part's results.
     const int row_node = node, row_head = head;
