@@ -320,6 +320,18 @@ def test_on_another_stream():
     s.close()
 
 
+def test_two_calls_at_once():
+    """Two streams, a workspace each."""
+    steps = [Step([3000, 70, 900], [9, 3, 30], 8, 2, seed=1), Step([500] * 20, [40] * 20, 8, 2, "any", seed=2)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(5):
+        for t, s in zip(steps, streams):
+            t.call(stream=s)
+    for t in steps:
+        t.check()
+
+
 def test_one_node_is_a_decode_step():
     """Single tokens give what libra_decode_attn gives over the same cache, to both sides' rounding."""
     prior = [700, 16, 3001, 0]
