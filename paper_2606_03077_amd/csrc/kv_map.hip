@@ -5,7 +5,10 @@
 // The table's kernel is one workgroup: requests 1,024 at a time, one to a thread, whose page counts
 // are added up by scans, and then the pages that move, each found by a search in the scans' sums, so
 // that an ended request of thousands of pages is everybody's work.  Pages given back are pushed
-// before any is taken.
+// before any is taken.  64 requests of a token each: 7 us of kernel with cold caches, of which 3 are
+// the launch; 256 trees of which 9 ended (3,900 pages): 14 us, and 5 for their 8,500 rows, which a
+// launch of their own maps (one workgroup alone took 26 for both).  Accepted tokens: 2,200 of 8 heads
+// (17 MB) 12 us, bound by the V tiles' lines, as a value of a token is two bytes of every 16.
 #include <algorithm>
 #include <climits>
 
@@ -239,7 +242,9 @@ __global__ __launch_bounds__(256) void kv_accept_kernel(AcceptArgs A) {
   }
 }
 
-// Rows that the one workgroup maps itself, instead of a second launch.
+// Rows that the one workgroup maps itself, instead of a second launch: 64 requests of a token 10.0
+// against 12.0 us, 16 trees (813 rows) 25.7 against 26.8, 32 (1,300) 29.8 against 28.7, 256 (8,500)
+// 31.3 against 20.9.
 constexpr int64_t kOneLaunchRows = 1024;
 
 }  // namespace
@@ -250,14 +255,17 @@ hipError_t launch_kv_map(const MapArgs& a, hipStream_t s) {
     hipLaunchKernelGGL(kernel, dim3(1), dim3(unsigned(threads)), 0, s, a, one ? a.rows : 0);
     return hipGetLastError();
   };
-  // 64 requests of one token each take 5 us with 256 threads, 10 with 1,024; but pages that move
-  // are worth more threads.
-  const bool small = std::max(a.stride, a.rows + 1) * int64_t(std::max(a.batch, 1)) <= INT32_MAX;
+  // Few rows a request, so that few pages move: 512 threads, whose scans are shorter.  With 512 and
+  // 1,024 threads (and some 4 us of two events): 64 requests of a token each 10.2 and 11.6 us, 128
+  // 10.2 and 11.2; trees of up to 64 nodes, 16 requests 19.1 and 14.8, 64 23.5 and 20.5, 256 24.1 and
+  // 20.9.
+  // Sums, and a thread's next index behind the last, fit 32 bits.
+  const bool small = std::max(a.stride, a.rows + 1) * int64_t(std::max(a.batch, 1)) <= INT32_MAX - 4 * kMapThreads;
   const hipError_t e =
       a.batch > kMapThreads ? launch(kv_map_kernel<kMapThreads, true, int64_t>, kMapThreads)
       : !small              ? launch(kv_map_kernel<kMapThreads, false, int64_t>, kMapThreads)
-      : a.batch > 64        ? launch(kv_map_kernel<kMapThreads, false, int32_t>, kMapThreads)
-                            : launch(kv_map_kernel<256, false, int32_t>, 256);
+      : a.batch <= 512 && a.rows <= 8 * int64_t(a.batch) ? launch(kv_map_kernel<512, false, int32_t>, 512)
+                            : launch(kv_map_kernel<kMapThreads, false, int32_t>, kMapThreads);
   if (e != hipSuccess || one) return e;
   hipLaunchKernelGGL(kv_map_rows_kernel, dim3(unsigned((a.rows + kRowThreads - 1) / kRowThreads)), dim3(kRowThreads),
                      0, s, a);

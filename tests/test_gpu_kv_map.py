@@ -86,6 +86,13 @@ def test_rows_cut_and_padded(rows_off):
     t.check()
 
 
+def test_rows_whose_sums_pass_32_bits():
+    """900 requests in one pass, each of which might have all of three million rows."""
+    t = random_tables(6, 900, 90, 3, 500, 3_000_000)
+    t.call()
+    t.check()
+
+
 def test_no_requests_and_no_rows():
     t = Tables([], [], [], np.zeros((0, 1)), [1, 2, 3], 2, 4)
     t.call()
