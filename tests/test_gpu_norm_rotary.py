@@ -240,6 +240,36 @@ def test_many_rows_and_replayed_gradients():
         assert all(torch.equal(a, b) for a, b in zip(outs, eager))
 
 
+@pytest.mark.parametrize("dtype,rows", [("bf16", 10007), ("fp32", 5003)])
+@pytest.mark.parametrize("interleaved", [False, True])
+def test_gradients_past_the_caches(dtype, rows, interleaved):
+    """Beyond the size from which the gradient goes past the caches: the bits of a part of the rows."""
+    hd, t, pos = Handle(rdim=64, interleaved=interleaved), TYPES[dtype], np.arange(rows)
+    q, k = randn((rows, 12, 128), t, 1), randn((rows, 2, 128), t, 2)
+    gq, gk = randn(q.shape, t, 3), randn(k.shape, t, 4)
+    wq, wk = weights(128, t, 5), weights(128, t, 6)
+    dq, dk, _, dwk = run_backward(hd, q, k, wq, wk, pos, gq, gk)
+    check_backward(k, wk, gk, hd, pos, dk, dwk, "k")
+    at = slice(rows - 300, rows)
+    few = run_backward(hd, q[at], k[at], wq, wk, pos[at], gq[at], gk[at])
+    assert torch.equal(few[0], dq[at]) and torch.equal(few[1], dk[at])
+
+
+def test_on_another_stream():
+    hd, rows, s = Handle(), 300, torch.cuda.Stream()
+    q, g, w, pos = randn((rows, 4, 128), torch.bfloat16, 1), randn((rows, 4, 128), torch.bfloat16, 2), \
+        weights(128, torch.bfloat16, 3), np.arange(rows)
+    want = run_forward(hd, q, None, w, None, pos)[0], *run_backward(hd, q, None, w, None, pos, g, None)[::2]
+    y, dx, dw = torch.empty_like(q), torch.empty_like(q), torch.empty(128, device="cuda")
+    ws = torch.empty(libra.libra_qk_norm_rotary_workspace_bytes(rows, 4, 0, 128), dtype=torch.uint8, device="cuda")
+    p = torch.from_numpy(pos).int().cuda()
+    torch.cuda.synchronize()
+    libra.libra_qk_norm_rotary(hd.h, q, None, w, None, EPS, p, y, None, stream=s)
+    libra.libra_qk_norm_rotary_backward(hd.h, g, None, q, None, w, None, EPS, p, dx, None, dw, None, ws, stream=s)
+    s.synchronize()
+    assert torch.equal(y, want[0]) and torch.equal(dx, want[1]) and torch.equal(dw, want[2])
+
+
 # --- the cache append ------------------------------------------------------------------------
 
 @pytest.mark.parametrize("rope", ROPES, ids=str)
