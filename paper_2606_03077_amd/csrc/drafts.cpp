@@ -11,6 +11,7 @@ using namespace libra;
 namespace {
 
 constexpr libra_norm_heads kNoHeads{};
+constexpr int32_t kMaxBatch = 1 << 30;  // indices behind the last one, in turns, fit 32 bits
 
 bool known_dtype(int32_t d) {
   return d == LIBRA_DTYPE_BF16 || d == LIBRA_DTYPE_FP16 || d == LIBRA_DTYPE_FP32;
@@ -99,6 +100,7 @@ libra_status libra_kv_map(int32_t batch, const int32_t* prior_lens, const int32_
     return set_error(LIBRA_E_INVAL, "batch / bt_stride / free_capacity / rows < 0");
   if (rows > INT32_MAX || free_capacity > INT32_MAX)
     return set_error(LIBRA_E_UNSUPPORTED, "rows and free_capacity must be < 2^31");
+  if (batch > kMaxBatch) return set_error(LIBRA_E_UNSUPPORTED, "batch must be <= 2^30");
   if (!num_free || !num_free_out || !row_starts)
     return set_error(LIBRA_E_INVAL, "num_free, num_free_out or row_starts is NULL");
   if (batch > 0 && (!prior_lens || !new_lens || !held_pages || !held_out || !refused ||
@@ -135,6 +137,7 @@ libra_status libra_kv_accept(libra_kv_layout layout, int32_t batch, const int32_
   const int32_t hkv = layout->desc.num_kv_heads;
   if (int64_t(batch) * hkv > INT32_MAX)
     return set_error(LIBRA_E_UNSUPPORTED, "batch * num_kv_heads must be < 2^31");
+  if (max_accepted > kMaxBatch) return set_error(LIBRA_E_UNSUPPORTED, "max_accepted must be <= 2^30");
   if (!prior_lens || !accepted || !counts || !block_table)
     return set_error(LIBRA_E_INVAL, "prior_lens, accepted, counts or block_table is NULL");
   const AcceptArgs a{static_cast<uint16_t*>(layout->desc.k_cache), static_cast<uint16_t*>(layout->desc.v_cache),
@@ -271,6 +274,7 @@ libra_status libra_tree_attn(libra_kv_layout layout, const void* q, int64_t rows
     return set_error(LIBRA_E_UNSUPPORTED, "num_q_heads / num_kv_heads > 16");
   if (rows > INT32_MAX / num_q_heads)
     return set_error(LIBRA_E_UNSUPPORTED, "rows * num_q_heads must be < 2^31");
+  if (batch > kMaxBatch) return set_error(LIBRA_E_UNSUPPORTED, "batch must be <= 2^30");
   if (!(scale > 0.f) || !std::isfinite(scale))
     return set_error(LIBRA_E_INVAL, "scale must be positive and finite");
   if (mask ? mask_words < 1 : mask_words != 0)
@@ -280,6 +284,7 @@ libra_status libra_tree_attn(libra_kv_layout layout, const void* q, int64_t rows
   if (rows == 0 || batch == 0) return LIBRA_OK;
   if (!q || !out) return set_error(LIBRA_E_INVAL, "q / out is NULL");
   if (!aligned16(q) || !aligned16(out)) return set_error(LIBRA_E_INVAL, "q / out must be 16-byte aligned");
+  if (q == out) return set_error(LIBRA_E_INVAL, "q and out must be apart");
   if (!prior_lens || !row_starts || !block_table)
     return set_error(LIBRA_E_INVAL, "prior_lens, row_starts or block_table is NULL");
   if (bt_stride < 1) return set_error(LIBRA_E_INVAL, "bt_stride must be positive");

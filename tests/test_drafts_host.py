@@ -34,6 +34,7 @@ MAP = dict(batch=3, prior=P, new=P, held=P, table=P, stride=4, free=P, capacity=
 @pytest.mark.parametrize("change,want", [
     (dict(batch=-1), INVAL), (dict(stride=-1), INVAL), (dict(capacity=-1), INVAL), (dict(rows=-1), INVAL),
     (dict(rows=2 ** 31), UNSUPPORTED), (dict(capacity=2 ** 31), UNSUPPORTED),
+    (dict(batch=2 ** 30 + 1), UNSUPPORTED),
     *[({k: None}, INVAL) for k in ("prior", "new", "held", "table", "free", "num_free", "slots", "positions",
                                    "starts", "held_out", "num_out", "refused")],
     *[({k: P + 2}, INVAL) for k in ("prior", "new", "held", "table", "free", "num_free", "depths",
@@ -48,7 +49,7 @@ ACCEPT = dict(layout=None, batch=3, prior=P, accepted=P, most=4, counts=P, table
 
 @pytest.mark.parametrize("change,want", [
     (dict(layout=0), INVAL), (dict(batch=-1), INVAL), (dict(most=-1), INVAL), (dict(stride=-1), INVAL),
-    (dict(batch=2 ** 30), UNSUPPORTED),
+    (dict(batch=2 ** 30), UNSUPPORTED), (dict(most=2 ** 30 + 1), UNSUPPORTED),
     *[({k: None}, INVAL) for k in ("prior", "accepted", "counts", "table")],
     (dict(batch=0), 0), (dict(most=0), 0)])
 def test_accept_refuses(handles, change, want):
@@ -157,7 +158,8 @@ TREE = dict(layout=None, q=P, rows=5, prior=P, starts=P, mask=P, words=1, table=
     (dict(words=0), INVAL), (dict(words=9), UNSUPPORTED), (dict(mask=None), INVAL), (dict(q=None), INVAL),
     (dict(out=None), INVAL), (dict(q=P + 8), INVAL), (dict(out=P + 8), INVAL), (dict(prior=None), INVAL),
     (dict(starts=None), INVAL), (dict(table=None), INVAL), (dict(stride=0), INVAL), (dict(ws=None), INVAL),
-    (dict(ws=P + 128), INVAL), (dict(ws_bytes=1 << 20), WORKSPACE), (dict(rows=0), 0), (dict(batch=0), 0)])
+    (dict(ws=P + 128), INVAL), (dict(ws_bytes=1 << 20), WORKSPACE), (dict(rows=0), 0), (dict(batch=0), 0),
+    (dict(out=P), INVAL), (dict(batch=2 ** 30 + 1), UNSUPPORTED)])
 def test_tree_refuses(handles, change, want):
     a = dict(dict(TREE, layout=handles[0]), **change)
     assert status("libra_tree_attn", *a.values()) == want
