@@ -5,10 +5,10 @@
 // The table's kernel is one workgroup: requests 1,024 at a time, one to a thread, whose page counts
 // are added up by scans, and then the pages that move, each found by a search in the scans' sums, so
 // that an ended request of thousands of pages is everybody's work.  Pages given back are pushed
-// before any is taken.  64 requests of a token each: 7 us of kernel with cold caches, of which 3 are
-// the launch; 256 trees of which 9 ended (3,900 pages): 14 us, and 5 for their 8,500 rows, which a
-// launch of their own maps (one workgroup alone took 26 for both).  Accepted tokens: 2,200 of 8 heads
-// (17 MB) 12 us, bound by the V tiles' lines, as a value of a token is two bytes of every 16.
+// before any is taken.  64 requests of a token each: 7 us of kernel with cold caches; 256 trees of
+// which 9 ended: 14 us, and 5 for their 8,500 rows, which a launch of their own maps.  Accepted
+// tokens: 2,157 of 8 heads (16.6 MB) 12 us, 22 with cold caches, bound by the V tiles' lines, as a
+// value of a token is two bytes of every 16.
 #include <algorithm>
 #include <climits>
 

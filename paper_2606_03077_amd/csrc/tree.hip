@@ -32,8 +32,8 @@
 // 319 us, 6.3 TB/s (a plain streaming read 7.0); 32 sequences of 4,000 tokens, 0.52 GB, 93 us with
 // 16 rows, 5.6 TB/s, of which some 9 are the time until the first copies land, and 120 with 128 rows,
 // whose scores and probabilities take as long as the copies.  256 rows: the matrix cores beside the
-// reads, 790-820 TFLOP/s (32 sequences of 8,192 tokens, 64 nodes, 4 heads to a KV head: 340 us; 272
-// without the copies).  The next step's scores among this step's products took wide trees from 411
+// reads, 775-820 TFLOP/s (32 sequences of 8,192 tokens, 64 nodes, 4 heads to a KV head: 337-353 us;
+// 272 without the copies).  The next step's scores among this step's products took wide trees from 411
 // to 333 us, a higher wave priority there than at probabilities this form from 383 to 349.
 // Non-temporal copies, whose lines displace nothing: 93 us instead of 166 with 16 rows, 165 instead of
 // 200 with 256.
@@ -59,7 +59,7 @@ constexpr int kStepKeys = 32;
 // many short items otherwise end last (trees of a 7B-class step 139 us at 0, 132 at 4, 128 at 6, 131
 // at 9; wide ones 322, 300, 307, 292; few long ones alike).
 constexpr int kItemCost = 6;
-constexpr int kTau = 8;
+constexpr int kTau = 8;  // a sum's exponent in base 2 from which the running maximum moves
 constexpr float kSumTau = float(1 << kTau);
 constexpr int kMaskWords = LIBRA_MAX_MASK_WORDS;
 constexpr int kPartBlock = 32 * kDim / 4;  // 32 rows of a part, in fours of floats
