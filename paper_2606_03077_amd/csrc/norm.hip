@@ -6,9 +6,9 @@
 // bound by HBM.  A workgroup takes rows in turns and keeps its part of dw in registers, eight
 // channels a thread; the parts go to the workspace, and a second launch adds them in a fixed order.
 //
-// 16,381 rows of 40 query and 8 key heads (bf16, 604 MB): 117 us, 5.1 TB/s (a large copy 4.9), and 7.6
-// for the second launch, which is a chain of a launch, one round of loads and a reduction.  Four heads'
-// loads at once took the first launch from 164 us to 117, 1,024 threads to 16 channels the second
+// 16,381 rows of 40 query and 8 key heads (bf16, 604 MB): 124 us, 4.9 TB/s, as a large copy, and 5 for
+// the second launch, which is a chain of a launch, one round of loads and a reduction.  Four heads'
+// loads at once took the first launch from 164 us to 118, 1,024 threads to 16 channels the second
 // from 22 to 8.
 #include <algorithm>
 #include <type_traits>
@@ -21,7 +21,10 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kMaxPairs = kMaxRotaryDim / 2;
-constexpr int kMaxParts = 1024;  // workgroups of one tensor
+// Workgroups of one tensor: with both, four to a CU, which run at once.  With 256, 512 and 1,024 of them
+// the whole pass (40 / 8 heads of bf16) took 29.4, 27.3 and 30.9 us at 1,021 rows, 78, 65 and 67 at
+// 4,093, 259, 201 and 199 at 16,381; 1,024 divided by the tensors' heads 30, 72 and 222.
+constexpr int kMaxParts = 512;
 // Bytes of dx from which nothing goes through the caches.  40 / 8 heads of bf16 between copies that
 // write x and dy and read dx, all three, past and through the caches: 2,003 rows (25 MB) 94 and 92
 // us, 4,093 150 and 150, 8,191 298 and 308, 10,007 353 and 366; with cold caches 36 and 45 a launch at
