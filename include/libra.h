@@ -633,10 +633,10 @@ typedef struct libra_norm_heads {
  *   n = x / sqrt(mean(x^2) + eps) over the head's channels,  u = weight n,  y = u turned as by
  *   libra_rotary_apply (channels past R: y = u),
  *
- * in float32 (a head whose squares exceed float32 gives 0), rounded once to y's type.  eps > 0.
- * dtype: LIBRA_DTYPE_BF16, _FP16 or _FP32, of x and out, which are aligned to it; weight_dtype: any
- * of these.  positions: device int32 [rows].  out may be x (the same strides), otherwise they must
- * not overlap.  q or k may be NULL. */
+ * in float32 (a head whose squares exceed float32 gives 0), rounded once to y's type.  eps: positive,
+ * and no subnormal number.  dtype: LIBRA_DTYPE_BF16, _FP16 or _FP32, of x and out, which are aligned to
+ * it; weight_dtype: any of these.  positions: device int32 [rows].  out may be x (the same strides),
+ * otherwise they must not overlap.  q or k may be NULL. */
 libra_status libra_qk_norm_rotary(libra_rotary rotary, int32_t dtype, int32_t weight_dtype, float eps,
                                   const int32_t* positions, int64_t rows, int32_t head_dim,
                                   const libra_norm_heads* q, const libra_norm_heads* k, void* stream);

@@ -1,6 +1,8 @@
 // Entry points of the drafted step's operators (declared and documented in include/libra.h).
+#include <cfloat>
 #include <climits>
 #include <cmath>
+#include <initializer_list>
 #include <string>
 
 #include "drafts.h"
@@ -18,8 +20,17 @@ bool known_dtype(int32_t d) {
 }
 size_t dtype_size(int32_t d) { return d == LIBRA_DTYPE_FP32 ? 4 : 2; }
 
+// Whether the arrays (of 32-bit values; some may be NULL) are aligned, with the error set if not.
+bool int32_arrays(std::initializer_list<const void*> arrays) {
+  for (const void* p : arrays)
+    if (!aligned_to(p, 4)) return set_error(LIBRA_E_INVAL, "32-bit arrays must be 4-byte aligned"), false;
+  return true;
+}
+
 libra_status check_eps(float eps) {
-  if (!(eps > 0.f) || !std::isfinite(eps)) return set_error(LIBRA_E_INVAL, "eps must be positive and finite");
+  // Below the normal numbers v_rsq_f32 takes 0 for it, and a head of zeros would give NaN.
+  if (!(eps >= FLT_MIN) || !std::isfinite(eps))
+    return set_error(LIBRA_E_INVAL, "eps must be positive, finite and no subnormal number");
   return LIBRA_OK;
 }
 
@@ -108,13 +119,9 @@ libra_status libra_kv_map(int32_t batch, const int32_t* prior_lens, const int32_
     return set_error(LIBRA_E_INVAL, "a per-request array is NULL");
   if (free_capacity > 0 && !free_pages) return set_error(LIBRA_E_INVAL, "free_pages is NULL");
   if (rows > 0 && (!slots || !positions)) return set_error(LIBRA_E_INVAL, "slots or positions is NULL");
-  for (const void* p : {static_cast<const void*>(prior_lens), static_cast<const void*>(new_lens),
-                        static_cast<const void*>(held_pages), static_cast<const void*>(block_table),
-                        static_cast<const void*>(free_pages), static_cast<const void*>(num_free),
-                        static_cast<const void*>(depths), static_cast<const void*>(positions),
-                        static_cast<const void*>(row_starts), static_cast<const void*>(held_out),
-                        static_cast<const void*>(num_free_out), static_cast<const void*>(refused)})
-    if (!aligned_to(p, 4)) return set_error(LIBRA_E_INVAL, "int32 arrays must be 4-byte aligned");
+  if (!int32_arrays({prior_lens, new_lens, held_pages, block_table, free_pages, num_free, depths, positions,
+                     row_starts, held_out, num_free_out, refused}))
+    return LIBRA_E_INVAL;
   if (!aligned_to(slots, 8)) return set_error(LIBRA_E_INVAL, "slots must be 8-byte aligned");
   const MapArgs a{prior_lens, new_lens, held_pages, block_table, bt_stride, free_pages, free_capacity,
                   num_free, depths, slots, positions, row_starts, held_out, num_free_out, refused,
@@ -134,6 +141,7 @@ libra_status libra_kv_accept(libra_kv_layout layout, int32_t batch, const int32_
   if (batch < 0 || max_accepted < 0 || bt_stride < 0)
     return set_error(LIBRA_E_INVAL, "batch / max_accepted / bt_stride < 0");
   if (batch == 0 || max_accepted == 0 || bt_stride == 0) return LIBRA_OK;
+  if (!int32_arrays({prior_lens, accepted, counts, block_table})) return LIBRA_E_INVAL;
   const int32_t hkv = layout->desc.num_kv_heads;
   if (int64_t(batch) * hkv > INT32_MAX)
     return set_error(LIBRA_E_UNSUPPORTED, "batch * num_kv_heads must be < 2^31");
@@ -287,6 +295,7 @@ libra_status libra_tree_attn(libra_kv_layout layout, const void* q, int64_t rows
   if (q == out) return set_error(LIBRA_E_INVAL, "q and out must be apart");
   if (!prior_lens || !row_starts || !block_table)
     return set_error(LIBRA_E_INVAL, "prior_lens, row_starts or block_table is NULL");
+  if (!int32_arrays({prior_lens, row_starts, mask, block_table, lse})) return LIBRA_E_INVAL;
   if (bt_stride < 1) return set_error(LIBRA_E_INVAL, "bt_stride must be positive");
   if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256)
     return set_error(LIBRA_E_INVAL, "workspace is NULL or not 256-byte aligned");

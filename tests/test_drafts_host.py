@@ -51,6 +51,7 @@ ACCEPT = dict(layout=None, batch=3, prior=P, accepted=P, most=4, counts=P, table
     (dict(layout=0), INVAL), (dict(batch=-1), INVAL), (dict(most=-1), INVAL), (dict(stride=-1), INVAL),
     (dict(batch=2 ** 30), UNSUPPORTED), (dict(most=2 ** 30 + 1), UNSUPPORTED),
     *[({k: None}, INVAL) for k in ("prior", "accepted", "counts", "table")],
+    *[({k: P + 2}, INVAL) for k in ("prior", "accepted", "counts", "table")],
     (dict(batch=0), 0), (dict(most=0), 0)])
 def test_accept_refuses(handles, change, want):
     a = dict(dict(ACCEPT, layout=handles[0]), **change)
@@ -75,7 +76,7 @@ def norm_status(handles, backward, change={}, q={}, k={}, ws=P, ws_bytes=1 << 30
 @pytest.mark.parametrize("backward", [False, True])
 @pytest.mark.parametrize("change,want", [
     (dict(rotary=None), INVAL), (dict(dim=64), INVAL), (dict(dtype=3), UNSUPPORTED),
-    (dict(weight_dtype=-1), UNSUPPORTED), (dict(eps=0.0), INVAL), (dict(eps=-1.0), INVAL),
+    (dict(weight_dtype=-1), UNSUPPORTED), (dict(eps=0.0), INVAL), (dict(eps=1e-39), INVAL), (dict(eps=-1.0), INVAL),
     (dict(eps=float("nan")), INVAL), (dict(eps=float("inf")), INVAL), (dict(rows=-1), INVAL),
     (dict(rows=2 ** 31), UNSUPPORTED), (dict(positions=None), INVAL)])
 def test_norm_refuses(handles, backward, change, want):
@@ -129,7 +130,7 @@ APPEND = dict(layout=None, rotary=None, weight_dtype=0, eps=1e-6, positions=P, s
 
 @pytest.mark.parametrize("change,want", [
     (dict(layout=None), INVAL), (dict(rotary=None), INVAL), (dict(weight_dtype=9), UNSUPPORTED),
-    (dict(eps=0.0), INVAL), (dict(rows=-1), INVAL), (dict(rows=2 ** 31), UNSUPPORTED),
+    (dict(eps=0.0), INVAL), (dict(eps=1e-39), INVAL), (dict(rows=-1), INVAL), (dict(rows=2 ** 31), UNSUPPORTED),
     (dict(q=None), INVAL), (dict(q_out=None), INVAL), (dict(q_weight=None), INVAL),
     (dict(k_weight=None), INVAL), (dict(k_weight=P + 1), INVAL), (dict(hkv=4), INVAL),
     (dict(slots=None), INVAL), (dict(positions=None), INVAL), (dict(k=None), INVAL), (dict(v=P + 8), INVAL),
@@ -159,7 +160,8 @@ TREE = dict(layout=None, q=P, rows=5, prior=P, starts=P, mask=P, words=1, table=
     (dict(out=None), INVAL), (dict(q=P + 8), INVAL), (dict(out=P + 8), INVAL), (dict(prior=None), INVAL),
     (dict(starts=None), INVAL), (dict(table=None), INVAL), (dict(stride=0), INVAL), (dict(ws=None), INVAL),
     (dict(ws=P + 128), INVAL), (dict(ws_bytes=1 << 20), WORKSPACE), (dict(rows=0), 0), (dict(batch=0), 0),
-    (dict(out=P), INVAL), (dict(batch=2 ** 30 + 1), UNSUPPORTED)])
+    (dict(out=P), INVAL), (dict(batch=2 ** 30 + 1), UNSUPPORTED),
+    *[({k: P + 2}, INVAL) for k in ("prior", "starts", "mask", "table", "lse")]])
 def test_tree_refuses(handles, change, want):
     a = dict(dict(TREE, layout=handles[0]), **change)
     assert status("libra_tree_attn", *a.values()) == want
