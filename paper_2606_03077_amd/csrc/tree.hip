@@ -3,7 +3,7 @@
 //
 // Lengths are read on the GPU, so the launch divides the work itself.  A KV head's N G (node, head)
 // rows are cut into tiles of M = 32 kWaves rows, an item is a tile over all P + N keys, and a step
-// is 32 keys of an item.  With U units in all, one a step and kItemCost before each item's first,
+// is 32 keys of an item.  With U units in all, one a step and item_cost before each item's first,
 // workgroup w takes those of the units [w q, (w + 1) q) in the items' order that are steps, q =
 // ceil(U / workgroups): some whole items, and at most a part of one before and of one behind them.
 // Parts are float32 results, normalised, with their log-sum-exps in slots 2 w (an item begun by
@@ -55,10 +55,6 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kStepKeys = 32;
-// What an item costs besides its steps (queries, masked steps, results), in steps: ranges that span
-// many short items otherwise end last (trees of a 7B-class step 139 us at 0, 132 at 4, 128 at 6, 131
-// at 9; wide ones 322, 300, 307, 292; few long ones alike).
-constexpr int kItemCost = 6;
 constexpr int kTau = 8;  // a sum's exponent in base 2 from which the running maximum moves
 constexpr float kSumTau = float(1 << kTau);
 constexpr int kMaskWords = LIBRA_MAX_MASK_WORDS;
@@ -108,6 +104,7 @@ struct TreeArgs {
   uint32_t last_page;
   int rows, most;  // query rows, tokens that a row of the block table can hold
   int batch, hkv, hq, group, mask_words;
+  int item_cost;  // units
   float sl2;
 };
 
@@ -169,17 +166,17 @@ struct Cursor {
     for (int b0 = 0; b0 < A.batch; b0 += 64) {
       window.load(A, b0, lane);
       window.count(A, lane, items, steps);
-      total += wave_sum(steps + kItemCost * items);
+      total += wave_sum(steps + A.item_cost * items);
     }
     each = (total + groups - 1) / groups;
     const int64_t begin = w * each, end = min(begin + each, total);
     if (begin >= total) return 0;
-    // Steps before a place in the ranges' units: of an item, kItemCost units and then its steps.
+    // Steps before a place in the ranges' units: of an item, A.item_cost units and then its steps.
     int64_t before = 0, steps_before = 0, first_step = -1;
     for (int b0 = 0; b0 < A.batch; b0 += 64) {
       if (window.first != b0) window.load(A, b0, lane);
       window.count(A, lane, items, steps);
-      int64_t upto = steps + kItemCost * items, upto_steps = steps;
+      int64_t upto = steps + A.item_cost * items, upto_steps = steps;
       const int64_t cost = upto;
 #pragma unroll
       for (int n = 1; n < 64; n <<= 1) {
@@ -192,9 +189,9 @@ struct Cursor {
         at_b = uniform(b0 + l);
         seq = window.get(A, at_b, lane);
         const int64_t in_seq = unit - before - uniform64(__shfl(upto - cost, l));
-        const int item_units = seq.steps + kItemCost;
+        const int item_units = seq.steps + A.item_cost;
         at_item = uniform(int(in_seq / item_units));
-        at_step = max(uniform(int(in_seq - int64_t(at_item) * item_units)) - kItemCost, 0);
+        at_step = max(uniform(int(in_seq - int64_t(at_item) * item_units)) - A.item_cost, 0);
         return steps_before + uniform64(__shfl(upto_steps - steps, l)) + int64_t(at_item) * seq.steps + at_step;
       };
       const int64_t here = before + uniform64(__shfl(upto, 63));
@@ -784,9 +781,21 @@ __global__ __launch_bounds__(kMergeThreads) void tree_merge_kernel(TreeArgs A, i
 // tokens and 8 KV heads, with four and with eight waves: 32 rows 105 and 106 us, 64 rows 117 and 116,
 // 128 rows 131 and 132, 132 rows 215 and 147, 256 rows 238 and 192; trees of a 7B-class step, 35 to
 // 112 rows, 138 and 145; one sequence of 16,000 tokens, whose parts are fewer with eight, 47 and 38.
+int64_t mean_rows(int64_t rows, int32_t batch, int32_t group) {
+  return (rows + std::max(batch, 1) - 1) / std::max(batch, 1) * group;
+}
 int waves_of(int64_t rows, int32_t batch, int32_t group) {
-  const int64_t mean = (rows + std::max(batch, 1) - 1) / std::max(batch, 1) * group;
+  const int64_t mean = mean_rows(rows, batch, group);
   return mean > 64 && mean <= 128 ? 4 : 8;
+}
+
+// What an item costs besides its steps (queries, masked steps, results), in steps: ranges that span
+// many short items otherwise end last.  A pass (attention and merge) at 6, 8, 10 and 12: 256 rows,
+// requests of 4,096 tokens at the median 276, 274, 269 and 269 us, others of such lengths 283, 278, 276 and
+// 276, 160 rows 223, 221, 219 and 220; trees of a 7B-class step 124, 124, 125 and 125, small trees 13.5
+// at 6 and 13.9 at 9, 64 requests of 50-600 tokens 33.1 and 34.5.
+int item_cost(int64_t rows, int32_t batch, int32_t group) {
+  return mean_rows(rows, batch, group) > 128 ? 10 : 6;
 }
 
 TreeArgs tree_args(const KvLayout& L, const TreeCall& c, int waves) {
@@ -805,6 +814,7 @@ TreeArgs tree_args(const KvLayout& L, const TreeCall& c, int waves) {
   A.rows = int(c.rows);
   A.most = int(std::min<int64_t>(c.stride * kPage, INT32_MAX - 64));
   A.last_page = uint32_t(std::min<int64_t>(L.desc.num_pages - 1, INT32_MAX));
+  A.item_cost = item_cost(c.rows, c.batch, c.hq / L.desc.num_kv_heads);
   A.batch = c.batch, A.hkv = L.desc.num_kv_heads, A.hq = c.hq, A.group = c.hq / A.hkv;
   A.sl2 = c.scale * kLog2e;
   return A;
