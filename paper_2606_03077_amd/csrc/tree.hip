@@ -842,9 +842,10 @@ hipError_t launch_tree_merge(const KvLayout& L, const TreeCall& c, hipStream_t s
   const int rows = 32 * waves, groups = groups_of(waves);
   // Items, at most, and with them the parts of one, about.
   const int64_t items = A.hkv * (int64_t(c.batch) + c.rows * A.group / rows);
+  const int live = int(std::min<int64_t>(rows, c.rows * A.group));  // of a tile, at most
   auto launch = [&](auto kernel, int64_t x, int per_row) {
-    hipLaunchKernelGGL(kernel, dim3(unsigned(x), unsigned(rows * per_row / kMergeGroups)), dim3(kMergeThreads), 0, s, A,
-                       groups, rows);
+    const int y = (live * per_row + kMergeGroups - 1) / kMergeGroups;
+    hipLaunchKernelGGL(kernel, dim3(unsigned(x), unsigned(y)), dim3(kMergeThreads), 0, s, A, groups, rows);
     return hipGetLastError();
   };
   // Groups of 16 threads to a row: 1, 4 and 16 took for 256 items of 256 rows 17, 37 and 179 us (with
