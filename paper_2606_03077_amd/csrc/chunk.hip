@@ -406,7 +406,9 @@ void chunk_kernel(std::conditional_t<kLow != 0, ChunkRotaryArgs, ChunkArgs> A) {
   // rare).  Pages past the end re-read the last page (the id row is padded with it); their
   // keys are >= kv1, so they are masked and their V zeroed.  The wave index is made scalar,
   // so the page, the LDS targets and the byte offsets are scalar arithmetic.  Two
-  // vector-memory operations per wave and call, in a fixed order; the waits count them.
+  // vector-memory operations per wave and call, in a fixed order; the waits count them.  The
+  // s_nop: a load to LDS needs a wait state after the write of the m0 that it reads, which the
+  // compiler does not put inside an asm block.
   auto tile_off = [&](int id) -> uint64_t { return uint64_t(uint32_t(id)) * page_bytes; };
   auto page_off = [&](int step) -> uint64_t {
     const int p = step * kStepPages + wpage;
@@ -419,7 +421,7 @@ void chunk_kernel(std::conditional_t<kLow != 0, ChunkRotaryArgs, ChunkArgs> A) {
       const int i = (2 * wave + c2) & 3;
       const uint32_t d = uint32_t(reinterpret_cast<uintptr_t>(&dst[wpage][i * 64]));
       const char* s = src + (off + i * 1024);
-      asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, off"
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off"
                    :
                    : "s"(d), "v"(s)
                    : "memory", "m0");

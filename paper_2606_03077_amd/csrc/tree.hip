@@ -384,9 +384,11 @@ __device__ __forceinline__ void load_query(const TreeArgs& A, const Seq& s, int 
       bits[i] = ok ? A.mask[size_t(s.row0 + node) * A.mask_words + i] : 0;
 }
 
-// One int per lane straight into LDS, lane after lane.
+// One int per lane straight into LDS, lane after lane.  The s_nop: a load to LDS may read an m0 that the
+// instruction right before it writes too early; one wait state is needed, which the compiler puts
+// between its own instructions, but not inside an asm block.
 __device__ __forceinline__ void copy_lds_dword(const int32_t* src, int32_t* dst) {
-  asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dword %1, off"
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, off"
                :
                : "s"(uniform(int(reinterpret_cast<uintptr_t>(dst)))), "v"(src)
                : "memory", "m0");
@@ -493,7 +495,7 @@ void tree_ring_kernel(TreeArgs A) {
     const int stage = uniform(int(reinterpret_cast<uintptr_t>(&ring[copied % kStages][0][0])));
 #pragma unroll
     for (int c = 0; c < kCopies; ++c) {
-      asm volatile("s_mov_b32 m0, %0\n\tglobal_load_lds_dwordx4 %1, %2 nt"
+      asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2 nt"
                    :
                    : "s"(stage + (piece0 + c) * 1024), "v"(lane_bytes), "s"(my_cache + at_page + c * 1024)
                    : "memory", "m0");
