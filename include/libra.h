@@ -684,8 +684,8 @@ libra_status libra_kv_append_norm(libra_kv_layout layout, libra_rotary rotary, i
  * libra_kv_map refused gives meaningless rows but no fault.
  *
  * workspace: device, 256-byte aligned, at least libra_tree_attn_workspace_bytes(rows, batch,
- * num_q_heads, num_kv_heads) bytes (0: bad arguments), of any contents; calls and graphs may share
- * one if they are ordered.  Results depend on how a launch divides the work (their last bits change
+ * num_q_heads, num_kv_heads) bytes (0: bad arguments), of any contents; what is enough for some rows
+ * and batch is enough for fewer of either.  Calls and graphs may share one if they are ordered.  Results depend on how a launch divides the work (their last bits change
  * with the other requests' lengths), and are the same for the same call. */
 size_t libra_tree_attn_workspace_bytes(int64_t rows, int32_t batch, int32_t num_q_heads,
                                        int32_t num_kv_heads);

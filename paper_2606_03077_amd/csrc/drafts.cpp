@@ -265,7 +265,7 @@ libra_status libra_kv_append_norm(libra_kv_layout layout, libra_rotary rotary, i
 size_t libra_tree_attn_workspace_bytes(int64_t rows, int32_t batch, int32_t num_q_heads,
                                        int32_t num_kv_heads) {
   if (rows < 0 || batch < 0 || num_q_heads <= 0 || num_kv_heads <= 0 || num_q_heads % num_kv_heads) return 0;
-  return tree_workspace(rows, batch, num_q_heads, num_kv_heads);
+  return tree_workspace();
 }
 
 libra_status libra_tree_attn(libra_kv_layout layout, const void* q, int64_t rows,
@@ -299,7 +299,7 @@ libra_status libra_tree_attn(libra_kv_layout layout, const void* q, int64_t rows
   if (bt_stride < 1) return set_error(LIBRA_E_INVAL, "bt_stride must be positive");
   if (!workspace || reinterpret_cast<uintptr_t>(workspace) % 256)
     return set_error(LIBRA_E_INVAL, "workspace is NULL or not 256-byte aligned");
-  if (ws_bytes < tree_workspace(rows, batch, num_q_heads, hkv))
+  if (ws_bytes < tree_workspace())
     return set_error(LIBRA_E_WORKSPACE, "workspace smaller than libra_tree_attn_workspace_bytes");
   const TreeCall c{q, rows, prior_lens, row_starts, mask, mask_words, block_table, bt_stride, batch,
                    num_q_heads, scale, workspace, out, lse};

@@ -96,7 +96,7 @@ struct TreeCall {
   void* out;
   float* lse;
 };
-size_t tree_workspace(int64_t rows, int32_t batch, int32_t hq, int32_t hkv);
+size_t tree_workspace();
 // The attention, and the merge of the parts of items that workgroups share.
 hipError_t launch_tree(const KvLayout& L, const TreeCall& c, hipStream_t s);
 hipError_t launch_tree_merge(const KvLayout& L, const TreeCall& c, hipStream_t s);

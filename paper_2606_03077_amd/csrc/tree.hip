@@ -824,9 +824,12 @@ TreeArgs tree_args(const KvLayout& L, const TreeCall& c, int waves) {
 
 }  // namespace
 
-size_t tree_workspace(int64_t rows, int32_t batch, int32_t hq, int32_t hkv) {
-  const int waves = waves_of(rows, batch, hq / hkv);
-  return size_t(groups_of(waves)) * (size_t(2) * 32 * waves * (kDim + 1) * sizeof(float) + sizeof(Split));
+// One size for both forms, so that a workspace for the largest step is enough for every smaller one:
+// their parts take the same bytes (groups_of(waves) * waves is fixed), the records those of more groups.
+size_t tree_workspace() {
+  constexpr size_t part_rows = size_t(2) * groups_of(8) * 32 * 8;
+  static_assert(part_rows == size_t(2) * groups_of(4) * 32 * 4 && groups_of(4) > groups_of(8));
+  return part_rows * (kDim + 1) * sizeof(float) + groups_of(4) * sizeof(Split);
 }
 
 hipError_t launch_tree(const KvLayout& L, const TreeCall& c, hipStream_t s) {
