@@ -644,9 +644,10 @@ libra_status libra_qk_norm_rotary(libra_rotary rotary, int32_t dtype, int32_t we
 /* Its gradient's pass.  With dy turned back (the negative angle, the same amplitude) to du:
  *
  *   dx = (weight du - n mean(weight du n)) / sqrt(mean(x^2) + eps),
- *   weight_grad = sum over rows and heads of du n (float32, overwritten; 0 where there are no rows).
+ *   weight_grad = sum over rows and heads of du n (float32, overwritten; 0 where there are no rows)
  *
- * The sums' order is fixed by the sizes, so equal calls give equal bits.  out may be x or grad (the
+ * (a head whose squares exceed float32 gives dx = 0 and adds nothing to weight_grad).  The sums'
+ * order is fixed by the sizes, so equal calls give equal bits.  out may be x or grad (the
  * same strides).  workspace: device, 16-byte aligned, libra_qk_norm_rotary_workspace_bytes of it
  * for weight gradients (not read without); calls that may overlap need one each. */
 size_t libra_qk_norm_rotary_workspace_bytes(int64_t rows, int32_t num_q_heads, int32_t num_k_heads,

@@ -3,7 +3,8 @@
 //   du = R^T dy,  dw = sum over rows and heads of du n,
 //   dx = r (w du - n mean(w du n)) = r (w du - x r^2 mean(w du x)).
 // x^2 and w du x are summed over a head together, so x and dy are read once and dx written once:
-// bound by HBM.  A workgroup takes rows in turns and keeps its part of dw in registers, eight
+// bound by HBM.  Where the second sum leaves float32's range (heads whose norm does, and where n is 0,
+// or gradients of 1e19) that of w du n takes its place.  A workgroup takes rows in turns and keeps its part of dw in registers, eight
 // channels a thread; the parts go to the workspace, and a second launch adds them in a fixed order.
 //
 // 16,381 rows of 40 query and 8 key heads (bf16, 604 MB): 124 us, 4.9 TB/s, as a large copy, and 5 for
@@ -113,7 +114,15 @@ __device__ __forceinline__ void back_wide(const RotaryArgs<kMaxPairs>& rot, cons
 #pragma unroll
           for (int e = 0; e < 4; ++e) along = __builtin_fmaf(v[e] * wb[e], g[e], along);
           const float s = norm_scale(group_sum(squares, per_head), C.dim, A.norm.eps);
-          const float m = group_sum(along, per_head) * s / float(C.dim);  // mean(w du n)
+          float m = group_sum(along, per_head) * s / float(C.dim);  // mean(w du n)
+          if (!__builtin_isfinite(m)) {  // the same in a head's threads
+            float t = 0.f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) t = __builtin_fmaf(u[e] * wa[e], f[e] * s, t);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) t = __builtin_fmaf(v[e] * wb[e], g[e] * s, t);
+            m = group_sum(t, per_head) / float(C.dim);
+          }
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
             const float n = f[e] * s, o = g[e] * s;
@@ -196,7 +205,14 @@ __device__ __forceinline__ void back_any(const RotaryArgs<kMaxPairs>& rot, const
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
     const float s = norm_scale(group_sum(squares, 64), C.dim, A.norm.eps);
-    const float m = group_sum(along, 64) * s / float(C.dim);
+    float m = group_sum(along, 64) * s / float(C.dim);
+    if (!__builtin_isfinite(m)) {
+      float t = 0.f;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i)
+        if (lane + 64 * i < C.dim) t = __builtin_fmaf(du[i] * norm_weight(A.norm, lane + 64 * i), f[i] * s, t);
+      m = group_sum(t, 64) / float(C.dim);
+    }
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
       const int d = lane + 64 * i;
