@@ -273,8 +273,21 @@ hipError_t launch_kv_map(const MapArgs& a, hipStream_t s) {
 }
 
 hipError_t launch_kv_accept(const AcceptArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL(kv_accept_kernel, dim3(unsigned(a.batch) * unsigned(a.hkv)), dim3(256), 0, s, a);
-  return hipGetLastError();
+  // A launch's threads are counted in 32 bits, and one of more runs a part of them without an error.
+  constexpr int64_t kMaxBlocks = int64_t(1) << 22;
+  const int64_t step = kMaxBlocks / a.hkv;
+  for (int64_t b0 = 0; b0 < a.batch; b0 += step) {
+    AcceptArgs part = a;
+    part.batch = int32_t(std::min(step, a.batch - b0));
+    part.prior += b0;
+    part.accepted += b0 * a.most;
+    part.counts += b0;
+    part.table += b0 * a.stride;
+    hipLaunchKernelGGL(kv_accept_kernel, dim3(unsigned(part.batch) * unsigned(a.hkv)), dim3(256), 0, s, part);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
 }
 
 }  // namespace libra
