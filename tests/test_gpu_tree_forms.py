@@ -11,7 +11,7 @@ import tree_codes
 from paper_2606_03077_amd import libra
 
 from test_gpu_kv_append import Cache
-from test_gpu_tree import I32, SCALE, f64, run, tree_masks
+from test_gpu_tree import I32, SCALE, Step, f64, run, tree_masks
 
 pytestmark = pytest.mark.gpu
 
@@ -42,6 +42,38 @@ def test_one_long_context_among_short_ones():
     """An item of far more parts than the others, which the merge joins, with one and more KV heads."""
     for hkv in (1, 2, 8):
         run([70, 30, 40, 300, 9000, 61, 0, 90], [3, 9, 1, 4, 5, 2, 8, 3], 4 * hkv, hkv)
+
+
+def test_chains_of_many_tokens():
+    """Without a mask a request may have any number of nodes: a prompt's."""
+    run([77, 0], [700, 1100], 2, 1, "chain")
+
+
+def test_requests_without_nodes_around_the_others():
+    """More than 64 of them at a time, before, between and after those that have any."""
+    rng = np.random.default_rng(3)
+    nodes, prior = np.zeros(420, int), rng.integers(0, 50, size=420)
+    for b, n, p in ((70, 3, 5000), (71, 9, 0), (200, 1, 16), (333, 40, 9000)):
+        nodes[b], prior[b] = n, p
+    run(prior.tolist(), nodes.tolist(), 4, 2)
+    run(prior.tolist(), nodes.tolist(), 4, 2, "chain", lse=False)
+
+
+def test_rows_before_the_first_request():
+    """row_starts need not begin at 0; the rows before are left as they were."""
+    s = Step([100, 2000, 3], [5, 70, 9], 8, 2, padding=7)
+    s.call()
+    s.check()
+    want, want_lse = s.out[:84].clone(), s.lse[:84].clone()
+    s.q, s.mask = s.q.roll(4, 0), s.mask.roll(4, 0)
+    s.starts += 4
+    s.out.fill_(5.0), s.lse.fill_(5.0)
+    s.call()
+    torch.cuda.synchronize()
+    assert torch.equal(s.out[4:88].view(torch.int16), want.view(torch.int16)) and torch.equal(s.lse[4:88], want_lse)
+    for t in (s.out, s.lse):
+        assert (t[:4] == 5.0).all() and (t[88:] == 5.0).all()
+    s.close()
 
 
 class Coded:
