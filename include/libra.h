@@ -686,8 +686,12 @@ libra_status libra_kv_append_norm(libra_kv_layout layout, libra_rotary rotary, i
  *
  * workspace: device, 256-byte aligned, at least libra_tree_attn_workspace_bytes(rows, batch,
  * num_q_heads, num_kv_heads) bytes (0: bad arguments), of any contents; what is enough for some rows
- * and batch is enough for fewer of either.  Calls and graphs may share one if they are ordered.  Results depend on how a launch divides the work (their last bits change
- * with the other requests' lengths), and are the same for the same call. */
+ * and batch is enough for fewer of either.  Calls and graphs may share one if they are ordered.
+ *
+ * Results are the same for the same call.  Their last bits change with how a launch divides the work,
+ * so with the other requests' lengths, and with the values of the request's other rows under the same
+ * KV head: rows that are computed together move their softmax's offset together.  A row is not the
+ * same bits in every batch. */
 size_t libra_tree_attn_workspace_bytes(int64_t rows, int32_t batch, int32_t num_q_heads,
                                        int32_t num_kv_heads);
 libra_status libra_tree_attn(libra_kv_layout layout, const void* q, int64_t rows,

@@ -6,9 +6,10 @@
 // are added up by scans, and then the pages that move, each found by a search in the scans' sums, so
 // that an ended request of thousands of pages is everybody's work.  Pages given back are pushed
 // before any is taken.  64 requests of a token each: 7 us of kernel with cold caches; 256 trees of
-// which 9 ended: 14 us, and 5 for their 8,500 rows, which a launch of their own maps.  Accepted
-// tokens: 2,157 of 8 heads (16.6 MB) 12 us, 22 with cold caches, bound by the V tiles' lines, as a
-// value of a token is two bytes of every 16.
+// which 9 ended: 14 us, and 5 for their 8,025 rows, which a launch of their own maps.  2,500 requests,
+// taken in turns of 1,024: 30 us a pass of a token each, 80 of trees (45,617 pages move, 77,922 rows).
+// Accepted tokens: 2,157 of 8 heads, of which 2,029 move (16.6 MB), 12 us, 22 with cold caches, bound
+// by the V tiles' lines, as a value of a token is two bytes of every 16.
 #include <algorithm>
 #include <climits>
 
@@ -242,9 +243,10 @@ __global__ __launch_bounds__(256) void kv_accept_kernel(AcceptArgs A) {
   }
 }
 
-// Rows that the one workgroup maps itself, instead of a second launch: 64 requests of a token 10.0
-// against 12.0 us, 16 trees (813 rows) 25.7 against 26.8, 32 (1,300) 29.8 against 28.7, 256 (8,500)
-// 31.3 against 20.9.
+// Rows that the one workgroup maps itself, instead of a second launch: 64 requests of a token 10.1
+// against 12.1 us (with cold caches, and some 4 of two events), trees of 16 requests (620 rows) 10.8
+// against 13.5, of 32 (900) 12.6 against 15.4, of 64 (2,494) 17.7 against 16.7, of 256 (8,025) 31.1
+// against 21.3.
 constexpr int64_t kOneLaunchRows = 1024;
 
 }  // namespace
@@ -256,9 +258,9 @@ hipError_t launch_kv_map(const MapArgs& a, hipStream_t s) {
     return hipGetLastError();
   };
   // Few rows a request, so that few pages move: 512 threads, whose scans are shorter.  With 512 and
-  // 1,024 threads (and some 4 us of two events): 64 requests of a token each 10.2 and 11.6 us, 128
-  // 10.2 and 11.2; trees of up to 64 nodes, 16 requests 19.1 and 14.8, 64 23.5 and 20.5, 256 24.1 and
-  // 20.9.
+  // 1,024 threads (cold caches, and some 4 us of two events): 64 requests of a token each 10.2 and 11.2
+  // us, 512 12.2 and 12.7; trees of up to 64 nodes, 16 requests 11.1 and 10.6, 32 13.5 and 12.6, 64 16.5
+  // and 17.1, 256 23.9 and 21.1.
   // Sums, and a thread's next index behind the last, fit 32 bits.
   const bool small = std::max(a.stride, a.rows + 1) * int64_t(std::max(a.batch, 1)) <= INT32_MAX - 4 * kMapThreads;
   const hipError_t e =

@@ -7,10 +7,10 @@
 // or gradients of 1e19) that of w du n takes its place.  A workgroup takes rows in turns and keeps its part of dw in registers, eight
 // channels a thread; the parts go to the workspace, and a second launch adds them in a fixed order.
 //
-// 16,381 rows of 40 query and 8 key heads (bf16, 604 MB): 124 us, 4.9 TB/s, as a large copy, and 5 for
-// the second launch, which is a chain of a launch, one round of loads and a reduction.  Four heads'
-// loads at once took the first launch from 164 us to 118, 1,024 threads to 16 channels the second
-// from 22 to 8.
+// 16,381 rows of 40 query and 8 key heads (bf16, 604 MB): 124-128 us, 4.7-4.9 TB/s (streams of two reads
+// to a write reach 6.3), and 5 for the second launch, which is a chain of a launch, one round of loads
+// and a reduction.  Four heads' loads at once took the first launch from 164 us to 118, 1,024 threads to
+// 16 channels the second from 22 to 8.
 #include <algorithm>
 #include <type_traits>
 
@@ -161,7 +161,9 @@ __global__ __launch_bounds__(kThreads) void norm_back_wide_kernel(RotaryArgs<kMa
 }
 
 // Any head size, R, alignment: a wave per head, whose values go through LDS, where a channel finds
-// its partner.
+// its partner.  A pass of 4,093 rows of 40 / 8 heads in bf16 (norms, gradients and their sum) takes
+// 268-272 us at head sizes 80 and 96 and at R = 20, 67 in the wide form; 2,047 rows in float32 144-158
+// and 57.  So a head takes the same time whatever its bytes: instructions and their latency bound it.
 template <class T>
 __device__ __forceinline__ void back_any(const RotaryArgs<kMaxPairs>& rot, const BackArgs<T>& A,
                                          const BackCall& C, int block, float (*shared)[kMaxRotaryHead]) {

@@ -15,7 +15,9 @@
 // Heads may be normalised before they are turned (kNorm, norm_*): the sum of squares is a reduction
 // over the lanes that hold the head, so a value is still read and written once.  16,381 rows of 40
 // query and 8 key heads (bf16): alone 76 us, 5.3 TB/s; on their way into the cache 106 us, 4.5 TB/s,
-// where the V tiles' transposition costs LDS conflicts besides; 16 rows 6 us, a chain of loads.
+// where the V tiles' transposition costs LDS conflicts besides; 16 rows 6 us, a chain of loads.  An
+// append whose R is no multiple of 8 is bound by its vector work (cosines of every head and channel,
+// weights one at a time): 267 us at R = 20 in either pairing.
 #include <algorithm>
 #include <type_traits>
 

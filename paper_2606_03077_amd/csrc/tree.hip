@@ -12,31 +12,34 @@
 // same keys share its L2.
 //
 // A step's K and V tiles, two pages, are copied from memory straight into an LDS ring (16 bytes a lane,
-// the tiles as stored) some steps ahead, across the ends of items, and shared by the waves.  Wave w holds 32 of the tile's rows as the columns of
-// its products, on v_mfma_f32_32x32x16_bf16:
+// the tiles as stored) some steps ahead, across the ends of items, and shared by the waves.  Wave w holds
+// 32 of the tile's rows as the columns of its products, on v_mfma_f32_32x32x16_bf16:
 //   S^T[32 keys x 32 rows] = K Q^T: 8 products over the 128 channels; lane (key m, half h) reads K
 //     granule (2 c + h) 16 + m % 16 of page m / 16 and gets the scores of keys 8 (r / 4) + 4 h + r % 4
 //     (r = 0 .. 15) for its row;
 //   O^T[128 channels x 32 rows] += V^T P^T: per page 4 products; a lane's probabilities of a page are
 //     its operand as they come out of the scores, V granule 128 h + d the other.
 // Softmax runs online in base 2 with the running maximum set on an item's first step and moved only
-// when a lane's sum of 16 probabilities exceeds 2^kTau.  Probabilities enter the products as bf16,
-// off by at most 2^-8 of each, their sum is taken in float32 before.
+// when a lane's sum of 16 probabilities exceeds 2^kTau, for the wave's 32 rows together: a row's last
+// bits depend on its neighbours'.  Probabilities enter the products as bf16, off by at most 2^-8 of
+// each, their sum is taken in float32 before.
 //
 // Steps that reach past the cached tokens are masked: a row's 32 bits of them are its mask's, shifted.
 // There the values may be those of nodes that a row does not see, or nothing; where any is not
 // finite, a product of a zero probability would be NaN, and the step takes finite values only
 // and adds the infinities and NaNs of seen nodes one by one (rare).
 //
-// What bounds it.  Up to 128 rows a KV head the reads: four requests of 115,000 tokens, 2.02 GB,
-// 319 us, 6.3 TB/s (a plain streaming read 7.0); 32 sequences of 4,000 tokens, 0.52 GB, 93 us with
-// 16 rows, 5.6 TB/s, of which some 9 are the time until the first copies land, and 120 with 128 rows,
-// whose scores and probabilities take as long as the copies.  256 rows: the matrix cores beside the
-// reads, 775-820 TFLOP/s (32 sequences of 8,192 tokens, 64 nodes, 4 heads to a KV head: 337-353 us;
-// 272 without the copies).  The next step's scores among this step's products took wide trees from 411
-// to 333 us, a higher wave priority there than at probabilities this form from 383 to 349.
-// Non-temporal copies, whose lines displace nothing: 93 us instead of 166 with 16 rows, 165 instead of
-// 200 with 256.
+// What bounds it.  Up to 128 rows a KV head the reads: four requests of 123,000 tokens, 2.02 GB,
+// 320 us, 6.3 TB/s (a plain streaming read 7.1); 32 sequences of 4,000 tokens, 0.53 GB, 92 us with
+// 16 rows, 5.7 TB/s, of which some 9 are the time until the first copies land, and 122 with 128 rows,
+// whose scores and probabilities take as long as the copies.  256 rows (32 sequences of 8,192 tokens,
+// 64 nodes, 4 heads to a KV head): 292-298 us after a fill of other memory, 344 a pass in a row of
+// them, 800-940 TFLOP/s.  There the matrix cores and the reads of LDS: a wave's 32 rows take all of a
+// step's 16 KiB from it, so the eight waves 128 KiB, 1,024 cycles at 128 bytes each, and the products
+// of a SIMD's two waves take 1,024 too.  The next step's scores among this step's products took wide
+// trees from 411 to 333 us; a higher wave priority there than at probabilities takes them from 303 to
+// 290 a pass.  Non-temporal copies, whose lines displace nothing: 92 us instead of 169 with 16 rows,
+// 163 instead of 200 with 256, after a fill of other memory.
 #include <algorithm>
 #include <cfloat>
 #include <climits>
@@ -398,9 +401,9 @@ __device__ __forceinline__ void wave_sync() {  // LDS operations of one wave com
   __builtin_amdgcn_wave_barrier();
 }
 
-// A tile's waves share each step's K and V through LDS.  Eight waves meet every two steps (345 us
-// against 367 every step, 32 x 8,192 tokens), four every step, as two steps would take two
-// more stages.
+// A tile's waves share each step's K and V through LDS.  Eight waves meet every two steps (a pass of
+// 256 rows over 32 x 8,192 tokens 344 us, 365 every step), four every step, as two steps would take
+// two more stages.
 template <int kWaves>
 struct Ring {
   static constexpr int kStages = kWaves;
@@ -779,10 +782,13 @@ __global__ __launch_bounds__(kMergeThreads) void tree_merge_kernel(TreeArgs A, i
 }
 
 // Waves of a workgroup, 32 rows each; waves without rows only copy.  Four where an average sequence
-// has 65 to 128 rows a KV head, eight otherwise.  Attention and merge of 32 sequences of 3,000-5,000
-// tokens and 8 KV heads, with four and with eight waves: 32 rows 105 and 106 us, 64 rows 117 and 116,
-// 128 rows 131 and 132, 132 rows 215 and 147, 256 rows 238 and 192; trees of a 7B-class step, 35 to
-// 112 rows, 138 and 145; one sequence of 16,000 tokens, whose parts are fewer with eight, 47 and 38.
+// has 65 to 128 rows a KV head, eight otherwise.  A pass over 32 sequences of 3,000-5,000 tokens and 8
+// KV heads, with four and with eight waves: 32 rows 98 and 99 us, 64 rows 110 and 109, 128 rows 125 and
+// 136, 132 rows 200 and 150, 256 rows 231 and 185; trees of a 7B-class step, 35 to 112 rows, 125-129
+// and 126; one sequence of 16,000 tokens, whose parts are fewer with eight, 38 and 28.  The mean tells
+// nothing of a batch's largest trees: one of more than 128 rows has two tiles of four waves, which both
+// read its keys and values.  64 requests of a 7B-class step with 1-24 nodes of 8 heads 162 and 154 us,
+// 1-32 of 7 heads 176 and 158, 1-32 of 8 heads 180 and 162.
 int64_t mean_rows(int64_t rows, int32_t batch, int32_t group) {
   return (rows + std::max(batch, 1) - 1) / std::max(batch, 1) * group;
 }
@@ -854,7 +860,10 @@ hipError_t launch_tree_merge(const KvLayout& L, const TreeCall& c, hipStream_t s
     return hipGetLastError();
   };
   // Groups of 16 threads to a row: 1, 4 and 16 took for 256 items of 256 rows 17, 37 and 179 us (with
-  // some 4 of two events), 16 items 12, 9 and 17, 8 items 19, 10 and 13, one 107, 30 and 23.
+  // some 4 of two events), 16 items 12, 9 and 17, 8 items 19, 10 and 13, one 107, 30 and 23.  The number
+  // of items does not tell where one has most of the parts: with a request of 131,072 tokens among 63 of
+  // 512-4,096 and 1, 2, 4 and 8 KV heads the merge takes 31, 60, 35 and 23 us, the attention 38, 64, 122
+  // and 231.
   if (groups <= 4 * items) return launch(tree_merge_kernel<1>, groups, 1);
   if (groups <= 32 * items) return launch(tree_merge_kernel<4>, std::min<int64_t>(items, groups), 4);
   return launch(tree_merge_kernel<16>, std::min<int64_t>(items, groups), 16);
