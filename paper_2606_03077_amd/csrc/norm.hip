@@ -3,9 +3,10 @@
 //   du = R^T dy,  dw = sum over rows and heads of du n,
 //   dx = r (w du - n mean(w du n)) = r (w du - x r^2 mean(w du x)).
 // x^2 and w du x are summed over a head together, so x and dy are read once and dx written once:
-// bound by HBM.  Where the second sum leaves float32's range (heads whose norm does, and where n is 0,
-// or gradients of 1e19) that of w du n takes its place.  A workgroup takes rows in turns and keeps its part of dw in registers, eight
-// channels a thread; the parts go to the workspace, and a second launch adds them in a fixed order.
+// bound by HBM.  Where the second sum leaves float32's range (heads whose squares do, so that n is 0,
+// or gradients of 1e19 and more) that of w du n takes its place.  A workgroup takes rows in turns and
+// keeps its part of dw in registers, eight channels a thread; the parts go to the workspace, and a
+// second launch adds them in a fixed order.
 //
 // 16,381 rows of 40 query and 8 key heads (bf16, 604 MB): 124-128 us, 4.7-4.9 TB/s (streams of two reads
 // to a write reach 6.3), and 5 for the second launch, which is a chain of a launch, one round of loads
